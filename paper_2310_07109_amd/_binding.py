@@ -14,7 +14,10 @@ SC_OK, SC_EINVAL, SC_EUNSUPPORTED, SC_EWORKSPACE, SC_EHIP, SC_ENOSCRATCH = 0, -1
 SC_NOALLOC_SCRATCH_BYTES = 16 << 20
 # bits of sc_validate_desc's result
 SC_VALID_LEN, SC_VALID_POS_RANGE, SC_VALID_POS_ORDER, SC_VALID_POS_UNUSED_FIRST = 1, 2, 4, 8
-SC_F32, SC_BF16 = 0, 1
+SC_F32, SC_BF16, SC_I8 = 0, 1, 2
+SC_ACT_NONE, SC_ACT_GELU = 0, 1
+SC_NORM_LAYER, SC_NORM_RMS = 0, 1
+SC_GATE_NONE, SC_GATE_CHANNEL, SC_GATE_SEQUENCE, SC_GATE_TOKEN = 0, 1, 2, 3
 SC_SCORE_FROM_PARTIALS, SC_SCORE_FROM_BAND_PROBS = 0, 1
 
 _lib = None
@@ -32,6 +35,28 @@ class _Desc(ctypes.Structure):
                 ("window", ctypes.c_int32), ("G", ctypes.c_int32), ("global_pos", ctypes.c_void_p),
                 ("valid_len", ctypes.c_void_p), ("softmax_scale", ctypes.c_float), ("dtype", ctypes.c_int32),
                 ("causal", ctypes.c_int32)]
+
+
+class _LinearDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("n", ctypes.c_int32), ("K", ctypes.c_int32), ("N", ctypes.c_int32),
+                ("valid_len", ctypes.c_void_p), ("x_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("act", ctypes.c_int32)]
+
+
+class _NormDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("n", ctypes.c_int32), ("D", ctypes.c_int32), ("valid_len", ctypes.c_void_p),
+                ("kind", ctypes.c_int32), ("post", ctypes.c_int32), ("pre", ctypes.c_int32),
+                ("gate_mode", ctypes.c_int32), ("eps", ctypes.c_float), ("res_scale", ctypes.c_float),
+                ("dtype", ctypes.c_int32)]
+
+
+class _I8Weight(ctypes.Structure):
+    _fields_ = [("wq", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+
+
+class _LayerI8(ctypes.Structure):
+    _fields_ = [("qkv", _I8Weight), ("o", _I8Weight), ("w1", _I8Weight), ("w2", _I8Weight)] + \
+        [(name, ctypes.c_void_p) for name in ("gate1", "ln1_w", "ln1_b", "gate2", "ln2_w", "ln2_b")]
 
 
 def lib_path() -> str:
@@ -63,7 +88,7 @@ def _open(path):
         raise RuntimeError(f"{path} is missing: build it with `python -m paper_2310_07109_amd.build`")
     L = ctypes.CDLL(path)
     vp, sz, i32, f32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.c_float
-    dp = ctypes.POINTER(_Desc)
+    dp, lp, np_ = ctypes.POINTER(_Desc), ctypes.POINTER(_LinearDesc), ctypes.POINTER(_NormDesc)
     sig = {
         "sc_status_str": (ctypes.c_char_p, [i32]),
         "sc_score_partials_size": (sz, [dp]),
@@ -84,6 +109,14 @@ def _open(path):
         "sc_encoder_stack_workspace_size": (sz, [dp, i32, i32]),
         "sc_encoder_stack": (i32, [dp, i32, vp, vp, vp, vp, vp, vp, i32, vp, i32, f32, vp, vp, vp, vp, vp, sz, vp]),
         "sc_validate_desc": (i32, [dp, vp, vp]),
+        "sc_i8_pitch": (ctypes.c_int64, [ctypes.c_int64]),
+        "sc_quantize_rows_i8": (i32, [i32, i32, i32, vp, i32, vp, vp, vp, vp]),
+        "sc_quantize_weight_i8": (i32, [i32, i32, i32, vp, vp, vp, vp]),
+        "sc_linear_i8_workspace_size": (sz, [lp]),
+        "sc_linear_i8": (i32, [lp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "sc_block_norm": (i32, [np_] + 12 * [vp]),
+        "sc_block_norm_backward_workspace_size": (sz, [np_]),
+        "sc_block_norm_backward": (i32, [np_] + 17 * [vp] + [sz, vp]),
         "sc_profile_window_kernel": (i32, [i32]),
         "sc_profile_window_kernel_read": (i32, [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double),
                                                  ctypes.c_int64, ctypes.POINTER(ctypes.c_int64)]),

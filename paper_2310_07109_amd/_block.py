@@ -1,0 +1,257 @@
+"""ctypes binding of the block operators of libsc.so (include/sc_block.h; argument marshalling only)."""
+from __future__ import annotations
+
+import ctypes
+
+from ._binding import (SC_ACT_NONE, SC_BF16, SC_F32, SC_GATE_CHANNEL, SC_GATE_NONE, SC_GATE_SEQUENCE, SC_I8,
+                       SC_NORM_LAYER, _check, _LinearDesc, _NormDesc, _on_stream, _opt, _ptr, _stream, _tensor, _ws,
+                       load)
+
+
+def _one_device(tensors, stream):
+    """The device of the tensors (None: absent), which is the stream's (default: the current one)."""
+    import torch
+    dev = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device}")
+    at = torch.cuda.current_device() if stream is None else stream.device_index
+    if dev.index != at:
+        raise ValueError(f"tensors on {dev}, stream on device {at}")
+    return dev
+
+
+def _float_type(code, what):
+    import torch
+    if code not in (SC_F32, SC_BF16):
+        raise ValueError(f"{what}: expected SC_F32 or SC_BF16, got {code}")
+    return torch.float32 if code == SC_F32 else torch.bfloat16
+
+
+def _code(t, name):
+    import torch
+    if t.dtype == torch.float32:
+        return SC_F32
+    if t.dtype == torch.bfloat16:
+        return SC_BF16
+    raise TypeError(f"{name}: expected torch.float32 or torch.bfloat16, got {t.dtype}")
+
+
+def _lengths(valid_len, B):
+    import torch
+    return None if valid_len is None else _tensor(valid_len, "valid_len", torch.int32, (B,))
+
+
+def sc_i8_pitch(K: int) -> int:
+    """Bytes of a row of K 8-bit values."""
+    return load().sc_i8_pitch(int(K))
+
+
+@_on_stream
+def sc_quantize_rows_i8(x, valid_len=None, xq=None, scale=None, stream=None):
+    """8-bit rows of x [B, n, K] (float32 or bf16).  Returns (xq int8 [B, n, pitch], scale float32 [B, n])."""
+    import torch
+    L = load()
+    code = _code(_tensor(x, "x"), "x")
+    B, n, K = x.shape
+    _lengths(valid_len, B)
+    shape = (B, n, L.sc_i8_pitch(K))
+    dev = _one_device((x, valid_len, xq, scale), stream)
+    xq = torch.empty(shape, dtype=torch.int8, device=dev) if xq is None else _tensor(xq, "xq", torch.int8, shape)
+    scale = torch.empty((B, n), dtype=torch.float32, device=dev) if scale is None else \
+        _tensor(scale, "scale", torch.float32, (B, n))
+    _check(L.sc_quantize_rows_i8(B, n, K, _ptr(valid_len), code, _ptr(x), _ptr(xq), _ptr(scale), _stream(stream)),
+           "sc_quantize_rows_i8")
+    return xq, scale
+
+
+@_on_stream
+def sc_quantize_weight_i8(w, wq=None, scale=None, stream=None):
+    """8-bit weights of w [K, N] (float32 or bf16).  Returns (wq int8 [N, pitch(K)], scale float32 [N])."""
+    import torch
+    L = load()
+    code = _code(_tensor(w, "w"), "w")
+    K, N = w.shape
+    shape = (N, L.sc_i8_pitch(K))
+    dev = _one_device((w, wq, scale), stream)
+    wq = torch.empty(shape, dtype=torch.int8, device=dev) if wq is None else _tensor(wq, "wq", torch.int8, shape)
+    scale = torch.empty((N,), dtype=torch.float32, device=dev) if scale is None else \
+        _tensor(scale, "scale", torch.float32, (N,))
+    _check(L.sc_quantize_weight_i8(K, N, code, _ptr(w), _ptr(wq), _ptr(scale), _stream(stream)),
+           "sc_quantize_weight_i8")
+    return wq, scale
+
+
+class LinearDesc:
+    """Geometry and types of an 8-bit product (mirrors sc_linear_desc).  valid_len: int32 device tensor [B] or
+    None."""
+
+    def __init__(self, B, n, K, N, valid_len=None, x_dtype=SC_BF16, out_dtype=SC_BF16, act=SC_ACT_NONE):
+        self.B, self.n, self.K, self.N = int(B), int(n), int(K), int(N)
+        self.valid_len = valid_len
+        self.x_dtype, self.out_dtype, self.act = int(x_dtype), int(out_dtype), int(act)
+
+    def c(self) -> _LinearDesc:
+        return _LinearDesc(self.B, self.n, self.K, self.N,
+                           None if self.valid_len is None else self.valid_len.data_ptr(), self.x_dtype,
+                           self.out_dtype, self.act)
+
+
+def sc_linear_i8_workspace_size(desc: LinearDesc) -> int:
+    return load().sc_linear_i8_workspace_size(ctypes.byref(desc.c()))
+
+
+@_on_stream
+def sc_linear_i8(desc: LinearDesc, x, wq, w_scale, bias=None, x_scale=None, out=None, workspace=None, stream=None):
+    """out [B, n, N] = act(x . W + bias).  x: [B, n, K] float, or 8-bit rows [B, n, pitch(K)] with x_scale [B, n];
+    wq, w_scale: as sc_quantize_weight_i8 returns them."""
+    import torch
+    L = load()
+    B, n, K, N = desc.B, desc.n, desc.K, desc.N
+    _lengths(desc.valid_len, B)
+    pitch = L.sc_i8_pitch(K)
+    if desc.x_dtype == SC_I8:
+        _tensor(x, "x", torch.int8, (B, n, pitch))
+        _tensor(x_scale, "x_scale", torch.float32, (B, n))
+    else:
+        _tensor(x, "x", _float_type(desc.x_dtype, "x_dtype"), (B, n, K))
+        if x_scale is not None:
+            raise ValueError("x_scale: only with 8-bit rows")
+    _tensor(wq, "wq", torch.int8, (N, pitch))
+    _tensor(w_scale, "w_scale", torch.float32, (N,))
+    if bias is not None:
+        _tensor(bias, "bias", torch.float32, (N,))
+    dev = _one_device((x, x_scale, wq, w_scale, bias, out, workspace, desc.valid_len), stream)
+    dt = _float_type(desc.out_dtype, "out_dtype")
+    out = torch.empty((B, n, N), dtype=dt, device=dev) if out is None else _tensor(out, "out", dt, (B, n, N))
+    cd = desc.c()
+    wsb = L.sc_linear_i8_workspace_size(ctypes.byref(cd))
+    if workspace is None:
+        workspace = _ws(wsb, dev) if wsb > 0 else None
+    else:
+        wsb = _tensor(workspace, "workspace").numel() * workspace.element_size()
+    _check(L.sc_linear_i8(ctypes.byref(cd), _ptr(x), _ptr(x_scale), _ptr(wq), _ptr(w_scale), _ptr(bias), _ptr(out),
+                          _ptr(workspace), wsb, _stream(stream)), "sc_linear_i8")
+    return out
+
+
+class NormDesc:
+    """Geometry and form of the norms around a block (mirrors sc_norm_desc).  valid_len: int32 device tensor [B]
+    or None."""
+
+    def __init__(self, B, n, D, valid_len=None, kind=SC_NORM_LAYER, post=False, pre=True, gate=SC_GATE_NONE, eps=1e-5,
+                 res_scale=1.0, dtype=SC_BF16):
+        self.B, self.n, self.D = int(B), int(n), int(D)
+        self.valid_len = valid_len
+        self.kind, self.post, self.pre, self.gate = int(kind), int(bool(post)), int(bool(pre)), int(gate)
+        self.eps, self.res_scale, self.dtype = float(eps), float(res_scale), int(dtype)
+
+    def c(self) -> _NormDesc:
+        return _NormDesc(self.B, self.n, self.D, None if self.valid_len is None else self.valid_len.data_ptr(),
+                         self.kind, self.post, self.pre, self.gate, self.eps, self.res_scale, self.dtype)
+
+    def gate_form(self):
+        """(shape, dtype) of the gate."""
+        import torch
+        if self.gate == SC_GATE_CHANNEL:
+            return (self.D,), torch.float32
+        return ((self.B, self.D) if self.gate == SC_GATE_SEQUENCE else (self.B, self.n, self.D)), \
+            _float_type(self.dtype, "dtype")
+
+
+def _norm_inputs(desc, x, t, gate, post_w, post_b, pre_w, pre_b):
+    import torch
+    shape, dt = (desc.B, desc.n, desc.D), _float_type(desc.dtype, "dtype")
+    _lengths(desc.valid_len, desc.B)
+    _tensor(x, "x", dt, shape)
+    if t is not None:
+        _tensor(t, "t", dt, shape)
+    if gate is not None:
+        gs, gt = desc.gate_form()
+        _tensor(gate, "gate", gt, gs)
+    for w, nm in ((post_w, "post_w"), (post_b, "post_b"), (pre_w, "pre_w"), (pre_b, "pre_b")):
+        if w is not None:
+            _tensor(w, nm, torch.float32, (desc.D,))
+    return shape, dt
+
+
+@_on_stream
+def sc_block_norm(desc: NormDesc, x, t=None, gate=None, post_w=None, post_b=None, pre_w=None, pre_b=None, r=True,
+                  y=True, quantized=False, stream=None):
+    """r = res_scale x + gate post(t), y = pre(r).  Returns (r, y, yq, yscale); absent outputs are None.
+
+    r / y: True (allocate), False (skip) or a preallocated tensor (r may be x); quantized: True, False or (yq,
+    yscale).  Without desc.pre, y is skipped."""
+    import torch
+    L = load()
+    shape, dt = _norm_inputs(desc, x, t, gate, post_w, post_b, pre_w, pre_b)
+    for o, nm in ((r, "r"), (y, "y")):
+        if isinstance(o, torch.Tensor):
+            _tensor(o, nm, dt, shape)
+    rt = _opt(r, lambda: torch.empty(shape, dtype=dt, device=x.device))
+    yt = _opt(y, lambda: torch.empty(shape, dtype=dt, device=x.device)) if desc.pre or y is not True else None
+    yq = ys = None
+    if quantized:
+        qshape = (desc.B, desc.n, L.sc_i8_pitch(desc.D))
+        if quantized is True:
+            yq = torch.empty(qshape, dtype=torch.int8, device=x.device)
+            ys = torch.empty(shape[:2], dtype=torch.float32, device=x.device)
+        else:
+            yq = _tensor(quantized[0], "yq", torch.int8, qshape)
+            ys = _tensor(quantized[1], "yscale", torch.float32, shape[:2])
+    _one_device((x, t, gate, post_w, post_b, pre_w, pre_b, rt, yt, yq, ys, desc.valid_len), stream)
+    _check(L.sc_block_norm(ctypes.byref(desc.c()), _ptr(x), _ptr(t), _ptr(gate), _ptr(post_w), _ptr(post_b),
+                           _ptr(pre_w), _ptr(pre_b), _ptr(rt), _ptr(yt), _ptr(yq), _ptr(ys), _stream(stream)),
+           "sc_block_norm")
+    return rt, yt, yq, ys
+
+
+def sc_block_norm_backward_workspace_size(desc: NormDesc) -> int:
+    return load().sc_block_norm_backward_workspace_size(ctypes.byref(desc.c()))
+
+
+@_on_stream
+def sc_block_norm_backward(desc: NormDesc, x, t=None, gate=None, post_w=None, post_b=None, pre_w=None, pre_b=None,
+                           dr=None, dy=None, grads=None, workspace=None, stream=None):
+    """Gradients of sc_block_norm from dr = dL/dr and dy = dL/dy.  Returns a dict of dx, dt, dgate, dpost_w,
+    dpost_b, dpre_w and dpre_b, None for what is absent: a weight that was not given has no gradient.
+
+    grads: optional dict of preallocated outputs; only those it names are computed."""
+    import torch
+    L = load()
+    shape, dt = _norm_inputs(desc, x, t, gate, post_w, post_b, pre_w, pre_b)
+    for g, nm in ((dr, "dr"), (dy, "dy")):
+        if g is not None:
+            _tensor(g, nm, dt, shape)
+    forms = {"dx": (x, shape, dt), "dt": (t, shape, dt), "dgate": (gate, None, None)}
+    if gate is not None:
+        forms["dgate"] = (gate, *desc.gate_form())
+    for nm, w in (("dpost_w", post_w), ("dpost_b", post_b), ("dpre_w", pre_w), ("dpre_b", pre_b)):
+        forms[nm] = (w, (desc.D,), torch.float32)
+    out = dict.fromkeys(forms)
+    if grads is None:
+        for nm, (src, s, ty) in forms.items():
+            if src is not None:
+                out[nm] = torch.empty(s, dtype=ty, device=x.device)
+    else:
+        for nm, g in grads.items():
+            if nm not in forms:
+                raise ValueError(f"grads: unknown output {nm}")
+            if g is not None:
+                if nm == "dgate" and gate is None:
+                    raise ValueError("dgate: there is no gate")
+                out[nm] = _tensor(g, nm, forms[nm][2], forms[nm][1])
+    dev = _one_device((x, t, gate, post_w, post_b, pre_w, pre_b, dr, dy, workspace, desc.valid_len, *out.values()),
+                      stream)
+    cd = desc.c()
+    wsb = L.sc_block_norm_backward_workspace_size(ctypes.byref(cd))
+    if workspace is None:
+        workspace = _ws(wsb, dev)
+    else:
+        wsb = _tensor(workspace, "workspace").numel() * workspace.element_size()
+    _check(L.sc_block_norm_backward(ctypes.byref(cd), _ptr(x), _ptr(t), _ptr(gate), _ptr(post_w), _ptr(post_b),
+                                    _ptr(pre_w), _ptr(pre_b), _ptr(dr), _ptr(dy), _ptr(out["dx"]), _ptr(out["dt"]),
+                                    _ptr(out["dgate"]), _ptr(out["dpost_w"]), _ptr(out["dpost_b"]),
+                                    _ptr(out["dpre_w"]), _ptr(out["dpre_b"]), _ptr(workspace), wsb,
+                                    _stream(stream)), "sc_block_norm_backward")
+    return out

@@ -14,12 +14,13 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libsc.so")
 # the same library with SC_DEBUG: device-side argument checks and a synchronisation per call (include/sc.h)
 DEBUG_OUT = os.path.join(HERE, "libsc_debug.so")
-DEBUG_SOURCE = "sc_api.hip"  # the only source SC_DEBUG changes
+DEBUG_SOURCES = ["sc_api.hip", "sc_block_api.hip"]  # the sources that SC_DEBUG changes
 # the VALU issue-rate probe behind the roofline figures (bench.py --probe-valu), a library of its own
 PROBE_OUT = os.path.join(HERE, "libsc_probe.so")
 PROBE_SOURCES = ["probe_valu.hip", "probe_lds.hip"]
 BUILD_DIR = os.path.join(HERE, "_build")
-SOURCES = ["sc_attention.hip", "sc_prune.hip", "sc_stack.hip", "sc_backward.hip", "sc_api.hip"]
+SOURCES = ["sc_attention.hip", "sc_prune.hip", "sc_stack.hip", "sc_backward.hip", "sc_linear.hip", "sc_norm.hip", "sc_api.hip",
+           "sc_block_api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = [
@@ -54,11 +55,12 @@ def _link(objs: list, out: str) -> None:
 
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=len(SOURCES) + len(PROBE_SOURCES) + 1) as ex:
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + len(PROBE_SOURCES) + len(DEBUG_SOURCES)) as ex:
+        debug = {s: ex.submit(_compile, s, True) for s in DEBUG_SOURCES}
         objs = list(ex.map(_compile, SOURCES + PROBE_SOURCES))
-        debug_obj = ex.submit(_compile, DEBUG_SOURCE, True).result()
+        debug = {s: f.result() for s, f in debug.items()}
     _link(objs[:len(SOURCES)], OUT)
-    _link([debug_obj if s == DEBUG_SOURCE else o for s, o in zip(SOURCES, objs)], DEBUG_OUT)
+    _link([debug.get(s, o) for s, o in zip(SOURCES, objs)], DEBUG_OUT)
     _link(objs[len(SOURCES):], PROBE_OUT)
     if verbose:
         print("built", OUT, DEBUG_OUT, "and", PROBE_OUT)

@@ -9,20 +9,13 @@
 #include <mutex>
 
 #include "../../include/sc.h"
+#include "sc_api_common.h"
 #include "sc_internal.h"
 
 namespace {
 
 using sc::AttnArgs;
 using sc::AttnGeom;
-
-bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
-  if (!a || !b || na == 0 || nb == 0) return false;
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
-}
-
-size_t elem_size(int dtype) { return dtype == SC_BF16 ? 2 : 4; }
 
 sc_status check_desc(const sc_attn_desc* d) {
   if (!d) return SC_EINVAL;
@@ -48,20 +41,6 @@ sc_status check_desc(const sc_attn_desc* d) {
 }
 
 size_t tensor_bytes(const sc_attn_desc* d) { return (size_t)d->B * d->n * d->H * d->d * elem_size(d->dtype); }
-
-// Carves 256-byte aligned pieces out of the caller's workspace.
-struct Carver {
-  char* base;
-  size_t off = 0;
-  explicit Carver(void* p) : base(static_cast<char*>(p)) {}
-  template <typename T>
-  T* take(size_t count) {
-    off = (off + 255) & ~size_t(255);
-    T* p = base ? reinterpret_cast<T*>(base + off) : nullptr;
-    off += count * sizeof(T);
-    return p;
-  }
-};
 
 AttnArgs make_attn_args(const sc_attn_desc* d, const AttnGeom& geo) {
   AttnArgs a;
@@ -121,47 +100,13 @@ size_t attn_ws_size(const sc_attn_desc* d) {
 }  // namespace
 
 #ifdef SC_DEBUG
-// Debug build: the device word of the descriptor check.
-static __device__ int32_t g_debug_err;
-#endif
-
 namespace {
-#ifdef SC_DEBUG
-// Debug build: before an entry point enqueues anything, its descriptor's
-// device-resident arrays are checked and the stream drained; then the entry
-// point's own work is waited for and a failed launch or execution reported.
 sc_status debug_pre(const sc_attn_desc* d, void* stream) {
   if (check_desc(d) != SC_OK) return SC_OK;  // the entry point reports it
-  int32_t* err = nullptr;
-  if (hipGetSymbolAddress(reinterpret_cast<void**>(&err), HIP_SYMBOL(g_debug_err)) != hipSuccess || !err)
-    return SC_EHIP;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  if (sc::launch_validate_desc(d->valid_len, d->G > 0 ? d->global_pos : nullptr, d->B, d->n, d->G, err, s) !=
-      hipSuccess)
-    return SC_EHIP;
-  int32_t bits = 0;
-  if (hipMemcpyAsync(&bits, err, sizeof(bits), hipMemcpyDeviceToHost, s) != hipSuccess ||
-      hipStreamSynchronize(s) != hipSuccess)
-    return SC_EHIP;
-  return bits != 0 ? SC_EINVAL : SC_OK;
+  return debug_rows(d->valid_len, d->G > 0 ? d->global_pos : nullptr, d->B, d->n, d->G, stream);
 }
-
-sc_status debug_post(sc_status st, void* stream) {
-  if (st != SC_OK) return st;
-  if (hipStreamSynchronize(static_cast<hipStream_t>(stream)) != hipSuccess || hipGetLastError() != hipSuccess)
-    return SC_EHIP;
-  return SC_OK;
-}
-#endif
 }  // namespace
-
-#ifdef SC_DEBUG
-#define SC_DEBUG_CALL(d, stream, call)          \
-  do {                                          \
-    const sc_status pre_ = debug_pre(d, stream); \
-    if (pre_ != SC_OK) return pre_;             \
-    return debug_post(call, stream);            \
-  } while (0)
+#define SC_DEBUG_CALL(d, stream, call) SC_DEBUG_RUN(debug_pre(d, stream), stream, call)
 #else
 #define SC_DEBUG_CALL(d, stream, call) return call
 #endif

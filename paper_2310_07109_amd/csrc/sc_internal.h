@@ -171,6 +171,53 @@ constexpr int kValidLen = 1, kValidPosRange = 2, kValidPosOrder = 4, kValidPosUn
 // *err = 0, then the bits of the violations found in valid_len [B] and
 // gpos [B, G] (NULL when G == 0).
 hipError_t launch_validate_desc(const int* valid_len, const int* gpos, int B, int n, int G, int* err, hipStream_t s);
+// 8-bit rows and products (sc_linear.hip).  Rows of K values take i8_pitch(K)
+// bytes.
+constexpr int kI8Pitch = 128;
+constexpr int kI8MaxK = 131072;  // 127 x 127 x K fits an int32
+inline int i8_pitch(int K) { return (K + kI8Pitch - 1) / kI8Pitch * kI8Pitch; }
+// packed: row p of xq and scale is the p-th surviving row of x, read through
+// xidx when given; else rows keep their places and padding rows become zeros.
+hipError_t launch_quant_rows(const void* x, int f32, int8_t* xq, float* scale, int B, int n, int K, const int* len,
+                             const int* xidx, int packed, hipStream_t s);
+hipError_t launch_quant_weight(const void* w, int f32, int8_t* wq, float* scale, int K, int N, hipStream_t s);
+struct Linear {
+  const int8_t* xq;  // [rows, pitch] (packed: the surviving rows; else [B, n, pitch])
+  const float* xs;
+  const int8_t* wq;  // [N, pitch]
+  const float* w_scale;
+  const float* bias;  // or null
+  void* out;          // [B, n, N]
+  int B, n, K, N;
+  const int* len;  // or null
+  int packed, skip_pad, gelu, out_f32;
+};
+hipError_t launch_linear_i8(const Linear& l, hipStream_t s);
+long long linear_tiles(long long rows, int N);  // workgroups of the product's grid
+
+// Block norms (sc_norm.hip).
+constexpr int kNormMaxD = 4096;
+struct Norm {
+  const void *x, *t, *gate;  // t, gate: or null
+  const float *post_w, *post_b, *pre_w, *pre_b;
+  void *r, *y;  // or null
+  int8_t* yq;   // or null, with yscale
+  float* yscale;
+  const void *dr, *dy;  // backward: gradients in and out, each or null
+  void *dx, *dt, *dgate;
+  float *dpost_w, *dpost_b, *dpre_w, *dpre_b;
+  float* ws;  // backward: partial sums
+  int B, n, D;
+  const int* len;   // or null
+  const int* xidx;  // or null: row j of sequence b takes x's row xidx[b, j] (forward)
+  int skip_pad;     // padding rows of the outputs are left as they are (forward)
+  int rms, post, pre, gate_mode, f32;
+  float eps, scale;
+};
+hipError_t launch_block_norm(const Norm& a, hipStream_t s);
+size_t block_norm_backward_floats(const Norm& a);
+hipError_t launch_block_norm_backward(const Norm& a, hipStream_t s);
+
 hipError_t launch_copy_i32(const int* src, int* dst, long long count, hipStream_t s);
 hipError_t launch_iota_orig(const int* valid_len, int* orig, int B, int n, hipStream_t s);
 

@@ -44,6 +44,7 @@
 
 #include "sc_device.h"
 #include "sc_internal.h"
+#include "sc_pack.h"
 
 namespace sc {
 namespace {
@@ -151,42 +152,6 @@ __global__ __launch_bounds__(256) void k_gemm_bf16(const __bf16* __restrict__ X,
     }
 }
 
-// ---------------------------------------------------------------------------
-// Packed rows.  The surviving rows of all sequences are numbered in sequence
-// order (packed row p of sequence b is its row p - pre[b], pre = exclusive
-// prefix sum of the lengths), so that the products run on ceil(R / BM) tiles
-// of R = sum of the lengths rows instead of one partly empty tile per
-// sequence and 128 rows.  Every workgroup derives the numbering from the
-// lengths itself: the host never learns them.
-
-// Wave 0 writes pre[0 .. B] (pre[B] = R); lengths clamped to [0, n], all n
-// without lengths.
-SC_DEV void pack_prefix(int* pre, const int* len, int B, int n) {
-  if (threadIdx.x >= 64) return;
-  const int lane = threadIdx.x;
-  int carry = 0;
-  for (int c = 0; c < B; c += 64) {
-    const int b = c + lane;
-    const int v = b < B ? (len ? clampi(len[b], 0, n) : n) : 0;
-    const int incl = prefix_sum(v);
-    if (b < B) pre[b] = carry + incl - v;
-    carry += __builtin_amdgcn_readlane(incl, 63);
-  }
-  if (lane == 0) pre[B] = carry;
-}
-
-// The sequence holding packed row p < pre[B]: the largest b with pre[b] <= p
-// (empty sequences share their start with the next one).
-SC_DEV int pack_seq(const int* pre, int B, int p) {
-  int lo = 0, hi = B - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (pre[mid] <= p) lo = mid;
-    else hi = mid - 1;
-  }
-  return lo;
-}
-
 // Tiles of the packed product.  R rows in tiles of bm rows: 256 once the
 // rows fill at least kBigRows (the taller tile's lower traffic per flop
 // pays); 64 when the 64-row tiles of an unsplit product still fit one round
@@ -232,12 +197,6 @@ constexpr int kStageBytes = 49152;  // stage buffers: 4 x (64 + 128), 3 x (128 +
 // X rows of 4 units (32 k) swizzle by bits 2-3 of the row, so that 16
 // consecutive rows read at one unit hit 16 distinct 16-byte bank groups
 SC_DEV int gx_off(int row, int unit) { return row * kGK + 8 * (unit ^ ((row >> 2) & 3)); }
-// s_waitcnt vmcnt(n) alone (expcnt and lgkmcnt at their no-wait maxima)
-template <int N>
-SC_DEV void wait_vm() {
-  static_assert(N >= 0 && N < 64, "vmcnt range");
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
-}
 SC_DEV int gw_off(int row, int unit) { return row * kBN + 8 * (unit ^ (2 * (row & 7))); }
 // W row held by LDS row r of a stage: within each 32-row chunk, LDS row
 // 4g + t holds k = 8g + t and LDS row 16 + 4g + t holds k = 8g + 4 + t.
@@ -525,17 +484,6 @@ SC_DEV void tile_rows4(int* grow, int* xrow, const int* pre, const int* xidx, in
   const int gr = b * n + (p - pre[b]);
   grow[threadIdx.x] = q < R ? gr : -1;
   xrow[threadIdx.x] = xidx ? b * n + clampi(xidx[gr], 0, n - 1) : gr;
-}
-
-// Waits until at most `later` (< kNBuf) stages of kPer loads are in flight.
-template <int kNBuf, int kPer, int kL = kNBuf - 1>
-SC_DEV void wait_stages(int later) {
-  if constexpr (kL == 0) {
-    wait_vm<0>();
-  } else {
-    if (later >= kL) wait_vm<kL * kPer>();
-    else wait_stages<kNBuf, kPer, kL - 1>(later);
-  }
 }
 
 template <int kM, int kMode>

@@ -1,0 +1,710 @@
+"""The block operators (include/sc_block.h) against plain float64 forms.
+
+Tolerances count roundings (u = 2^-24 of float32, half a step of the storage type at the end):
+  quantised rows  the integers are those of the exact quotient, scales the correctly rounded a / 127: equal.
+  products        the integer sum is exact; (float)acc, its product with the row's scale and the FMA with the
+                  channel's scale and the bias round once each: 3 u |acc sx sw| + u |v|.  GELU passes the error on
+                  with slope <= 1.13 and adds its own: of |v| Phi(-|v|), by the polynomial's fit, 1.6e-4 (bf16) or
+                  (float32) 1e-6 up to 3, 2.5e-6 up to 5, 3e-5 up to 9 and all of it beyond (below 2e-18); the
+                  exponential's 2^-23 on top; for bf16 all of it beyond 5 (1.5e-6).
+  norms           a normalised value of a row: sums of D values in chains of at most 40 additions, the deviation
+                  from the mean, the factor and the product: 50 u (1 + |hat| + max|v| / sigma).  The rest per operation.
+  gradients       the same through the chain on magnitudes; sums over rows in chains of at most 64 additions.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2310_07109_amd as sc
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = {"f32": (torch.float32, sc.SC_F32, 2.0 ** -24), "bf16": (torch.bfloat16, sc.SC_BF16, 2.0 ** -8)}
+
+
+def gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def lens_of(spec, B, n):
+    if spec is None:
+        return None, torch.full((B,), n)
+    L = torch.tensor([spec[b % len(spec)] for b in range(B)], dtype=torch.int32)
+    return L.to(DEV), L.clamp(0, n).long()
+
+
+def valid_mask(L, n):
+    return torch.arange(n)[None, :] < L[:, None]
+
+
+def off_by_one(t):
+    """The same values one element past an aligned address."""
+    buf = torch.empty(t.numel() + 1, dtype=t.dtype, device=t.device)
+    buf[1:] = t.reshape(-1)
+    return buf[1:].view(t.shape)
+
+
+def assert_close(got, want, tol, what):
+    got = got.double().cpu()
+    assert got.shape == want.shape, what
+    bad = ~((got - want).abs() <= tol)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} off, worst " \
+        f"{float(((got - want).abs() / tol.clamp(min=1e-300))[bad].max()):.3g} times the tolerance"
+
+
+# ------------------------------------------------------------------ rows ----
+def exact_quant(x):
+    """(integers, float32 scales) of rows of finite values, in float64: 127 x is exact there, and its quotient is
+    never rounded across a border (the nearest border is 2^-33 away or met exactly)."""
+    a = x.abs().amax(-1)
+    q = torch.round(127.0 * x.double() / a.double().clamp(min=1e-300)[..., None])
+    q = torch.where(a[..., None] > 0, q, 0.0)
+    return q, (a.float() / 127).float()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,n,K,lens", [(1, 1, 1, None), (2, 3, 7, None), (3, 5, 128, (5, 0, 3)), (1, 9, 200, (4,)),
+                                        (2, 4, 1000, None), (1, 3, 1024, None), (1, 3, 1025, None),
+                                        (1, 2, 4096, None), (1, 2, 4104, None), (1, 2, 9001, None)])
+def test_quantize_rows(B, n, K, lens, dtype):
+    g = gen(K)
+    dt = TYPES[dtype][0]
+    x = torch.randn((B, n, K), generator=g) * torch.exp(3 * torch.randn((B, n, 1), generator=g))
+    x = x.to(dt)
+    x[0, 0] = 0                      # a row of zeros
+    if n > 1:
+        x[0, 1, : K // 2] = x[0, 1].abs().max() / 2      # quotients of 63.5: halfway, to the even integer
+    L_dev, L = lens_of(lens, B, n)
+    q, s = exact_quant(x.float() if dtype == "bf16" else x)
+    m = valid_mask(L, n)
+    for place in (lambda t: t, off_by_one):
+        xq, scale = sc.sc_quantize_rows_i8(place(x.to(DEV)), valid_len=L_dev)
+        assert xq.shape == (B, n, sc.sc_i8_pitch(K))
+        assert torch.equal(xq[..., :K].double().cpu(), torch.where(m[..., None], q, 0.0))
+        assert not xq[..., K:].any()
+        assert torch.equal(scale.cpu(), torch.where(m, s, torch.zeros(())))
+
+
+def test_quantize_float32_quotients_next_to_borders():
+    """x one float32 step either side of a border of 127 x / a, for many a: the exact quotient decides."""
+    a = torch.from_numpy(np.random.default_rng(5).uniform(1, 2, 64).astype(np.float32))
+    k = torch.arange(127, dtype=torch.float64) + 0.5
+    x = (k[None, :] * a.double()[:, None] / 127).float()
+    rows = torch.cat([a[:, None], x, torch.nextafter(x, torch.tensor(0.)), torch.nextafter(x, torch.tensor(9.)), -x], 1)
+    q, _ = exact_quant(rows)
+    xq, _ = sc.sc_quantize_rows_i8(rows[None].contiguous().to(DEV))
+    assert torch.equal(xq[0, :, : rows.shape[1]].double().cpu(), q)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_quantize_extreme_rows(dtype):
+    """Rows near both ends of the type's range, denormal ones among them, and rows with an infinity or a NaN."""
+    dt = TYPES[dtype][0]
+    base = torch.linspace(-1, 1, 96, dtype=torch.float64)
+    top = torch.finfo(dt).max
+    rows = torch.stack([base * s for s in (top, 2.0 ** 100, 2.0 ** 64, 1.0, 2.0 ** -64, 2.0 ** -100, 2.0 ** -126,
+                                           2.0 ** -130, 2.0 ** -133)]).to(dt)
+    odd = torch.stack([base.to(dt)] * 4)
+    odd[0, 5], odd[1, 0], odd[2, 95] = float("inf"), float("nan"), -float("inf")
+    x = torch.cat([rows, odd])[None].contiguous()
+    q, s = exact_quant(rows)
+    xq, scale = sc.sc_quantize_rows_i8(x.to(DEV))
+    assert torch.equal(xq[0, : len(rows), :96].double().cpu(), q)
+    assert torch.equal(scale[0, : len(rows)].cpu(), s)
+    assert scale[0, len(rows):-1].isnan().all() and not xq[0, len(rows):-1].any()
+    assert torch.equal(xq[0, -1], xq[0, 3]) and scale[0, -1] == scale[0, 3]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K,N", [(1, 1), (100, 70), (128, 64), (513, 129), (700, 200)])
+def test_quantize_weight(K, N, dtype):
+    w = torch.randn((K, N), generator=gen(N)).to(TYPES[dtype][0])
+    w[:, N // 2] = 0
+    q, s = exact_quant((w.float() if dtype == "bf16" else w).t())
+    wq, scale = sc.sc_quantize_weight_i8(w.to(DEV))
+    assert torch.equal(wq[:, :K].double().cpu(), q) and not wq[:, K:].any()
+    assert torch.equal(scale.cpu(), s)
+
+
+# -------------------------------------------------------------- products ----
+def gelu64(v):
+    return v * 0.5 * torch.special.erfc(-v / math.sqrt(2))
+
+
+def linear_case(B, n, K, N, lens, x_type, bias, seed):
+    g = gen(seed)
+    L_dev, L = lens_of(lens, B, n)
+    x = torch.randn((B, n, K), generator=g) * torch.exp(torch.randn((B, n, 1), generator=g))
+    x = x.to(TYPES["bf16" if x_type == "bf16" else "f32"][0])
+    for b in range(B):  # padding rows hold anything
+        x[b, int(L[b]):] = float("nan")
+    w = torch.randn((K, N), generator=g) / math.sqrt(K)
+    wq, ws = sc.sc_quantize_weight_i8(w.to(DEV))
+    bias = torch.randn(N, generator=g) if bias else None
+    return L_dev, L, x, wq, ws, bias
+
+
+def linear_reference(x, L, wq, ws, bias, K, gelu, out_type):
+    """(outputs, tolerance) in float64."""
+    B, n, _ = x.shape
+    m = valid_mask(L, n)
+    q, s = exact_quant(torch.where(m[..., None], x.float(), 0.0))
+    acc = q @ wq[:, :K].double().cpu().t()
+    p = acc * s.double()[..., None] * ws.double().cpu()
+    v = p if bias is None else p + bias.double()
+    tol = 3 * U * p.abs() + U * v.abs()
+    if gelu:
+        a = v.abs()
+        tail = a * 0.5 * torch.special.erfc(a / math.sqrt(2))
+        if out_type == "bf16":
+            own = torch.where(a < 5, 1.7e-4 * tail, tail + 1.5e-6)
+        else:
+            own = torch.where(a < 3, 1e-6, torch.where(a < 5, 2.5e-6, torch.where(a < 9, 3e-5, 1.0))) * tail
+        out = gelu64(v)
+        tol = 1.13 * tol + own + 2.0 ** -23 * tail + U * out.abs()
+    else:
+        out = v
+    tol = tol + TYPES[out_type][2] * (out.abs() + tol) + 1e-44
+    zero = torch.zeros((), dtype=torch.float64)
+    return torch.where(m[..., None], out, zero), torch.where(m[..., None], tol, zero)
+
+
+LINEAR = [
+    # B, n, K, N, lens, x, out, gelu, bias
+    (1, 1, 1, 1, None, "bf16", "bf16", False, True),
+    (1, 1, 512, 1536, None, "bf16", "bf16", False, True),
+    (1, 3, 130, 17, None, "f32", "f32", True, False),
+    (2, 7, 64, 31, (7, 3), "bf16", "f32", False, True),
+    (5, 8, 768, 200, (8, 0, 1, 5, 0), "bf16", "bf16", True, True),
+    (1, 16, 8200, 40, None, "bf16", "bf16", False, False),
+    (2, 16, 257, 129, (16, 9), "i8", "bf16", True, True),
+    (3, 40, 500, 111, (40, 13, 0), "f32", "f32", False, True),
+    (2, 65, 128, 64, None, "i8", "f32", False, False),
+    (1, 300, 1000, 264, None, "bf16", "bf16", True, True),
+    (16, 33, 96, 520, (33, 1, 0, 17), "bf16", "bf16", False, True),
+    (4, 1000, 256, 1030, (1000, 3, 999, 512), "bf16", "bf16", False, True),      # 128 x 128 tiles
+    (4, 1000, 200, 1111, (1000, 3, 999, 512), "f32", "f32", True, True),
+    (7, 2100, 128, 1152, (2100, 0, 2099, 2100), "bf16", "bf16", True, False),    # 256 x 128 tiles
+    (7, 2100, 130, 1153, (2100, 0, 2099, 2100), "i8", "f32", False, True),
+    (300, 3, 77, 90, (3, 0, 2, 1), "bf16", "bf16", False, True),                 # many short sequences
+]
+
+
+@pytest.mark.parametrize("case", LINEAR, ids=lambda c: "-".join(str(v) for v in c[:4]) + f"-{c[5]}-{c[6]}")
+def test_linear(case):
+    B, n, K, N, lens, x_type, out_type, gelu, has_bias = case
+    L_dev, L, x, wq, ws, bias = linear_case(B, n, K, N, lens, x_type, has_bias, seed=B * n + K)
+    d = sc.LinearDesc(B, n, K, N, valid_len=L_dev, out_dtype=TYPES[out_type][1],
+                      x_dtype=sc.SC_I8 if x_type == "i8" else TYPES[x_type][1],
+                      act=sc.SC_ACT_GELU if gelu else sc.SC_ACT_NONE)
+    want, tol = linear_reference(x, L, wq, ws, bias, K, gelu, out_type)
+    b = None if bias is None else bias.to(DEV)
+    xd, xs = x.to(DEV), None
+    if x_type == "i8":
+        xd, xs = sc.sc_quantize_rows_i8(xd)
+    out = torch.full((B, n, N), float("nan"), dtype=TYPES[out_type][0], device=DEV)
+    sc.sc_linear_i8(d, xd, wq, ws, bias=b, x_scale=xs, out=out)
+    assert_close(out, want, tol, "aligned")
+    # the same call, and on other alignments: the same bits
+    again = sc.sc_linear_i8(d, xd if x_type == "i8" else off_by_one(xd), wq, off_by_one(ws),
+                            bias=None if b is None else off_by_one(b), x_scale=xs, out=off_by_one(out.clone()))
+    assert torch.equal(again, out)
+
+
+@pytest.mark.parametrize("x_type", ["bf16", "i8"])
+def test_linear_row_depends_on_itself_alone(x_type):
+    """One row alone, among few, and among many rows (other kernels and tiles): the same bits."""
+    K, N, n = 384, 1152, 20000
+    x = torch.randn((1, n, K), generator=gen(3)).to(torch.bfloat16).to(DEV)
+    wq, ws = sc.sc_quantize_weight_i8(torch.randn((K, N), generator=gen(4)).to(DEV))
+    bias = torch.randn(N, generator=gen(5)).to(DEV)
+
+    def run(rows):
+        part, xs = x[:, rows].contiguous(), None
+        if x_type == "i8":
+            part, xs = sc.sc_quantize_rows_i8(part)
+        d = sc.LinearDesc(1, part.shape[1], K, N, x_dtype=sc.SC_I8 if x_type == "i8" else sc.SC_BF16,
+                          act=sc.SC_ACT_GELU)
+        return sc.sc_linear_i8(d, part, wq, ws, bias=bias, x_scale=xs)[0]
+    whole = run(slice(0, n))
+    for lo, hi in ((0, 1), (17, 20), (100, 117), (1000, 1064), (5000, 5200), (7000, 9500), (11, 16011)):
+        assert torch.equal(run(slice(lo, hi)), whole[lo:hi]), (lo, hi)
+
+
+def test_linear_extremes():
+    """Sums at the ends of int32 (K at its limit, all 127), zero rows, rows with NaN and infinity."""
+    K = 131072
+    wq = torch.full((2, K), 127, dtype=torch.int8, device=DEV)
+    wq[1] = -127
+    xq = torch.full((1, 2, K), 127, dtype=torch.int8, device=DEV)
+    one = torch.ones(2, device=DEV)
+    d = sc.LinearDesc(1, 2, K, 2, x_dtype=sc.SC_I8, out_dtype=sc.SC_F32)
+    out = sc.sc_linear_i8(d, xq, wq, one, x_scale=one[None].contiguous())
+    top = float(np.float32(127 * 127 * K))
+    assert out[0].tolist() == [[top, -top], [top, -top]]
+    x = torch.randn((1, 40, 256), generator=gen(1)).to(DEV)
+    x[0, 3], x[0, 4, 7], x[0, 5, 9], x[0, 6, 0] = 0, float("nan"), float("inf"), -float("inf")
+    w, s = sc.sc_quantize_weight_i8(torch.randn((256, 200), generator=gen(2)).to(DEV))
+    b = torch.randn(200, generator=gen(3)).to(DEV)
+    for n in (40, 8):
+        for act in (sc.SC_ACT_NONE, sc.SC_ACT_GELU):
+            d = sc.LinearDesc(1, n, 256, 200, x_dtype=sc.SC_F32, out_dtype=sc.SC_F32, act=act)
+            out = sc.sc_linear_i8(d, x[:, :n].contiguous(), w, s, bias=b)
+            assert out[0, 4:7].isnan().all() and not out[0, :4].isnan().any() and not out[0, 7:].isnan().any()
+            if act == sc.SC_ACT_NONE:
+                assert torch.equal(out[0, 3], b)
+
+
+def test_gelu_far_tails():
+    """Large arguments of either sign, through a product that passes them on: v above, 0 below."""
+    d = sc.LinearDesc(1, 1, 1, 6, x_dtype=sc.SC_F32, out_dtype=sc.SC_F32, act=sc.SC_ACT_GELU)
+    x = torch.ones((1, 1, 1), device=DEV)
+    wq = torch.zeros((6, 128), dtype=torch.int8, device=DEV)
+    bias = torch.tensor([1e30, -1e30, 20.0, -20.0, float("inf"), -float("inf")], device=DEV)
+    for out_type in (sc.SC_F32, sc.SC_BF16):
+        d.out_dtype = out_type
+        out = sc.sc_linear_i8(d, x, wq, torch.ones(6, device=DEV), bias=bias)[0, 0].float().tolist()
+        want = torch.tensor([1e30, 0, 20, 0, float("inf"), 0]).to(TYPES["f32" if out_type == sc.SC_F32 else "bf16"][0])
+        assert out == want.float().tolist()
+
+
+# ----------------------------------------------------------------- norms ----
+GATES = {"none": sc.SC_GATE_NONE, "channel": sc.SC_GATE_CHANNEL, "sequence": sc.SC_GATE_SEQUENCE,
+         "token": sc.SC_GATE_TOKEN}
+
+
+def norm_inputs(B, n, D, lens, dtype, gate, post, pre, bias, seed, offset=0.0):
+    g = gen(seed)
+    dt = TYPES[dtype][0]
+    L_dev, L = lens_of(lens, B, n)
+    rnd = lambda *s: torch.randn(s, generator=g)  # noqa: E731
+    t = dict(x=(rnd(B, n, D) + offset).to(dt), t=(0.7 * rnd(B, n, D)).to(dt), gate=None, post_w=None, post_b=None,
+             pre_w=None, pre_b=None)
+    if gate != "none":
+        shape = {"channel": (D,), "sequence": (B, D), "token": (B, n, D)}[gate]
+        t["gate"] = (0.5 + 0.3 * rnd(*shape)).to(torch.float32 if gate == "channel" else dt)
+    for nm, on in (("post", post), ("pre", pre)):
+        if on:
+            t[nm + "_w"] = 1 + 0.2 * rnd(D)
+            t[nm + "_b"] = 0.3 * rnd(D) if bias else None
+    dr, dy = rnd(B, n, D).to(dt), rnd(B, n, D).to(dt)
+    m = valid_mask(L, n)[..., None]
+    for k in ("x", "t"):  # padding rows hold anything
+        t[k] = torch.where(m, t[k], torch.full((), float("nan"), dtype=dt))
+    dr, dy = (torch.where(m, v, torch.full((), float("inf"), dtype=dt)) for v in (dr, dy))
+    return L_dev, L, t, dr, dy
+
+
+def dev(t):
+    return {k: None if v is None else v.to(DEV) for k, v in t.items()}
+
+
+def norm64(v, kind, eps):
+    if kind == "layer":
+        v = v - v.mean(-1, keepdim=True)
+    inv = (v.pow(2).mean(-1, keepdim=True) + eps).rsqrt()
+    return v * inv, inv
+
+
+def hat_error(hat, inv, size):
+    """Error of a normalised row whose unnormalised values are sums of magnitude `size`."""
+    return 50 * U * (1 + hat.abs() + size.amax(-1, keepdim=True) * inv)
+
+
+def norm_reference(t, mask, kind, eps, scale, post, pre, gate, dr=None, dy=None):
+    """Outputs, and with dr or dy the gradients, each as (values, tolerance before storage), in float64 by the formulas."""
+    z = {k: None if v is None else torch.where(mask, v.double(), 0.0) if k in ("x", "t") else v.double()
+         for k, v in t.items()}
+    gt = z["gate"]
+    if gt is None:
+        gt = torch.ones(())
+    elif gate == "sequence":
+        gt = gt[:, None]
+    u, eu = z["t"], torch.zeros_like(z["t"])
+    pw = z["post_w"] if z["post_w"] is not None else torch.ones(())
+    pb = z["post_b"] if z["post_b"] is not None else torch.zeros(())
+    if post:
+        that, tinv = norm64(u, kind, eps)
+        et = hat_error(that, tinv, u.abs())
+        u = that * pw + pb
+        eu = et * pw.abs() + 2 * U * (u.abs() + (that * pw).abs())
+    r = scale * z["x"] + gt * u
+    size = (scale * z["x"]).abs() + (gt * u).abs()
+    er = gt.abs() * eu + 3 * U * size
+    o = {"r": (r, er)}
+    if pre:
+        w = z["pre_w"] if z["pre_w"] is not None else torch.ones(())
+        b = z["pre_b"] if z["pre_b"] is not None else torch.zeros(())
+        rhat, rinv = norm64(r, kind, eps)
+        # r's own error: through the row's mean and deviation too
+        erm = er.amax(-1, keepdim=True) * rinv
+        eh = hat_error(rhat, rinv, size) + er * rinv + erm * (1 + rhat.abs())
+        o["y"] = (rhat * w + b, eh * w.abs() + 2 * U * ((rhat * w).abs() + (rhat * w + b).abs()))
+    if dr is None and dy is None:
+        return {k: (torch.where(mask, v, 0.0), torch.where(mask, e, 0.0)) for k, (v, e) in o.items()}
+
+    def input_grad(g, eg, hat, inv, eh):
+        """(inv (g - [mean g] - hat mean(g hat)), its error), eg and eh the errors of g and hat."""
+        mg = lambda a: a.mean(-1, keepdim=True)  # noqa: E731
+        d = g - hat * mg(g * hat)
+        e = eg + hat.abs() * mg(eg * hat.abs()) + hat.abs() * mg(g.abs() * eh) + eh * mg((g * hat).abs())
+        sz = g.abs() + hat.abs() * mg((g * hat).abs())
+        if kind == "layer":
+            d = d - mg(g)
+            e, sz = e + mg(eg), sz + mg(g.abs())
+        rel = (eh / (1 + hat.abs())).amax(-1, keepdim=True)  # of inv
+        return inv * d, inv * (e + 50 * U * sz + rel * (d.abs() + sz))
+    zero = torch.zeros_like(r)
+    g, eg = (torch.where(mask, dr.double(), 0.0), zero) if dr is not None else (zero, zero)
+    rows = lambda a: a.sum((0, 1))  # noqa: E731
+    o = {}
+    if dy is not None:
+        dyz = torch.where(mask, dy.double(), 0.0)
+        o["dpre_w"] = (rows(dyz * rhat), rows(dyz.abs() * torch.where(mask, eh, 0.0)) + 64 * U * rows((dyz * rhat).abs()))
+        o["dpre_b"] = (rows(dyz), 64 * U * rows(dyz.abs()))
+        d, e = input_grad(dyz * w, U * (dyz * w).abs(), rhat, rinv, eh)
+        g, eg = g + d, eg + e + U * (g + d).abs()
+    g, eg = torch.where(mask, g, 0.0), torch.where(mask, eg, 0.0)
+    o["dx"] = (scale * g, abs(scale) * eg + U * (scale * g).abs())
+    if t["gate"] is not None:
+        dg, edg = g * u, eg * u.abs() + g.abs() * eu + U * (g * u).abs()
+        dg, edg = torch.where(mask, dg, 0.0), torch.where(mask, edg, 0.0)
+        if gate == "token":
+            o["dgate"] = (dg, edg)
+        else:
+            axes = (0, 1) if gate == "channel" else 1
+            o["dgate"] = (dg.sum(axes), edg.sum(axes) + 64 * U * dg.abs().sum(axes))
+        g, eg = g * gt, eg * gt.abs() + U * (g * gt).abs()
+    if post:
+        em = torch.where(mask, et, 0.0)
+        o["dpost_w"] = (rows(g * that), rows(eg * that.abs() + g.abs() * em) + 64 * U * rows((g * that).abs()))
+        o["dpost_b"] = (rows(g), rows(eg) + 64 * U * rows(g.abs()))
+        g, eg = input_grad(g * pw, eg * pw.abs() + U * (g * pw).abs(), that, tinv, et)
+        g, eg = torch.where(mask, g, 0.0), torch.where(mask, eg, 0.0)
+    o["dt"] = (g, eg)
+    return o
+
+
+def with_storage(v, e, half):
+    return v, e + half * (v.abs() + e) + 1e-44
+
+
+NORM = [
+    # B, n, D, lens, dtype, kind, gate, post, pre, bias, scale
+    (1, 1, 1, None, "f32", "layer", "none", False, True, True, 1.0),
+    (1, 1, 512, None, "bf16", "rms", "none", True, True, False, 1.0),
+    (2, 3, 7, (3, 1), "bf16", "layer", "channel", True, True, True, 1.5),
+    (3, 5, 64, (5, 0, 2), "f32", "rms", "token", True, True, True, 0.81),
+    (2, 9, 200, None, "bf16", "layer", "sequence", False, True, True, 1.0),
+    (2, 6, 257, (6, 5), "f32", "layer", "sequence", True, False, True, -0.5),
+    (5, 40, 768, (40, 0, 17, 1, 39), "bf16", "layer", "none", False, True, True, 1.5),
+    (3, 33, 770, (33, 20, 2), "bf16", "rms", "token", False, True, False, 1.0),
+    (4, 50, 1024, (50, 49, 0, 25), "bf16", "layer", "sequence", True, True, True, 1.0),
+    (2, 30, 1025, (30, 11), "bf16", "layer", "channel", True, True, True, 1.0),
+    (1, 70, 1111, None, "f32", "layer", "channel", True, True, True, 1.0),
+    (2, 20, 2048, (20, 7), "bf16", "rms", "channel", True, True, False, 1.0),
+    (1, 9, 2052, None, "bf16", "layer", "none", True, True, True, 1.0),
+    (1, 9, 4095, None, "bf16", "layer", "token", True, True, True, 1.0),
+    (2, 9, 4096, (9, 4), "f32", "layer", "none", False, True, True, 1.5),
+    (40, 50, 96, tuple(range(0, 51, 7)), "f32", "layer", "sequence", True, True, True, 1.0),   # more rows than slots
+    (600, 3, 36, (3, 0, 2), "bf16", "layer", "sequence", True, True, True, 1.0),               # more items than blocks
+    (700, 4, 20, (4, 1), "bf16", "rms", "channel", False, True, True, 1.0),
+]
+NORM_IDS = ["-".join(str(v) for v in c[:3]) + f"-{c[4]}-{c[5]}-{c[6]}" for c in NORM]
+
+
+def norm_setup(case, seed=0, offset=0.0):
+    B, n, D, lens, dtype, kind, gate, post, pre, bias, scale = case
+    L_dev, L, t, dr, dy = norm_inputs(B, n, D, lens, dtype, gate, post, pre, bias, seed + D + B, offset)
+    d = sc.NormDesc(B, n, D, valid_len=L_dev, kind=sc.SC_NORM_LAYER if kind == "layer" else sc.SC_NORM_RMS, post=post,
+                    pre=pre, gate=GATES[gate], eps=1e-5, res_scale=scale, dtype=TYPES[dtype][1])
+    mask = valid_mask(L, n)[..., None]
+    s32 = float(np.float32(scale))
+    ref = lambda **g: norm_reference(t, mask, kind, float(np.float32(1e-5)), s32, post, pre, gate, **g)  # noqa: E731
+    return d, t, dr, dy, mask, ref
+
+
+@pytest.mark.parametrize("case", NORM, ids=NORM_IDS)
+def test_norm(case):
+    d, t, _, _, mask, ref = norm_setup(case)
+    half = TYPES[case[4]][2]
+    a = dev(t)
+    r, y, yq, ys = sc.sc_block_norm(d, **a, quantized=bool(d.pre))
+    want = ref()
+    assert_close(r, *with_storage(*want["r"], half), "r")
+    if not d.pre:
+        assert y is None and yq is None
+        return
+    assert_close(y, *with_storage(*want["y"], half), "y")
+    q, s = sc.sc_quantize_rows_i8(y, valid_len=d.valid_len)  # the 8-bit rows are those of y as stored
+    assert torch.equal(yq, q) and torch.equal(ys, s)
+    # each output alone, in place, and on other alignments
+    assert torch.equal(sc.sc_block_norm(d, **a, r=False)[1], y)
+    assert torch.equal(sc.sc_block_norm(d, **a, y=False)[0], r)
+    x2 = a["x"].clone()
+    sc.sc_block_norm(d, **dict(a, x=x2), r=x2, y=False)
+    assert torch.equal(x2, r)
+    o = {k: None if v is None else off_by_one(v) for k, v in a.items()}
+    r2, y2, yq2, ys2 = sc.sc_block_norm(d, **o, quantized=True)
+    assert_close(r2, *with_storage(*want["r"], half), "r, odd addresses")
+    assert_close(y2, *with_storage(*want["y"], half), "y, odd addresses")
+    q, s = sc.sc_quantize_rows_i8(y2, valid_len=d.valid_len)
+    assert torch.equal(yq2, q) and torch.equal(ys2, s)
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("offset", [0.0, 300.0])
+def test_norm_alone_without_block_or_weights(kind, offset):
+    """t absent (an embedding's norm), no weights; rows whose mean is far from zero."""
+    case = (2, 11, 300, (11, 4), "f32", kind, "none", False, True, False, 1.25)
+    d, t, _, _, mask, _ = norm_setup(case, offset=offset)
+    t = dict(t, pre_w=None, t=torch.zeros_like(t["t"]))
+    want = norm_reference(t, mask, kind, float(np.float32(1e-5)), 1.25, False, True, "none")
+    r, y, _, _ = sc.sc_block_norm(d, t["x"].to(DEV))
+    assert_close(r, *with_storage(*want["r"], U), "r")
+    assert_close(y, *with_storage(*want["y"], U), "y")
+
+
+def test_norm_constant_and_zero_rows():
+    """A constant row has no deviation: LayerNorm gives the bias; a row of zeros the same, RMS too."""
+    x = torch.zeros((1, 3, 96), device=DEV)
+    x[0, 1] = 4.0
+    b = torch.randn(96, generator=gen(1)).to(DEV)
+    w = torch.ones(96, device=DEV)
+    y = sc.sc_block_norm(sc.NormDesc(1, 3, 96, dtype=sc.SC_F32), x, pre_w=w, pre_b=b, r=False)[1]
+    assert torch.equal(y[0], b.expand(3, 96)), "constant rows"
+    y = sc.sc_block_norm(sc.NormDesc(1, 3, 96, dtype=sc.SC_F32, kind=sc.SC_NORM_RMS), x, pre_w=w, pre_b=b, r=False)[1]
+    assert torch.equal(y[0, 0], b) and (y[0, 1] - b - 1).abs().max() < 1e-6
+
+
+NAMES = ("dx", "dt", "dgate", "dpost_w", "dpost_b", "dpre_w", "dpre_b")
+
+
+def check_grads(got, want, case, what):
+    half = TYPES[case[4]][2]
+    for k in NAMES:
+        if got[k] is None:
+            continue
+        stored = half if k in ("dx", "dt") or (k == "dgate" and case[6] in ("token", "sequence")) else U
+        assert_close(got[k], *with_storage(*want[k], stored), f"{what}: {k}")
+
+
+@pytest.mark.parametrize("case", NORM, ids=NORM_IDS)
+def test_norm_backward(case):
+    d, t, dr, dy, mask, ref = norm_setup(case, seed=1)
+    a = dev(t)
+    gr, gy = dr.to(DEV), dy.to(DEV)
+    have = {"dx", "dt"} | {"d" + k for k in t if k not in ("x", "t") and t[k] is not None}
+    for use_r, use_y in ((True, True), (False, True), (True, False)):
+        use_y = use_y and bool(d.pre)
+        if not (use_r or use_y):
+            continue
+        want = ref(dr=dr if use_r else None, dy=dy if use_y else None)
+        if not use_y and d.pre:  # no gradient reaches the norm's weights
+            want["dpre_w"] = want["dpre_b"] = (torch.zeros(d.D, dtype=torch.float64),) * 2
+        got = sc.sc_block_norm_backward(d, **a, dr=gr if use_r else None, dy=gy if use_y else None)
+        assert {k for k in NAMES if got[k] is not None} == have
+        check_grads(got, want, case, f"dr {use_r} dy {use_y}")
+    want = ref(dr=dr, dy=dy if d.pre else None)
+    kw = dict(dr=gr, dy=gy if d.pre else None)
+    got = sc.sc_block_norm_backward(d, **a, **kw)
+    # again: the same bits; some outputs alone, dx in place of dr and dt of dy; odd addresses
+    again = sc.sc_block_norm_backward(d, **a, **kw)
+    assert all(got[k] is None or torch.equal(got[k], again[k]) for k in NAMES)
+    r2, y2 = gr.clone(), gy.clone()
+    part = sc.sc_block_norm_backward(d, **a, dr=r2, dy=y2 if d.pre else None,
+                                     grads=dict(dx=r2, **(dict(dt=y2) if d.pre else {})))
+    assert torch.equal(r2, got["dx"]) and part["dpre_w"] is None
+    assert not d.pre or torch.equal(y2, got["dt"])
+    odd = {k: None if v is None else off_by_one(v) for k, v in a.items()}
+    check_grads(sc.sc_block_norm_backward(d, **odd, dr=off_by_one(gr), dy=off_by_one(gy) if d.pre else None), want,
+                case, "odd addresses")
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+def test_norm_backward_against_differences(kind):
+    """The kernel's gradients along random directions against central differences of the float64 forward, whose error
+    for a step h is h^2 / 6 times the third derivative: Richardson's extrapolation of two steps leaves 1e-8 here."""
+    case = (3, 6, 60, (6, 4, 1), "f32", kind, "sequence", True, True, True, 1.5)
+    d, t, dr, dy, mask, ref = norm_setup(case, seed=2)
+    got = sc.sc_block_norm_backward(d, **dev(t), dr=dr.to(DEV), dy=dy.to(DEV))
+    want = ref(dr=dr, dy=dy)
+    z = {k: None if v is None else v.double() for k, v in t.items()}
+    zr, zy = (torch.where(mask, v.double(), 0.0) for v in (dr, dy))
+
+    def loss(k, step, direction):
+        s = dict(z)
+        s[k] = z[k] + step * direction
+        o = norm_reference(s, mask, kind, float(np.float32(1e-5)), 1.5, True, True, "sequence")
+        return float((o["r"][0] * zr).sum() + (o["y"][0] * zy).sum())
+    for i, k in enumerate(("x", "t", "gate", "post_w", "post_b", "pre_w", "pre_b")):
+        v = torch.randn(t[k].shape, generator=gen(50 + i), dtype=torch.float64)
+        diff = lambda h: (loss(k, h, v) - loss(k, -h, v)) / (2 * h)  # noqa: E731
+        slope = (4 * diff(1e-4) - diff(2e-4)) / 3
+        g, e = got["d" + k].double().cpu(), want["d" + k][1]
+        size = float((g * v).abs().sum())
+        # the formula's gradients lie on the differences, the kernel's within their own tolerance
+        assert abs(float((want["d" + k][0] * v).sum()) - slope) <= 1e-8 * (1 + size), k
+        assert abs(float((g * v).sum()) - slope) <= float((with_storage(g, e, U)[1] * v.abs()).sum()) + 1e-8 * (1 + size), k
+
+
+# ------------------------------------------------------------------ used ----
+def feed_forward(d, ln, x, w1, s1, b1, w2, s2, F):
+    """A post-norm feed-forward block as a program runs it: norm -> 8-bit rows -> product with GELU -> product -> norm."""
+    _, y, yq, ys = sc.sc_block_norm(d, x, quantized=True, r=False, **ln)
+    h = sc.sc_linear_i8(sc.LinearDesc(d.B, d.n, d.D, F, d.valid_len, sc.SC_I8, act=sc.SC_ACT_GELU), yq, w1, s1, b1, ys)
+    t = sc.sc_linear_i8(sc.LinearDesc(d.B, d.n, F, d.D, d.valid_len), h, w2, s2)
+    return sc.sc_block_norm(d, y, t, r=False, **ln)[1], (y, h, t)
+
+
+def ff_setup(B=3, n=50, D=128, F=512, lens=(50, 0, 31)):
+    g = gen(9)
+    L_dev, L = lens_of(lens, B, n)
+    rnd = lambda *s: torch.randn(s, generator=g).to(DEV)  # noqa: E731
+    d = sc.NormDesc(B, n, D, valid_len=L_dev)
+    ln = dict(pre_w=1 + 0.1 * rnd(D), pre_b=0.1 * rnd(D))
+    w1, s1 = sc.sc_quantize_weight_i8(rnd(D, F) / math.sqrt(D))
+    w2, s2 = sc.sc_quantize_weight_i8(rnd(F, D) / math.sqrt(F))
+    return d, ln, rnd(B, n, D).to(torch.bfloat16), w1, s1, 0.1 * rnd(F), w2, s2, F
+
+
+def test_feed_forward_together():
+    """The operators chained, each against its own reference on the rows that it was given."""
+    args = ff_setup()
+    d, ln, x, w1, s1, b1, w2, s2, F = args
+    out, (y, h, t) = feed_forward(*args)
+    mask = valid_mask(d.valid_len.cpu().long(), d.n)[..., None]
+    w = dict(x=x.cpu(), t=torch.zeros_like(x.cpu()), gate=None, post_w=None, post_b=None,
+             **{k: v.cpu() for k, v in ln.items()})
+    eps = float(np.float32(1e-5))
+    assert_close(y, *with_storage(*norm_reference(w, mask, "layer", eps, 1.0, False, True, "none")["y"], 2.0 ** -8), "y")
+    L = d.valid_len.cpu().long()
+    assert_close(h, *linear_reference(y.cpu(), L, w1, s1, b1.cpu(), d.D, True, "bf16"), "h")
+    assert_close(t, *linear_reference(h.cpu(), L, w2, s2, None, F, False, "bf16"), "t")
+    w.update(x=y.cpu(), t=t.cpu())
+    assert_close(out, *with_storage(*norm_reference(w, mask, "layer", eps, 1.0, False, True, "none")["y"], 2.0 ** -8), "out")
+
+
+def test_captured_and_replayed():
+    """Forward and backward captured once and replayed between other eager work: every replay gives the eager bits, and
+    two graphs with workspaces of their own keep apart."""
+    args = ff_setup()
+    d, ln, x = args[:3]
+    dy = torch.randn(x.shape, generator=gen(4)).to(DEV).to(torch.bfloat16)
+
+    def step():
+        out, (y, _, t) = feed_forward(*args)
+        g = sc.sc_block_norm_backward(d, y, t, dy=dy, **ln)
+        return [out] + [v for v in g.values() if v is not None]
+    want = [v.clone() for v in step()]
+    x0 = x.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs = step()
+        graphs.append((g, outs))
+    for i in range(4):
+        g, outs = graphs[i % 2]
+        for o in outs:
+            o.fill_(float("nan"))
+        x.copy_(-x0)                 # other work of the program on the same inputs
+        step()
+        x.copy_(x0)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), i
+
+
+def test_other_stream():
+    """On a stream of its own: outputs and workspaces belong to it, results are the same."""
+    args = ff_setup()
+    d, ln, x = args[:3]
+    want, (y, _, t) = feed_forward(*args)
+    dy = torch.randn(x.shape, generator=gen(4)).to(DEV).to(torch.bfloat16)
+    grads = sc.sc_block_norm_backward(d, y, t, dy=dy, **ln)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    w1, s1, b1, F = args[3], args[4], args[5], args[8]
+    _, y2, yq, ys = sc.sc_block_norm(d, x, quantized=True, r=False, stream=s, **ln)
+    h = sc.sc_linear_i8(sc.LinearDesc(d.B, d.n, d.D, F, d.valid_len, sc.SC_I8, act=sc.SC_ACT_GELU), yq, w1, s1, b1, ys,
+                        stream=s)
+    t2 = sc.sc_linear_i8(sc.LinearDesc(d.B, d.n, F, d.D, d.valid_len), h, args[6], args[7], stream=s)
+    out = sc.sc_block_norm(d, y2, t2, r=False, stream=s, **ln)[1]
+    g2 = sc.sc_block_norm_backward(d, y2, t2, dy=dy, stream=s, **ln)
+    s.synchronize()
+    assert torch.equal(out, want)
+    assert all(grads[k] is None or torch.equal(grads[k], g2[k]) for k in NAMES)
+
+
+def test_lengths_out_of_range_are_clamped():
+    """valid_len beyond [0, n] is clamped (include/sc_block.h): as n or 0, nothing else is touched."""
+    x = torch.randn((2, 5, 64), generator=gen(1)).to(DEV).to(torch.bfloat16)
+    w, s = sc.sc_quantize_weight_i8(torch.randn((64, 32), generator=gen(2)).to(DEV))
+    res = []
+    for L in ((99, -3), (5, 0)):
+        L = torch.tensor(L, dtype=torch.int32, device=DEV)
+        res.append((sc.sc_linear_i8(sc.LinearDesc(2, 5, 64, 32, valid_len=L), x, w, s),
+                    sc.sc_block_norm(sc.NormDesc(2, 5, 64, valid_len=L), x)[1],
+                    sc.sc_block_norm_backward(sc.NormDesc(2, 5, 64, valid_len=L), x, dy=x)["dx"],
+                    sc.sc_quantize_rows_i8(x, valid_len=L)[0]))
+    assert all(torch.equal(a, b) for a, b in zip(*res))
+
+
+def test_binding_refusals():
+    x = torch.zeros((2, 8, 64), dtype=torch.bfloat16, device=DEV)
+    w, s = sc.sc_quantize_weight_i8(torch.ones((64, 32), device=DEV))
+    d = sc.LinearDesc(2, 8, 64, 32)
+    with pytest.raises(ValueError, match="contiguous"):
+        sc.sc_linear_i8(d, x.transpose(0, 1).contiguous().transpose(0, 1), w, s)
+    with pytest.raises(TypeError, match="x: expected"):
+        sc.sc_linear_i8(d, x.float(), w, s)
+    with pytest.raises(ValueError, match="wq: expected shape"):
+        sc.sc_linear_i8(d, x, w[:, :64].contiguous(), s)
+    with pytest.raises(ValueError, match="x_scale"):
+        sc.sc_linear_i8(d, x, w, s, x_scale=torch.ones((2, 8), device=DEV))
+    with pytest.raises(TypeError, match="valid_len"):
+        sc.sc_linear_i8(sc.LinearDesc(2, 8, 64, 32, valid_len=torch.ones(2, dtype=torch.int64, device=DEV)), x, w, s)
+    with pytest.raises(sc.ScError, match="workspace"):
+        sc.sc_linear_i8(d, x, w, s, workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
+    n = sc.NormDesc(2, 8, 64, gate=sc.SC_GATE_CHANNEL)
+    with pytest.raises(TypeError, match="gate: expected torch.float32"):
+        sc.sc_block_norm(n, x, x, gate=x[0, 0].contiguous())
+    with pytest.raises(sc.ScError):
+        sc.sc_block_norm(n, x, x)                                     # a gate is missing
+    with pytest.raises(sc.ScError):
+        sc.sc_block_norm(sc.NormDesc(2, 8, 64), x, x.clone(), y=x)    # y over x
+    with pytest.raises(ValueError, match="dgate"):
+        sc.sc_block_norm_backward(sc.NormDesc(2, 8, 64), x, x.clone(), dy=x, grads=dict(dgate=x))
+
+
+def test_debug_library_refuses_bad_lengths():
+    import ctypes
+    import os
+    if not os.path.exists(sc.debug_lib_path()):
+        pytest.skip("libsc_debug.so not built")
+    L = sc.load_debug()
+    x = torch.randn((2, 5, 64), generator=gen(1)).to(DEV)
+    y = torch.full_like(x, -7.0)
+    for lens, ok in (((5, 2), True), ((6, 2), False), ((5, -1), False)):
+        d = sc.NormDesc(2, 5, 64, valid_len=torch.tensor(lens, dtype=torch.int32, device=DEV), dtype=sc.SC_F32)
+        y.fill_(-7.0)
+        rc = L.sc_block_norm(ctypes.byref(d.c()), x.data_ptr(), None, None, None, None, None, None, None, y.data_ptr(),
+                             None, None, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+        assert rc == (0 if ok else -1)
+        if ok:
+            assert torch.equal(y, sc.sc_block_norm(d, x, r=False)[1])
+        else:
+            assert (y == -7.0).all()
