@@ -10,6 +10,9 @@
  *   sc_block_norm          r = res_scale x + gate * post(t), y = pre(r), y also
  *                          as 8-bit rows for the next product;
  *   sc_block_norm_backward its gradients;
+ *   sc_encoder_stack_i8    sc_encoder_stack (sc.h) with these products, biases,
+ *                          norm weights, residual scale and gates: the form in
+ *                          which a trained encoder is served.
  *
  * The conventions of sc.h hold: device tensors owned by the caller, scratch
  * memory from `workspace`, everything enqueued on `stream` without
@@ -163,6 +166,45 @@ sc_status sc_block_norm_backward(const sc_norm_desc *desc, const void *x, const 
                                  const void *dr, const void *dy, void *dx, void *dt, void *dgate, float *dpost_w,
                                  float *dpost_b, float *dpre_w, float *dpre_b, void *workspace, size_t ws_bytes,
                                  void *stream);
+
+/* ---------------------------------------------------------------- stack -- */
+
+/* One 8-bit product of a layer, laid out by sc_quantize_weight_i8. */
+typedef struct sc_i8_weight {
+  const int8_t *wq;
+  const float *scale;
+  const float *bias; /* or NULL */
+} sc_i8_weight;
+
+/* One layer of sc_encoder_stack_i8 (all pointers to the device). */
+typedef struct sc_layer_i8 {
+  sc_i8_weight qkv; /* D -> 3 D, columns q | k | v                      */
+  sc_i8_weight o;   /* D -> D                                           */
+  sc_i8_weight w1;  /* D -> ffn_dim                                     */
+  sc_i8_weight w2;  /* ffn_dim -> D                                     */
+  const float *gate1, *ln1_w, *ln1_b; /* float32 [D] or NULL: after the attention     */
+  const float *gate2, *ln2_w, *ln2_b; /* float32 [D] or NULL: after the feed-forward  */
+} sc_layer_i8;
+
+size_t sc_encoder_stack_i8_workspace_size(const sc_attn_desc *desc, int32_t n_layers, int32_t ffn_dim);
+
+/*
+ * sc_encoder_stack on 8-bit products, with the parts that a trained encoder
+ * has: with lin(w, v) the product of sc_linear_i8 on the rows of v, quantised
+ * per token,
+ *   qkv = bf16(lin(qkv, x));  O and the pruning as in sc_encoder_stack;
+ *   x1  = bf16(LayerNorm(res_scale x + gate1 * bf16(lin(o, O))) ln1_w + ln1_b)
+ *   h   = bf16(GELU(lin(w1, x1)))
+ *   x   = bf16(LayerNorm(res_scale x1 + gate2 * bf16(lin(w2, h))) ln2_w + ln2_b)
+ *   layers  HOST array of n_layers; ffn_dim >= 1; res_scale finite.
+ * Every other argument and error as for sc_encoder_stack; x_out rows at or
+ * beyond final_len are left untouched, as there.
+ */
+sc_status sc_encoder_stack_i8(const sc_attn_desc *desc, int32_t n_layers, const int32_t *windows, const void *x_in,
+                              const sc_layer_i8 *layers, int32_t ffn_dim, const float *thresholds,
+                              int32_t keep_global, float ln_eps, float res_scale, void *x_out, int32_t *final_len,
+                              int32_t *orig_idx, int32_t *kept_per_layer, void *workspace, size_t ws_bytes,
+                              void *stream);
 
 #ifdef __cplusplus
 }

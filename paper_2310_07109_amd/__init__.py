@@ -19,8 +19,9 @@ from ._binding import (SC_BF16, SC_F32, SC_SCORE_FROM_BAND_PROBS, SC_SCORE_FROM_
                        SC_ENOSCRATCH, SC_VALID_LEN, SC_VALID_POS_RANGE, SC_VALID_POS_ORDER,
                        SC_VALID_POS_UNUSED_FIRST, debug_lib_path, load_debug, sc_validate_desc, SC_ACT_GELU, SC_ACT_NONE, SC_GATE_CHANNEL, SC_GATE_NONE,
                        SC_GATE_SEQUENCE, SC_GATE_TOKEN, SC_I8, SC_NORM_LAYER, SC_NORM_RMS)
-from ._block import (LinearDesc, NormDesc, sc_block_norm, sc_block_norm_backward,  # noqa
-                     sc_block_norm_backward_workspace_size, sc_i8_pitch, sc_linear_i8, sc_linear_i8_workspace_size,
+from ._block import (LayerI8, LinearDesc, NormDesc, sc_block_norm, sc_block_norm_backward,  # noqa
+                     sc_block_norm_backward_workspace_size, sc_encoder_stack_i8,
+                     sc_encoder_stack_i8_workspace_size, sc_i8_pitch, sc_linear_i8, sc_linear_i8_workspace_size,
                      sc_quantize_rows_i8, sc_quantize_weight_i8)
 
 __all__ = [
@@ -37,5 +38,6 @@ __all__ = [
     "SC_I8", "SC_ACT_NONE", "SC_ACT_GELU", "SC_NORM_LAYER", "SC_NORM_RMS", "SC_GATE_NONE", "SC_GATE_CHANNEL",
     "SC_GATE_SEQUENCE", "SC_GATE_TOKEN", "LinearDesc", "NormDesc", "sc_i8_pitch", "sc_quantize_rows_i8",
     "sc_quantize_weight_i8", "sc_linear_i8", "sc_linear_i8_workspace_size", "sc_block_norm",
-    "sc_block_norm_backward", "sc_block_norm_backward_workspace_size",
+    "sc_block_norm_backward", "sc_block_norm_backward_workspace_size", "LayerI8", "sc_encoder_stack_i8",
+    "sc_encoder_stack_i8_workspace_size",
 ]

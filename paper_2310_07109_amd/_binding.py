@@ -109,6 +109,8 @@ def _open(path):
         "sc_encoder_stack_workspace_size": (sz, [dp, i32, i32]),
         "sc_encoder_stack": (i32, [dp, i32, vp, vp, vp, vp, vp, vp, i32, vp, i32, f32, vp, vp, vp, vp, vp, sz, vp]),
         "sc_validate_desc": (i32, [dp, vp, vp]),
+        "sc_encoder_stack_i8_workspace_size": (sz, [dp, i32, i32]),
+        "sc_encoder_stack_i8": (i32, [dp, i32, vp, vp, vp, i32, vp, i32, f32, f32, vp, vp, vp, vp, vp, sz, vp]),
         "sc_i8_pitch": (ctypes.c_int64, [ctypes.c_int64]),
         "sc_quantize_rows_i8": (i32, [i32, i32, i32, vp, i32, vp, vp, vp, vp]),
         "sc_quantize_weight_i8": (i32, [i32, i32, i32, vp, vp, vp, vp]),

@@ -4,7 +4,8 @@ from __future__ import annotations
 import ctypes
 
 from ._binding import (SC_ACT_NONE, SC_BF16, SC_F32, SC_GATE_CHANNEL, SC_GATE_NONE, SC_GATE_SEQUENCE, SC_I8,
-                       SC_NORM_LAYER, _check, _LinearDesc, _NormDesc, _on_stream, _opt, _ptr, _stream, _tensor, _ws,
+                       SC_NORM_LAYER, _check, _I8Weight, _LayerI8,
+                       _LinearDesc, _NormDesc, _min_bytes, _on_stream, _opt, _ptr, _stream, _tensor, _ws,
                        load)
 
 
@@ -255,3 +256,69 @@ def sc_block_norm_backward(desc: NormDesc, x, t=None, gate=None, post_w=None, po
                                     _ptr(out["dpre_w"]), _ptr(out["dpre_b"]), _ptr(workspace), wsb,
                                     _stream(stream)), "sc_block_norm_backward")
     return out
+
+
+class LayerI8:
+    """One layer of sc_encoder_stack_i8 (mirrors sc_layer_i8).  qkv, o, w1, w2: (wq, scale) or (wq, scale, bias) with
+    wq, scale as sc_quantize_weight_i8 returns them; the rest float32 [D] or None."""
+
+    def __init__(self, qkv, o, w1, w2, gate1=None, ln1_w=None, ln1_b=None, gate2=None, ln2_w=None, ln2_b=None):
+        self.products = {nm: tuple(w) + (None,) * (3 - len(w)) for nm, w in
+                         (("qkv", qkv), ("o", o), ("w1", w1), ("w2", w2))}
+        self.vectors = dict(gate1=gate1, ln1_w=ln1_w, ln1_b=ln1_b, gate2=gate2, ln2_w=ln2_w, ln2_b=ln2_b)
+
+    def tensors(self):
+        return [t for w in self.products.values() for t in w] + list(self.vectors.values())
+
+    def check(self, where, D, F):
+        import torch
+        L = load()
+        for nm, K, N in (("qkv", D, 3 * D), ("o", D, D), ("w1", D, F), ("w2", F, D)):
+            wq, scale, bias = self.products[nm]
+            _tensor(wq, f"{where}.{nm}", torch.int8, (N, L.sc_i8_pitch(K)))
+            _tensor(scale, f"{where}.{nm} scale", torch.float32, (N,))
+            if bias is not None:
+                _tensor(bias, f"{where}.{nm} bias", torch.float32, (N,))
+        for nm, t in self.vectors.items():
+            if t is not None:
+                _tensor(t, f"{where}.{nm}", torch.float32, (D,))
+
+    def c(self) -> _LayerI8:
+        addr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        return _LayerI8(*(_I8Weight(*map(addr, w)) for w in self.products.values()), *map(addr, self.vectors.values()))
+
+
+def sc_encoder_stack_i8_workspace_size(desc, n_layers: int, ffn_dim: int) -> int:
+    return load().sc_encoder_stack_i8_workspace_size(ctypes.byref(desc.c()), int(n_layers), int(ffn_dim))
+
+
+@_on_stream
+def sc_encoder_stack_i8(desc, x_in, layers, ffn_dim, thresholds, windows=None, keep_global=True, ln_eps=1e-5,
+                        res_scale=1.0, x_out=None, workspace=None, stream=None):
+    """The encoder stack on 8-bit products (layers: a list of LayerI8).  Returns (x_out, final_len, orig_idx,
+    kept_per_layer)."""
+    import torch
+    L = load()
+    cd = desc.c()
+    nl, B, n, D, F = len(layers), desc.B, desc.n, desc.H * desc.d, int(ffn_dim)
+    _tensor(x_in, "x_in", torch.bfloat16, (B, n, D))
+    if x_out is not None:
+        _tensor(x_out, "x_out", torch.bfloat16, (B, n, D))
+    if len(thresholds) != nl or (windows is not None and len(windows) != nl):
+        raise ValueError("thresholds and windows: one per layer")
+    for i, y in enumerate(layers):
+        y.check(f"layers[{i}]", D, F)
+    dev = _one_device((x_in, x_out, workspace, desc.valid_len, desc.global_pos,
+                       *(t for y in layers for t in y.tensors())), stream)
+    x_out = torch.empty_like(x_in) if x_out is None else x_out
+    i32 = dict(dtype=torch.int32, device=dev)
+    final_len, orig, kpl = torch.empty((B,), **i32), torch.empty((B, n), **i32), torch.empty((nl, B), **i32)
+    th = (ctypes.c_float * nl)(*[float(t) for t in thresholds])
+    win = None if windows is None else (ctypes.c_int32 * nl)(*[int(w) for w in windows])
+    wsb = L.sc_encoder_stack_i8_workspace_size(ctypes.byref(cd), nl, F)
+    ws = _ws(wsb, dev) if workspace is None else _min_bytes(_tensor(workspace, "workspace"), "workspace", wsb)
+    _check(L.sc_encoder_stack_i8(ctypes.byref(cd), nl, win, _ptr(x_in), (_LayerI8 * nl)(*(y.c() for y in layers)), F,
+                                 th, int(bool(keep_global)), ctypes.c_float(ln_eps), ctypes.c_float(res_scale),
+                                 _ptr(x_out), _ptr(final_len), _ptr(orig), _ptr(kpl), _ptr(ws), wsb,
+                                 _stream(stream)), "sc_encoder_stack_i8")
+    return x_out, final_len, orig, kpl

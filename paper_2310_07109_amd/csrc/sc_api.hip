@@ -8,7 +8,7 @@
 #include <cstring>
 #include <mutex>
 
-#include "../../include/sc.h"
+#include "../../include/sc_block.h"
 #include "sc_api_common.h"
 #include "sc_internal.h"
 
@@ -556,11 +556,15 @@ struct StackWs {
   float *t, *scores, *partials;
   float* split;  // slabs of the split reductions of the output and second feed-forward products
   int *len_a, *len_b, *gp_a, *gp_b, *orig_a, *orig_b, *keep_idx, *new_index;
+  // 8-bit stack: rows quantised for a product (packed) and by a norm (in place), and their scales
+  int8_t *xq, *yq;
+  float *xs, *ys;
   AttnArgs attn;
 };
 
-// Workspace of the stack; F = feed-forward width (0: attention-only layers).
-size_t carve_stack(const sc_attn_desc* d, int F, void* base, StackWs* ws) {
+// Workspace of the stack; F = feed-forward width (0: attention-only layers); i8:
+// the 8-bit stack's, whose products leave bf16 rows in t and do not split.
+size_t carve_stack(const sc_attn_desc* d, int F, bool i8, void* base, StackWs* ws) {
   const AttnGeom geo = sc::attn_geom(d->n, d->window, d->G);
   const size_t D = (size_t)d->H * d->d, bn = (size_t)d->B * d->n, G = (size_t)d->G;
   Carver c(base);
@@ -571,8 +575,12 @@ size_t carve_stack(const sc_attn_desc* d, int F, void* base, StackWs* ws) {
   w.xb = c.take<__bf16>(bn * D);
   w.x1 = F > 0 ? c.take<__bf16>(bn * D) : nullptr;
   w.h = F > 0 ? c.take<__bf16>(bn * (size_t)F) : nullptr;
-  w.t = c.take<float>(bn * D);
-  w.split = c.take<float>((size_t)sc::kGemmSplitRows * D);
+  w.t = c.take<float>(i8 ? (bn * D + 1) / 2 : bn * D);
+  w.split = i8 ? nullptr : c.take<float>((size_t)sc::kGemmSplitRows * D);
+  w.xq = i8 ? c.take<int8_t>(bn * sc::i8_pitch(std::max((int)D, F))) : nullptr;
+  w.yq = i8 ? c.take<int8_t>(bn * sc::i8_pitch((int)D)) : nullptr;
+  w.xs = i8 ? c.take<float>(bn) : nullptr;
+  w.ys = i8 ? c.take<float>(bn) : nullptr;
   w.scores = c.take<float>(bn);
   w.partials = c.take<float>(sc::partials_floats(d->B, d->H, d->n, geo, d->G));
   w.len_a = c.take<int>(d->B);
@@ -601,6 +609,85 @@ void set_window(AttnArgs& a, int n, int window, int G) {
   a.nkb = geo.nkb;
 }
 
+// Collects the launches' status.
+struct Launches {
+  bool ok = true;
+  void operator()(hipError_t e) { ok = ok && e == hipSuccess; }
+};
+
+// The rows' bookkeeping, swapped from layer to layer.
+struct StackRows {
+  int *len_cur, *len_nxt, *gp_cur, *gp_nxt, *orig_cur, *orig_nxt;
+  void next() {
+    std::swap(len_cur, len_nxt);
+    std::swap(gp_cur, gp_nxt);
+    std::swap(orig_cur, orig_nxt);
+  }
+};
+StackRows stack_rows(const sc_attn_desc* d, const StackWs& w, Launches& chk, hipStream_t s) {
+  const StackRows r{w.len_a, w.len_b, w.gp_a, w.gp_b, w.orig_a, w.orig_b};
+  chk(sc::launch_copy_i32(d->valid_len, r.len_cur, d->B, s));
+  if (d->G > 0) chk(sc::launch_copy_i32(d->global_pos, r.gp_cur, (long long)d->B * d->G, s));
+  chk(sc::launch_iota_orig(d->valid_len, r.orig_cur, d->B, d->n, s));
+  return r;
+}
+
+// Layer l from its fused projection w.qkv: attention into w.o, scores, and the
+// survivors' rows in w.keep_idx, rows.len_nxt, gp_nxt and orig_nxt.
+void attend_and_prune(const sc_attn_desc* d, const StackWs& w, const StackRows& rows, int window, int l,
+                      float threshold, int32_t keep_global, int32_t* kept_per_layer, Launches& chk, hipStream_t s) {
+  const int B = d->B, n = d->n, H = d->H, G = d->G;
+  const size_t D = (size_t)H * d->d;
+  // a2-a5: sparse attention reading q|k|v out of the fused projection
+  AttnArgs a = w.attn;
+  set_window(a, n, window, G);
+  a.q = w.qkv;
+  a.k = w.qkv + D;
+  a.v = w.qkv + 2 * D;
+  a.ld_in = 3 * (long long)D;
+  a.bs_in = a.ld_in * n;
+  a.out = w.o;
+  a.ld_out = (long long)D;
+  a.bs_out = a.ld_out * n;
+  a.lse = nullptr;
+  a.skip_pad_out = 1;  // O is read only at the kept rows
+  a.span_major = l > 0 ? 1 : 0;  // pruned layers: short sequences in an n-row batch (n up to 4096: always)
+  a.valid_len = rows.len_cur;
+  a.gpos = G > 0 ? rows.gp_cur : nullptr;
+  set_partials(a, w.partials);
+  chk(sc::launch_window_attention(SC_BF16, a, s));
+  // a6: importance scores
+  const AttnGeom geo = sc::attn_geom(n, window, G);
+  chk(sc::launch_score_from_partials(w.partials, rows.len_cur, G > 0 ? rows.gp_cur : nullptr, B, n, H, G, geo, w.scores,
+                                     s));
+  // a7-a8: threshold and scan.  The rows are not moved: the output projection
+  // and the residual read O and the layer's input through keep_idx (copying
+  // both took 20 us per call on average over 12 layers of B16 n2048 D768)
+  sc::PruneArgs p;
+  p.scores = w.scores;
+  p.valid_len = rows.len_cur;
+  p.gpos = G > 0 ? rows.gp_cur : nullptr;
+  p.B = B;
+  p.n = n;
+  p.G = G;
+  p.threshold = threshold;
+  p.keep_global = keep_global ? 1 : 0;
+  p.topk = 0;
+  p.keep_ratio = 0.f;
+  p.keep_idx = w.keep_idx;
+  p.new_len = rows.len_nxt;
+  p.new_gpos = G > 0 ? rows.gp_nxt : nullptr;
+  p.orig_in = rows.orig_cur;
+  p.orig_out = rows.orig_nxt;
+  p.new_index = w.new_index;
+  p.len_copy = kept_per_layer ? kept_per_layer + (size_t)l * B : nullptr;
+  sc::GatherArgs ga;
+  std::memset(&ga, 0, sizeof(ga));
+  ga.B = B;
+  ga.n = n;
+  chk(sc::launch_prune_gather(p, ga, s));
+}
+
 // Layers of the stack: windows (host, NULL = desc->window for every layer);
 // W1 / W2 NULL = attention-only layers, else feed-forward width F.
 sc_status run_stack(const sc_attn_desc* d, int32_t n_layers, const int32_t* windows, const void* x_in,
@@ -623,102 +710,168 @@ sc_status run_stack(const sc_attn_desc* d, int32_t n_layers, const int32_t* wind
     if (ffn && (!W1[l] || !W2[l])) return SC_EINVAL;
     if (windows && windows[l] < 0) return SC_EINVAL;
   }
-  const size_t need = carve_stack(d, ffn ? F : 0, nullptr, nullptr);
+  const size_t need = carve_stack(d, ffn ? F : 0, false, nullptr, nullptr);
   if (!workspace || ws_bytes < need) return SC_EWORKSPACE;
   const size_t D = (size_t)d->H * d->d, bn = (size_t)d->B * d->n, xb = bn * D * 2;
   if (overlaps(x_out, xb, x_in, xb) || overlaps(x_out, xb, workspace, need) || overlaps(x_in, xb, workspace, need))
     return SC_EINVAL;
   StackWs w;
-  carve_stack(d, ffn ? F : 0, workspace, &w);
+  carve_stack(d, ffn ? F : 0, false, workspace, &w);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int B = d->B, n = d->n, H = d->H, G = d->G, Di = (int)D;
-  bool ok = true;
-  auto chk = [&](hipError_t e) { ok = ok && e == hipSuccess; };
-  int *len_cur = w.len_a, *len_nxt = w.len_b, *gp_cur = w.gp_a, *gp_nxt = w.gp_b;
-  int *orig_cur = w.orig_a, *orig_nxt = w.orig_b;
-  chk(sc::launch_copy_i32(d->valid_len, len_cur, B, s));
-  if (G > 0) chk(sc::launch_copy_i32(d->global_pos, gp_cur, (long long)B * G, s));
-  chk(sc::launch_iota_orig(d->valid_len, orig_cur, B, n, s));
+  const int B = d->B, n = d->n, Di = (int)D;
+  Launches chk;
+  StackRows rows = stack_rows(d, w, chk, s);
   const __bf16* cur = static_cast<const __bf16*>(x_in);
-  for (int l = 0; l < n_layers && ok; ++l) {
+  for (int l = 0; l < n_layers && chk.ok; ++l) {
     const int window = windows ? windows[l] : d->window;
     __bf16* nxt = (l == n_layers - 1) ? static_cast<__bf16*>(x_out) : ((l & 1) ? w.xb : w.xa);
     // a1: qkv projection of the surviving rows
-    chk(sc::launch_gemm_bf16(cur, Wqkv[l], w.qkv, sc::kGemmBf16, B, n, Di, 3 * Di, len_cur, nullptr, nullptr, s));
-    // a2-a5: sparse attention reading q|k|v out of the fused projection
-    AttnArgs a = w.attn;
-    set_window(a, n, window, G);
-    a.q = w.qkv;
-    a.k = w.qkv + D;
-    a.v = w.qkv + 2 * D;
-    a.ld_in = 3 * (long long)D;
-    a.bs_in = a.ld_in * n;
-    a.out = w.o;
-    a.ld_out = (long long)D;
-    a.bs_out = a.ld_out * n;
-    a.lse = nullptr;
-    a.skip_pad_out = 1;  // O is read only at the kept rows
-    a.span_major = l > 0 ? 1 : 0;  // pruned layers: short sequences in an n-row batch (n up to 4096: always)
-    a.valid_len = len_cur;
-    a.gpos = G > 0 ? gp_cur : nullptr;
-    set_partials(a, w.partials);
-    chk(sc::launch_window_attention(SC_BF16, a, s));
-    // a6: importance scores
-    const AttnGeom geo = sc::attn_geom(n, window, G);
-    chk(sc::launch_score_from_partials(w.partials, len_cur, G > 0 ? gp_cur : nullptr, B, n, H, G, geo, w.scores, s));
-    // a7-a8: threshold and scan.  The rows are not moved: the output projection
-    // and the residual read O and the layer's input through keep_idx (copying
-    // both took 20 us per call on average over 12 layers of B16 n2048 D768)
-    sc::PruneArgs p;
-    p.scores = w.scores;
-    p.valid_len = len_cur;
-    p.gpos = G > 0 ? gp_cur : nullptr;
-    p.B = B;
-    p.n = n;
-    p.G = G;
-    p.threshold = thresholds[l];
-    p.keep_global = keep_global ? 1 : 0;
-    p.topk = 0;
-    p.keep_ratio = 0.f;
-    p.keep_idx = w.keep_idx;
-    p.new_len = len_nxt;
-    p.new_gpos = G > 0 ? gp_nxt : nullptr;
-    p.orig_in = orig_cur;
-    p.orig_out = orig_nxt;
-    p.new_index = w.new_index;
-    p.len_copy = kept_per_layer ? kept_per_layer + (size_t)l * B : nullptr;
-    sc::GatherArgs ga;
-    std::memset(&ga, 0, sizeof(ga));
-    ga.B = B;
-    ga.n = n;
-    chk(sc::launch_prune_gather(p, ga, s));
+    chk(sc::launch_gemm_bf16(cur, Wqkv[l], w.qkv, sc::kGemmBf16, B, n, Di, 3 * Di, rows.len_cur, nullptr, nullptr, s));
+    attend_and_prune(d, w, rows, window, l, thresholds[l], keep_global, kept_per_layer, chk, s);
     // a9: output projection, residual, LayerNorm on the survivors
-    chk(sc::launch_gemm_bf16(w.o, Wo[l], w.t, sc::kGemmF32, B, n, Di, Di, len_nxt, w.keep_idx, w.split, s));
+    chk(sc::launch_gemm_bf16(w.o, Wo[l], w.t, sc::kGemmF32, B, n, Di, Di, rows.len_nxt, w.keep_idx, w.split, s));
     if (!ffn) {
-      chk(sc::launch_residual_layernorm(cur, w.t, nxt, B, n, Di, ln_eps, len_nxt, w.keep_idx, w.split, Di, s));
+      chk(sc::launch_residual_layernorm(cur, w.t, nxt, B, n, Di, ln_eps, rows.len_nxt, w.keep_idx, w.split, Di, s));
     } else {
       // feed-forward block: h = GELU(x1 . W1), then LayerNorm(x1 + h . W2)
-      chk(sc::launch_residual_layernorm(cur, w.t, w.x1, B, n, Di, ln_eps, len_nxt, w.keep_idx, w.split, Di, s));
-      chk(sc::launch_gemm_bf16(w.x1, W1[l], w.h, sc::kGemmGeluBf16, B, n, Di, F, len_nxt, nullptr, nullptr, s));
-      chk(sc::launch_gemm_bf16(w.h, W2[l], w.t, sc::kGemmF32, B, n, F, Di, len_nxt, nullptr, w.split, s));
-      chk(sc::launch_residual_layernorm(w.x1, w.t, nxt, B, n, Di, ln_eps, len_nxt, nullptr, w.split, F, s));
+      chk(sc::launch_residual_layernorm(cur, w.t, w.x1, B, n, Di, ln_eps, rows.len_nxt, w.keep_idx, w.split, Di, s));
+      chk(sc::launch_gemm_bf16(w.x1, W1[l], w.h, sc::kGemmGeluBf16, B, n, Di, F, rows.len_nxt, nullptr, nullptr, s));
+      chk(sc::launch_gemm_bf16(w.h, W2[l], w.t, sc::kGemmF32, B, n, F, Di, rows.len_nxt, nullptr, w.split, s));
+      chk(sc::launch_residual_layernorm(w.x1, w.t, nxt, B, n, Di, ln_eps, rows.len_nxt, nullptr, w.split, F, s));
     }
     cur = nxt;
-    int* tmp;
-    tmp = len_cur; len_cur = len_nxt; len_nxt = tmp;
-    tmp = gp_cur; gp_cur = gp_nxt; gp_nxt = tmp;
-    tmp = orig_cur; orig_cur = orig_nxt; orig_nxt = tmp;
+    rows.next();
   }
-  chk(sc::launch_copy_i32(len_cur, final_len, B, s));
-  if (orig_idx) chk(sc::launch_copy_i32(orig_cur, orig_idx, (long long)bn, s));
-  return ok ? SC_OK : SC_EHIP;
+  chk(sc::launch_copy_i32(rows.len_cur, final_len, B, s));
+  if (orig_idx) chk(sc::launch_copy_i32(rows.orig_cur, orig_idx, (long long)bn, s));
+  return chk.ok ? SC_OK : SC_EHIP;
+}
+
+// The 8-bit stack's sizes, beside check_desc.
+sc_status check_stack_i8(const sc_attn_desc* d, int32_t n_layers, int32_t F) {
+  const sc_status st = check_desc(d);
+  if (st != SC_OK) return st;
+  if (n_layers < 1 || F < 1) return SC_EINVAL;
+  if (d->dtype != SC_BF16 || d->causal) return SC_EUNSUPPORTED;
+  const long long D = (long long)d->H * d->d, bn = (long long)d->B * d->n, pd = sc::i8_pitch((int)std::min(D, 4096LL));
+  if (D > 2048 || F > sc::kI8MaxK || d->B > sc::kPackMaxB || d->n * 3 * D * 2 >= (1LL << 32)) return SC_EUNSUPPORTED;
+  const long long pf = sc::i8_pitch(F);
+  if (bn * std::max(pd, pf) >= (1LL << 32) || F * pd >= (1LL << 32) || D * pf >= (1LL << 32)) return SC_EUNSUPPORTED;
+  if (sc::linear_tiles(bn, (int)std::max(3 * D, (long long)F)) >= (1LL << 24) - 8) return SC_EUNSUPPORTED;
+  return SC_OK;
+}
+
+bool weight_ok(const sc_i8_weight& w) {
+  return w.wq && w.scale && reinterpret_cast<uintptr_t>(w.wq) % 16 == 0;
+}
+
+sc_status run_stack_i8(const sc_attn_desc* d, int32_t n_layers, const int32_t* windows, const void* x_in,
+                       const sc_layer_i8* layers, int32_t F, const float* thresholds, int32_t keep_global,
+                       float ln_eps, float res_scale, void* x_out, int32_t* final_len, int32_t* orig_idx,
+                       int32_t* kept_per_layer, void* workspace, size_t ws_bytes, void* stream) {
+  const sc_status st = check_stack_i8(d, n_layers, F);
+  if (st != SC_OK) return st;
+  if (!x_in || !layers || !thresholds || !x_out || !final_len) return SC_EINVAL;
+  if (!(ln_eps > 0.f) || !std::isfinite(ln_eps) || !std::isfinite(res_scale)) return SC_EINVAL;
+  for (int l = 0; l < n_layers; ++l) {
+    const sc_layer_i8& y = layers[l];
+    if (!weight_ok(y.qkv) || !weight_ok(y.o) || !weight_ok(y.w1) || !weight_ok(y.w2)) return SC_EINVAL;
+    if (windows && windows[l] < 0) return SC_EINVAL;
+  }
+  const size_t need = carve_stack(d, F, true, nullptr, nullptr);
+  if (!workspace || ws_bytes < need) return SC_EWORKSPACE;
+  const size_t bn = (size_t)d->B * d->n, xb = bn * d->H * d->d * 2;
+  if (overlaps(x_out, xb, x_in, xb) || overlaps(x_out, xb, workspace, need) || overlaps(x_in, xb, workspace, need))
+    return SC_EINVAL;
+  StackWs w;
+  carve_stack(d, F, true, workspace, &w);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int B = d->B, n = d->n, D = d->H * d->d;
+  Launches chk;
+  StackRows rows = stack_rows(d, w, chk, s);
+  __bf16* t = reinterpret_cast<__bf16*>(w.t);
+  // out = lin(wt, v): 8-bit rows of the survivors (len), packed or in place
+  auto linear = [&](const int8_t* q, const float* qs, int packed, const sc_i8_weight& wt, void* out, int K, int N,
+                    const int* len, int gelu) {
+    sc::Linear a;
+    std::memset(&a, 0, sizeof(a));
+    a.xq = q;
+    a.xs = qs;
+    a.wq = wt.wq;
+    a.w_scale = wt.scale;
+    a.bias = wt.bias;
+    a.out = out;
+    a.B = B;
+    a.n = n;
+    a.K = K;
+    a.N = N;
+    a.len = len;
+    a.packed = packed;
+    a.skip_pad = 1;
+    a.gelu = gelu;
+    chk(sc::launch_linear_i8(a, s));
+  };
+  auto quantise = [&](const void* v, int K, const int* len, const int* xidx) {
+    chk(sc::launch_quant_rows(v, 0, w.xq, w.xs, B, n, K, len, xidx, 1, s));
+  };
+  // y = LayerNorm(res_scale x + gate t) w + b on the survivors, and its 8-bit rows in place
+  auto norm = [&](const void* x, const int* xidx, const float* gate, const float* lw, const float* lb, void* y,
+                  bool q) {
+    sc::Norm a;
+    std::memset(&a, 0, sizeof(a));
+    a.x = x;
+    a.t = t;
+    a.gate = gate;
+    a.pre_w = lw;
+    a.pre_b = lb;
+    a.y = y;
+    a.yq = q ? w.yq : nullptr;
+    a.yscale = q ? w.ys : nullptr;
+    a.B = B;
+    a.n = n;
+    a.D = D;
+    a.len = rows.len_nxt;
+    a.xidx = xidx;
+    a.skip_pad = 1;
+    a.pre = 1;
+    a.gate_mode = gate ? SC_GATE_CHANNEL : SC_GATE_NONE;
+    a.eps = ln_eps;
+    a.scale = res_scale;
+    chk(sc::launch_block_norm(a, s));
+  };
+  const void* cur = x_in;
+  for (int l = 0; l < n_layers && chk.ok; ++l) {
+    const sc_layer_i8& y = layers[l];
+    void* nxt = l == n_layers - 1 ? x_out : (l & 1) ? w.xb : w.xa;
+    // the norm that ends a layer leaves the next one's rows quantised
+    if (l == 0) {
+      quantise(cur, D, rows.len_cur, nullptr);
+      linear(w.xq, w.xs, 1, y.qkv, w.qkv, D, 3 * D, rows.len_cur, 0);
+    } else {
+      linear(w.yq, w.ys, 0, y.qkv, w.qkv, D, 3 * D, rows.len_cur, 0);
+    }
+    attend_and_prune(d, w, rows, windows ? windows[l] : d->window, l, thresholds[l], keep_global, kept_per_layer, chk,
+                     s);
+    quantise(w.o, D, rows.len_nxt, w.keep_idx);
+    linear(w.xq, w.xs, 1, y.o, t, D, D, rows.len_nxt, 0);
+    norm(cur, w.keep_idx, y.gate1, y.ln1_w, y.ln1_b, w.x1, true);
+    linear(w.yq, w.ys, 0, y.w1, w.h, D, F, rows.len_nxt, 1);
+    quantise(w.h, F, rows.len_nxt, nullptr);
+    linear(w.xq, w.xs, 1, y.w2, t, F, D, rows.len_nxt, 0);
+    norm(w.x1, nullptr, y.gate2, y.ln2_w, y.ln2_b, nxt, l + 1 < n_layers);
+    cur = nxt;
+    rows.next();
+  }
+  chk(sc::launch_copy_i32(rows.len_cur, final_len, B, s));
+  if (orig_idx) chk(sc::launch_copy_i32(rows.orig_cur, orig_idx, (long long)bn, s));
+  return chk.ok ? SC_OK : SC_EHIP;
 }
 
 }  // namespace
 
 size_t sc_encoder_attn_stack_workspace_size(const sc_attn_desc* d, int32_t n_layers) {
   if (check_desc(d) != SC_OK || n_layers < 1) return 0;
-  return carve_stack(d, 0, nullptr, nullptr);
+  return carve_stack(d, 0, false, nullptr, nullptr);
 }
 
 static sc_status sc_encoder_attn_stack_impl(const sc_attn_desc* d, int32_t n_layers, const void* x_in,
@@ -739,9 +892,23 @@ sc_status sc_encoder_attn_stack(const sc_attn_desc* d, int32_t n_layers, const v
                                            final_len, orig_idx, kept_per_layer, workspace, ws_bytes, stream));
 }
 
+size_t sc_encoder_stack_i8_workspace_size(const sc_attn_desc* d, int32_t n_layers, int32_t ffn_dim) {
+  return check_stack_i8(d, n_layers, ffn_dim) == SC_OK ? carve_stack(d, ffn_dim, true, nullptr, nullptr) : 0;
+}
+
+sc_status sc_encoder_stack_i8(const sc_attn_desc* d, int32_t n_layers, const int32_t* windows, const void* x_in,
+                              const sc_layer_i8* layers, int32_t ffn_dim, const float* thresholds,
+                              int32_t keep_global, float ln_eps, float res_scale, void* x_out, int32_t* final_len,
+                              int32_t* orig_idx, int32_t* kept_per_layer, void* workspace, size_t ws_bytes,
+                              void* stream) {
+  SC_DEBUG_CALL(d, stream,
+                run_stack_i8(d, n_layers, windows, x_in, layers, ffn_dim, thresholds, keep_global, ln_eps, res_scale,
+                             x_out, final_len, orig_idx, kept_per_layer, workspace, ws_bytes, stream));
+}
+
 size_t sc_encoder_stack_workspace_size(const sc_attn_desc* d, int32_t n_layers, int32_t ffn_dim) {
   if (check_desc(d) != SC_OK || n_layers < 1 || ffn_dim <= 0) return 0;
-  return carve_stack(d, ffn_dim, nullptr, nullptr);
+  return carve_stack(d, ffn_dim, false, nullptr, nullptr);
 }
 
 static sc_status sc_encoder_stack_impl(const sc_attn_desc* d, int32_t n_layers, const int32_t* windows,

@@ -178,3 +178,40 @@ def test_binding_refuses_host_and_wrong_tensors():
         sc.sc_linear_i8(sc.LinearDesc(2, 8, 64, 64), [1.0], x, x)
     with pytest.raises(ValueError, match="SC_F32 or SC_BF16"):
         sc.sc_block_norm(norm_desc(dtype=sc.SC_I8), x, x)
+
+
+def stack_desc(**kw):
+    a = dict(B=2, n=256, H=2, window=64, valid_len=Addr(A[0]))
+    a.update(kw)
+    return sc.Desc(**a)
+
+
+def layer_i8(**kw):
+    w = (A[2], A[3], None)
+    parts = dict(qkv=w, o=w, w1=w, w2=w)
+    parts.update(kw)
+    return B._LayerI8(*(B._I8Weight(*parts[k]) for k in ("qkv", "o", "w1", "w2")), *([None] * 6))
+
+
+def test_stack_i8_refusals():
+    L = sc.load()
+    th = (ctypes.c_float * 1)(0.0)
+
+    def call(x=A[1], layer=None, layers=True, F=64, th=th, eps=1e-5, scale=1.0, out=A[4], fl=A[5], work=A[6], wb=1 << 32,
+             nl=1, windows=None, **kw):
+        arr = (B._LayerI8 * 1)(layer or layer_i8()) if layers else None
+        return L.sc_encoder_stack_i8(ctypes.byref(stack_desc(**kw).c()), nl, windows, x, arr, F, th, 1,
+                                     ctypes.c_float(eps), ctypes.c_float(scale), out, fl, None, None, work, wb, None)
+
+    for bad in (dict(nl=0), dict(F=0), dict(x=None), dict(layers=False), dict(th=None), dict(out=None), dict(fl=None),
+                dict(eps=0.0), dict(scale=float("nan")), dict(layer=layer_i8(w2=(None, A[3], None))),
+                dict(layer=layer_i8(o=(A[2], None, None))), dict(layer=layer_i8(qkv=(A[2] + 8, A[3], None))),
+                dict(windows=(ctypes.c_int32 * 1)(-1)), dict(out=A[1] + 64), dict(work=A[4]), dict(valid_len=None)):
+        assert call(**bad) == B.SC_EINVAL, bad
+    for big in (dict(dtype=sc.SC_F32), dict(causal=True), dict(B=8193, n=16), dict(H=33), dict(F=131073),
+                dict(B=64, n=16384, F=8192)):
+        assert call(**big) == B.SC_EUNSUPPORTED, big
+    need = sc.sc_encoder_stack_i8_workspace_size(stack_desc(), 1, 64)
+    assert need > 0 and sc.sc_encoder_stack_i8_workspace_size(stack_desc(), 1, 0) == 0
+    assert call(work=None) == B.SC_EWORKSPACE
+    assert call(wb=need - 1) == B.SC_EWORKSPACE
