@@ -63,92 +63,148 @@ struct RowReduce {
   }
 };
 
-// kVec consecutive elements as one access.
-template <int kVec>
-SC_DEV void load_vec(const float* p, float* v) {
-  if constexpr (kVec == 4) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(p);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = x[q];
-  } else {
-    v[0] = *p;
+// One access of a thread: kVec elements of T, as the bits that buffer loads and
+// stores move.
+template <typename T, int kVec>
+struct Bits;
+template <>
+struct Bits<float, 4> {
+  using Raw = __attribute__((ext_vector_type(4))) unsigned;
+  SC_DEV static Raw load(__amdgpu_buffer_rsrc_t r, int off) { return __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0); }
+  SC_DEV static void store(__amdgpu_buffer_rsrc_t r, int off, Raw v) {
+    __builtin_amdgcn_raw_buffer_store_b128(v, r, off, 0, 0);
   }
-}
-template <int kVec>
-SC_DEV void load_vec(const __bf16* p, float* v) {
-  if constexpr (kVec == 4) {
-    const bf16x4 x = *reinterpret_cast<const bf16x4*>(p);
+  SC_DEV static void unpack(Raw v, float* f) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = (float)x[q];
-  } else {
-    v[0] = (float)*p;
+    for (int q = 0; q < 4; ++q) {
+      const unsigned e = v[q];  // the bit cast of a vector's element reads its first one
+      f[q] = __builtin_bit_cast(float, e);
+    }
   }
-}
-template <int kVec>
-SC_DEV void store_vec(float* p, const float* v) {
-  if constexpr (kVec == 4)
-    *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-  else
-    *p = v[0];
-}
-template <int kVec>
-SC_DEV void store_vec(__bf16* p, const float* v) {
-  if constexpr (kVec == 4)
-    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-  else
-    *p = (__bf16)v[0];
+  SC_DEV static Raw pack(const float* f) {
+    return Raw{__builtin_bit_cast(unsigned, f[0]), __builtin_bit_cast(unsigned, f[1]),
+               __builtin_bit_cast(unsigned, f[2]), __builtin_bit_cast(unsigned, f[3])};
+  }
+};
+template <>
+struct Bits<__bf16, 4> {
+  using Raw = __attribute__((ext_vector_type(2))) unsigned;
+  SC_DEV static Raw load(__amdgpu_buffer_rsrc_t r, int off) { return __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0); }
+  SC_DEV static void store(__amdgpu_buffer_rsrc_t r, int off, Raw v) {
+    __builtin_amdgcn_raw_buffer_store_b64(v, r, off, 0, 0);
+  }
+  SC_DEV static void unpack(Raw v, float* f) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      f[2 * q] = __builtin_bit_cast(float, v[q] << 16);
+      f[2 * q + 1] = __builtin_bit_cast(float, v[q] & 0xffff0000u);
+    }
+  }
+  SC_DEV static Raw pack(const float* f) { return Raw{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])}; }
+};
+template <>
+struct Bits<float, 1> {
+  using Raw = unsigned;
+  SC_DEV static Raw load(__amdgpu_buffer_rsrc_t r, int off) { return __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0); }
+  SC_DEV static void store(__amdgpu_buffer_rsrc_t r, int off, Raw v) {
+    __builtin_amdgcn_raw_buffer_store_b32(v, r, off, 0, 0);
+  }
+  SC_DEV static void unpack(Raw v, float* f) { *f = __builtin_bit_cast(float, v); }
+  SC_DEV static Raw pack(const float* f) { return __builtin_bit_cast(unsigned, *f); }
+};
+template <>
+struct Bits<__bf16, 1> {
+  using Raw = unsigned short;
+  SC_DEV static Raw load(__amdgpu_buffer_rsrc_t r, int off) { return __builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0); }
+  SC_DEV static void store(__amdgpu_buffer_rsrc_t r, int off, Raw v) {
+    __builtin_amdgcn_raw_buffer_store_b16(v, r, off, 0, 0);
+  }
+  SC_DEV static void unpack(Raw v, float* f) { *f = __builtin_bit_cast(float, (unsigned)v << 16); }
+  SC_DEV static Raw pack(const float* f) { return __builtin_bit_cast(unsigned short, (__bf16)*f); }
+};
+
+// One row of a tensor as a buffer of its D elements: accesses beyond it load zeros
+// and store nothing, so the channels past D need no branch, nor does an absent
+// tensor (a buffer of no elements).  With a branch around each access the compiler
+// waited for every load on its own (backward of 32768 x 1024: 229 us).
+template <typename T>
+SC_DEV __amdgpu_buffer_rsrc_t row_buffer(const T* base, long long row, int D, bool present) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base) + row * D, 0, present ? D * (int)sizeof(T) : 0,
+                                           0x00027000);
 }
 
-// The channels of a thread: kPer groups of kVec, group u at (u kTpr + thread) kVec.
-template <int kVec, int kPer, int kTpr>
+// The channels of a thread: kPer accesses of kVec, access u at (u kTpr + thread)
+// kVec; kWidth of them in all, D used.
+template <typename T, int kVec, int kPer, int kTpr>
 struct Cols {
+  using B = Bits<T, kVec>;
+  using Raw = typename B::Raw;
+  static constexpr int kWidth = kVec * kPer * kTpr, kPerThread = kPer;
   int D, t;  // t: thread of the row
   SC_DEV int at(int u) const { return (u * kTpr + t) * kVec; }
   SC_DEV bool in(int u) const { return at(u) < D; }
-  template <typename T>
-  SC_DEV void load(const T* row, float* v) const {
+  SC_DEV void load(__amdgpu_buffer_rsrc_t r, Raw (&v)[kPer]) const {
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) v[u] = B::load(r, at(u) * (int)sizeof(T));
+  }
+  SC_DEV void unpack(const Raw (&r)[kPer], float* v) const {
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) B::unpack(r[u], v + u * kVec);
+  }
+  SC_DEV void store(__amdgpu_buffer_rsrc_t r, const float* v) const {
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) B::store(r, at(u) * (int)sizeof(T), B::pack(v + u * kVec));
+  }
+  SC_DEV void zero(__amdgpu_buffer_rsrc_t r) const {
+    const float z[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) B::store(r, at(u) * (int)sizeof(T), B::pack(z));
+  }
+  // one of the weight rows in LDS
+  SC_DEV void weights(const float* lds, float* v) const {
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
-      if (in(u)) {
-        load_vec<kVec>(row + at(u), v + u * kVec);
-      } else {
+      if constexpr (kVec == 4) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(lds + at(u));
 #pragma unroll
-        for (int q = 0; q < kVec; ++q) v[u * kVec + q] = 0.f;
+        for (int q = 0; q < 4; ++q) v[4 * u + q] = x[q];
+      } else {
+        v[u] = lds[at(u)];
       }
     }
   }
-  template <typename T>
-  SC_DEV void store(T* row, const float* v) const {
-#pragma unroll
-    for (int u = 0; u < kPer; ++u)
-      if (in(u)) store_vec<kVec>(row + at(u), v + u * kVec);
-  }
-  template <typename T>
-  SC_DEV void zero(T* row) const {
-    const float z[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int u = 0; u < kPer; ++u)
-      if (in(u)) store_vec<kVec>(row + at(u), z);
-  }
 };
+
+// Both norms' weights and a gate by channel in LDS, a row of kWidth each: absent
+// ones are 1 and 0, the channels past D are 0 (so that sums over them stay 0).
+enum { kPostW, kPostB, kPreW, kPreB, kGateRow, kWeights };
+template <int kWidth>
+SC_DEV void stage_weights(float* lds, const Norm& a) {
+  const float* src[kWeights] = {a.post_w, a.post_b, a.pre_w, a.pre_b,
+                                a.gate_mode == kGateChannel ? static_cast<const float*>(a.gate) : nullptr};
+#pragma unroll
+  for (int k = 0; k < kWeights; ++k)
+    for (int i = threadIdx.x; i < kWidth; i += blockDim.x)
+      lds[k * kWidth + i] = i >= a.D ? 0.f : src[k] ? src[k][i] : k == kPostB || k == kPreB ? 0.f : 1.f;
+  __syncthreads();
+}
 
 // v -> (v - mean) / sqrt(var + eps), or v / sqrt(mean(v^2) + eps); channels beyond
 // D stay 0.  Returns the factor.
-template <int kVec, int kPer, int kTpr>
-SC_DEV float normalise(float* v, const Cols<kVec, kPer, kTpr>& c, RowReduce<kTpr>& red, bool rms, float eps,
-                       float fd) {
-  constexpr int E = kVec * kPer;
+template <typename C, typename R, int E>
+SC_DEV float normalise(float (&v)[E], const C& c, R& red, bool rms, float eps, float fd) {
+  constexpr int kPer = C::kPerThread, kVec = E / kPer;
   if (!rms) {
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i) s += v[i];
     const float mean = red.sum(s) / fd;  // divided: a constant row has no deviation
 #pragma unroll
-    for (int u = 0; u < kPer; ++u)
-      if (c.in(u)) {
+    for (int u = 0; u < kPer; ++u) {
+      const float m = c.in(u) ? mean : 0.f;
 #pragma unroll
-        for (int q = 0; q < kVec; ++q) v[u * kVec + q] -= mean;
-      }
+      for (int q = 0; q < kVec; ++q) v[u * kVec + q] -= m;
+    }
   }
   float s = 0.f;
 #pragma unroll
@@ -159,103 +215,135 @@ SC_DEV float normalise(float* v, const Cols<kVec, kPer, kTpr>& c, RowReduce<kTpr
   return inv;
 }
 
-// v = v w + b (w, b: or null)
-template <int kVec, int kPer, int kTpr>
-SC_DEV void affine(float* v, const float* w, const float* b, const Cols<kVec, kPer, kTpr>& c) {
-  constexpr int E = kVec * kPer;
+// v = v w + b from the weight rows
+template <typename C, int E>
+SC_DEV void affine(float (&v)[E], const float* lds, int w, int b, const C& c) {
+  float p[E], q[E];
+  c.weights(lds + w * C::kWidth, p);
+  c.weights(lds + b * C::kWidth, q);
+#pragma unroll
+  for (int i = 0; i < E; ++i) v[i] = fmaf(v[i], p[i], q[i]);
+}
+template <typename C, int E>
+SC_DEV void times(float (&v)[E], const float* lds, int w, const C& c) {
   float p[E];
-  if (w) {
-    c.load(w, p);
+  c.weights(lds + w * C::kWidth, p);
 #pragma unroll
-    for (int i = 0; i < E; ++i) v[i] *= p[i];
-  }
-  if (b) {
-    c.load(b, p);
-#pragma unroll
-    for (int i = 0; i < E; ++i) v[i] += p[i];
-  }
+  for (int i = 0; i < E; ++i) v[i] *= p[i];
 }
 
-template <typename T, int kVec, int kPer, int kTpr>
-SC_DEV void load_gate(float* g, const Norm& a, long long row, int b, const Cols<kVec, kPer, kTpr>& c) {
-  if (a.gate_mode == kGateChannel)
-    c.load(static_cast<const float*>(a.gate), g);
-  else
-    c.load(static_cast<const T*>(a.gate) + (a.gate_mode == kGateSequence ? b : row) * (long long)a.D, g);
+// A word of an array that the launch does not write, at a wave-uniform index: by a
+// scalar load, which does not wait for the rows in flight.
+SC_DEV int scalar_load(const int* p, long long i) {
+  return ((const __attribute__((address_space(4))) int*)p)[i];
 }
 
-// Rows dealt round-robin over the launch's row slots.
+// A row's sequence and whether it is padding; all of it wave-uniform.
+struct RowAt {
+  unsigned row;
+  int b;
+  bool live;
+};
+SC_DEV RowAt row_at(const Norm& a, unsigned row, bool exists) {
+  RowAt r;
+  r.row = row;
+  r.b = exists ? (int)(row / (unsigned)a.n) : 0;
+  r.live = exists && (!a.len || (int)(row - (unsigned)r.b * a.n) < clampi(scalar_load(a.len, r.b), 0, a.n));
+  return r;
+}
+// The gate's row of a gate by sequence or token.
+SC_DEV long long gate_row(const Norm& a, const RowAt& r) {
+  return a.gate_mode == kGateSequence ? (long long)r.b : (long long)r.row;
+}
+SC_DEV bool gate_rows(const Norm& a) { return a.gate_mode >= kGateSequence; }
+
+// Rows dealt round-robin over the launch's row slots.  The next row's loads are in
+// flight while a row is computed, the first row's while the weights are staged.
 template <typename T, int kVec, int kPer, int kTpr>
 __global__ __launch_bounds__(kThreads<kTpr>) void k_norm(Norm a) {
   constexpr int E = kVec * kPer, kRows = kThreads<kTpr> / kTpr;
+  using C = Cols<T, kVec, kPer, kTpr>;
   __shared__ float slots[2 * kTpr / 64];
+  __shared__ __attribute__((aligned(16))) float lw[kWeights * C::kWidth];
   RowReduce<kTpr> red{slots};
-  const Cols<kVec, kPer, kTpr> c{a.D, (int)threadIdx.x % kTpr};
+  const C c{a.D, (int)threadIdx.x % kTpr};
   const float fd = (float)a.D;
   const int Dp = (a.D + kI8Pitch - 1) / kI8Pitch * kI8Pitch;
-  const long long rows = (long long)a.B * a.n;
-  const int slot = kTpr == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
-  for (long long row = (long long)blockIdx.x * kRows + slot; row < rows; row += (long long)gridDim.x * kRows) {
-    const int b = (int)(row / a.n), j = (int)(row - (long long)b * a.n);
-    T* r = static_cast<T*>(a.r) + row * a.D;
-    T* y = static_cast<T*>(a.y) + row * a.D;
+  const unsigned rows = (unsigned)a.B * (unsigned)a.n, step = gridDim.x * kRows;
+  const unsigned slot = kTpr == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+  typename C::Raw rx[kPer], rt[kPer], rg[kPer];
+  auto fetch = [&](const RowAt& r) {
+    long long from = r.row;
+    if (a.xidx && r.live) from = (long long)r.b * a.n + clampi(scalar_load(a.xidx, r.row), 0, a.n - 1);
+    c.load(row_buffer(static_cast<const T*>(a.x), from, a.D, r.live), rx);
+    c.load(row_buffer(static_cast<const T*>(a.t), r.row, a.D, r.live && a.t), rt);
+    if (gate_rows(a)) c.load(row_buffer(static_cast<const T*>(a.gate), gate_row(a, r), a.D, r.live), rg);
+  };
+  RowAt cur = row_at(a, blockIdx.x * kRows + slot, blockIdx.x * kRows + slot < rows);
+  fetch(cur);
+  stage_weights<C::kWidth>(lw, a);
+  for (; cur.row < rows;) {
+    const unsigned nrow = cur.row + step;  // below 2^31 + 2^24
+    const RowAt next = row_at(a, nrow, nrow < rows);
+    const long long row = cur.row;
+    const auto r = row_buffer(static_cast<const T*>(a.r), row, a.D, a.r);
+    const auto y = row_buffer(static_cast<const T*>(a.y), row, a.D, a.y);
     int8_t* yq = a.yq + row * Dp;
-    if (a.len && j >= clampi(a.len[b], 0, a.n)) {
-      if (a.skip_pad) continue;
-      if (a.r) c.zero(r);
-      if (a.y) c.zero(y);
-      if (a.yq) {
-        for (int k = 4 * c.t; k < Dp; k += 4 * kTpr) *reinterpret_cast<unsigned*>(yq + k) = 0u;
-        if (c.t == 0) a.yscale[row] = 0.f;
-      }
-      continue;
-    }
-    const long long from = a.xidx ? row - j + clampi(a.xidx[row], 0, a.n - 1) : row;
-    float x[E], v[E];
-    c.load(static_cast<const T*>(a.x) + from * a.D, x);
-#pragma unroll
-    for (int i = 0; i < E; ++i) x[i] *= a.scale;
-    if (a.t) {
-      c.load(static_cast<const T*>(a.t) + row * a.D, v);
-      float g[E];
-      if (a.gate_mode) load_gate<T>(g, a, row, b, c);
-      if (a.post) {
-        normalise(v, c, red, a.rms, a.eps, fd);
-        affine(v, a.post_w, a.post_b, c);
-      }
-      if (a.gate_mode) {
-#pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = fmaf(g[i], v[i], x[i]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < E; ++i) x[i] += v[i];
-      }
-    }
-    if (a.r) c.store(r, x);
-    if (!a.pre) continue;
-    normalise(x, c, red, a.rms, a.eps, fd);
-    affine(x, a.pre_w, a.pre_b, c);
-    if (a.y) c.store(y, x);
-    if (a.yq) {  // the stored values, in the row's type
-      float m = 0.f;
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        x[i] = (float)(T)x[i];
-        m = vmax(m, fabsf(x[i]));
-      }
-      const RowQuant q = row_quant(red.max(m));
-#pragma unroll
-      for (int u = 0; u < kPer; ++u) {
-        if constexpr (kVec == 4) {
-          const unsigned p = pack_i8(quant_one<T>(q, x[4 * u]), quant_one<T>(q, x[4 * u + 1]),
-                                     quant_one<T>(q, x[4 * u + 2]), quant_one<T>(q, x[4 * u + 3]));
-          if (c.at(u) < Dp) *reinterpret_cast<unsigned*>(yq + c.at(u)) = p & q.live;
-        } else {
-          if (c.at(u) < Dp) yq[c.at(u)] = (int8_t)(quant_one<T>(q, x[u]) & q.live);
+    if (!cur.live) {
+      fetch(next);
+      if (!a.skip_pad) {
+        if (a.r) c.zero(r);
+        if (a.y) c.zero(y);
+        if (a.yq) {
+          for (int k = 4 * c.t; k < Dp; k += 4 * kTpr) *reinterpret_cast<unsigned*>(yq + k) = 0u;
+          if (c.t == 0) a.yscale[row] = 0.f;
         }
       }
-      if (c.t == 0) a.yscale[row] = q.scale;
+      cur = next;
+      continue;
     }
+    float x[E], v[E], g[E];
+    c.unpack(rx, x);
+    c.unpack(rt, v);
+    if (gate_rows(a))
+      c.unpack(rg, g);
+    else
+      c.weights(lw + kGateRow * C::kWidth, g);
+    fetch(next);
+    if (a.post) {
+      normalise(v, c, red, a.rms, a.eps, fd);
+      affine(v, lw, kPostW, kPostB, c);
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] = fmaf(g[i], v[i], a.scale * x[i]);
+    if (a.r) c.store(r, x);
+    if (a.pre) {
+      normalise(x, c, red, a.rms, a.eps, fd);
+      affine(x, lw, kPreW, kPreB, c);
+      if (a.y) c.store(y, x);
+      if (a.yq) {  // the stored values, in the row's type
+        float m = 0.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          x[i] = (float)(T)x[i];
+          m = vmax(m, fabsf(x[i]));
+        }
+        const RowQuant q = row_quant(red.max(m));
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+          if (c.at(u) >= Dp) continue;
+          if constexpr (kVec == 4) {
+            const unsigned p = pack_i8(quant_one<T>(q, x[4 * u]), quant_one<T>(q, x[4 * u + 1]),
+                                       quant_one<T>(q, x[4 * u + 2]), quant_one<T>(q, x[4 * u + 3]));
+            *reinterpret_cast<unsigned*>(yq + c.at(u)) = p & q.live;
+          } else {
+            yq[c.at(u)] = (int8_t)(quant_one<T>(q, x[u]) & q.live);
+          }
+        }
+        if (c.t == 0) a.yscale[row] = q.scale;
+      }
+    }
+    cur = next;
   }
 }
 
@@ -269,10 +357,8 @@ __global__ __launch_bounds__(kThreads<kTpr>) void k_norm(Norm a) {
 // rows unless the gate goes by sequence), keeps the sums of its channels in
 // registers, adds its row slots in order through LDS and leaves one partial
 // record; k_norm_sums adds the records in order.
-template <int kVec, int kPer, int kTpr>
-SC_DEV void norm_input_grad(float* g, const float* hat, float inv, const Cols<kVec, kPer, kTpr>& c,
-                            RowReduce<kTpr>& red, bool rms, float fd) {
-  constexpr int E = kVec * kPer;
+template <typename R, int E>
+SC_DEV void norm_input_grad(float (&g)[E], const float (&hat)[E], float inv, R& red, bool rms, float fd) {
   float s = 0.f, m = 0.f;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
@@ -282,10 +368,11 @@ SC_DEV void norm_input_grad(float* g, const float* hat, float inv, const Cols<kV
   s = red.sum(s) / fd;
   m = rms ? 0.f : red.sum(m) / fd;
 #pragma unroll
-  for (int i = 0; i < E; ++i) g[i] = inv * (g[i] - m - hat[i] * s);
+  for (int i = 0; i < E; ++i) g[i] = inv * (g[i] - fmaf(hat[i], s, m));
 }
 
-constexpr int kNormBlocks = 512;  // blocks of the backward launch at most
+constexpr int kNormFwdBlocks = 2048;  // blocks of the forward launch at most
+constexpr int kNormBlocks = 512;      // and of the backward launch
 enum { kSumPreW, kSumPreB, kSumPostW, kSumPostB, kSumGate, kSums };
 
 struct NormPlan {
@@ -303,107 +390,119 @@ NormPlan norm_plan(const Norm& a, int rows_per_block, bool seq) {
   return p;
 }
 
-// Adds the kRows row slots of v in order and stores the sum of the block's
-// channels at out.  buf: LDS, kRows x D floats for kRows > 1.
-template <int kVec, int kPer, int kTpr>
-SC_DEV void block_sum(const float* v, float* out, float* buf, const Cols<kVec, kPer, kTpr>& c) {
-  constexpr int kRows = kThreads<kTpr> / kTpr;
-  if constexpr (kRows == 1) {
-    c.store(out, v);
-  } else {
-    __syncthreads();
-    c.store(buf + (threadIdx.x / kTpr) * c.D, v);
-    __syncthreads();
-    for (int k = threadIdx.x; k < c.D; k += 256) {
-      float s = buf[k];
+// Adds the row slots of v in order and stores the sum of the block's channels at
+// out.  buf: LDS, kRows x kWidth floats.
+template <typename C, int kRows, int E>
+SC_DEV void block_sum(const float (&v)[E], float* out, float* buf, const C& c) {
+  constexpr int kPer = C::kPerThread, kVec = E / kPer;
+  const int slot = threadIdx.x / (blockDim.x / kRows);
+  __syncthreads();
 #pragma unroll
-      for (int i = 1; i < kRows; ++i) s += buf[i * c.D + k];
-      out[k] = s;
-    }
+  for (int u = 0; u < kPer; ++u)
+#pragma unroll
+    for (int q = 0; q < kVec; ++q) buf[slot * C::kWidth + c.at(u) + q] = v[u * kVec + q];
+  __syncthreads();
+  for (int k = threadIdx.x; k < c.D; k += blockDim.x) {
+    float s = buf[k];
+#pragma unroll
+    for (int i = 1; i < kRows; ++i) s += buf[i * C::kWidth + k];
+    out[k] = s;
   }
 }
 
 template <typename T, int kVec, int kPer, int kTpr>
-__global__ __launch_bounds__(kThreads<kTpr>) void k_norm_bwd(Norm a, NormPlan pl) {
+__global__ __launch_bounds__(kThreads<kTpr>) __attribute__((amdgpu_waves_per_eu(2))) void k_norm_bwd(Norm a, NormPlan pl) {
   constexpr int E = kVec * kPer, kRows = kThreads<kTpr> / kTpr;
-  extern __shared__ __attribute__((aligned(16))) float buf[];
+  using C = Cols<T, kVec, kPer, kTpr>;
   __shared__ float slots[2 * kTpr / 64];
+  __shared__ __attribute__((aligned(16))) float lw[kWeights * C::kWidth];  // the row slots' sums at the end
+  static_assert(kRows <= kWeights, "sums of the row slots");
   RowReduce<kTpr> red{slots};
-  const Cols<kVec, kPer, kTpr> c{a.D, (int)threadIdx.x % kTpr};
+  const C c{a.D, (int)threadIdx.x % kTpr};
   const float fd = (float)a.D;
-  const int slot = kTpr == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+  const unsigned slot = kTpr == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
   const bool seq = norm_seq(a);
   float sum[kSums][E];
 #pragma unroll
   for (int k = 0; k < kSums; ++k)
 #pragma unroll
     for (int i = 0; i < E; ++i) sum[k][i] = 0.f;
-  const long long items = (long long)pl.Bs * pl.nch;
+  typename C::Raw rx[kPer], rt[kPer], rg[kPer], rr[kPer], ry[kPer];
+  auto fetch = [&](const RowAt& r) {
+    c.load(row_buffer(static_cast<const T*>(a.t), r.row, a.D, r.live && a.t), rt);
+    c.load(row_buffer(static_cast<const T*>(a.x), r.row, a.D, r.live), rx);
+    if (gate_rows(a)) c.load(row_buffer(static_cast<const T*>(a.gate), gate_row(a, r), a.D, r.live), rg);
+    c.load(row_buffer(static_cast<const T*>(a.dy), r.row, a.D, r.live && a.dy), ry);
+    c.load(row_buffer(static_cast<const T*>(a.dr), r.row, a.D, r.live && a.dr), rr);
+  };
+  const unsigned items = (unsigned)pl.Bs * (unsigned)pl.nch, step = (unsigned)pl.nch * kRows;
   float* gpart = a.ws + (long long)pl.blocks * kSums * a.D;
-  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
-    const int bs = (int)(it / pl.nch), ch = (int)(it - (long long)bs * pl.nch);
-    for (long long k = ch * kRows + slot; k < pl.ns; k += pl.nch * kRows) {
-      const long long row = (long long)bs * pl.ns + k;
-      const int b = (int)(row / a.n), j = (int)(row - (long long)b * a.n);
-      if (a.len && j >= clampi(a.len[b], 0, a.n)) {
-        if (a.dx) c.zero(static_cast<T*>(a.dx) + row * a.D);
-        if (a.dt) c.zero(static_cast<T*>(a.dt) + row * a.D);
-        if (a.dgate && a.gate_mode == kGateToken) c.zero(static_cast<T*>(a.dgate) + row * a.D);
+  bool staged = false;
+  for (unsigned it = blockIdx.x; it < items; it += gridDim.x) {
+    const unsigned bs = it / (unsigned)pl.nch, first = bs * (unsigned)pl.ns;
+    const unsigned end = first + (unsigned)pl.ns;  // this item's rows: below 2^31
+    unsigned row = first + (it - bs * (unsigned)pl.nch) * kRows + slot;
+    RowAt cur = row_at(a, row, row < end);
+    fetch(cur);
+    if (!staged) stage_weights<C::kWidth>(lw, a);
+    staged = true;
+    for (; cur.row < end;) {
+      const RowAt next = row_at(a, cur.row + step, cur.row + step < end);
+      const auto dx = row_buffer(static_cast<const T*>(a.dx), cur.row, a.D, a.dx);
+      const auto dt = row_buffer(static_cast<const T*>(a.dt), cur.row, a.D, a.dt);
+      const bool token = a.dgate && a.gate_mode == kGateToken;
+      const auto dg = row_buffer(static_cast<const T*>(a.dgate), cur.row, a.D, token);
+      if (!cur.live) {
+        fetch(next);
+        c.zero(dx);
+        c.zero(dt);
+        if (token) c.zero(dg);
+        cur = next;
         continue;
       }
-      float x[E], that[E], g[E], dr[E], dy[E], tinv = 0.f;
-      c.load(static_cast<const T*>(a.x) + row * a.D, x);
-      if (a.t) c.load(static_cast<const T*>(a.t) + row * a.D, that);
-      if (a.gate_mode) load_gate<T>(g, a, row, b, c);
-      if (a.dr) {
-        c.load(static_cast<const T*>(a.dr) + row * a.D, dr);
-      } else {
-#pragma unroll
-        for (int i = 0; i < E; ++i) dr[i] = 0.f;
-      }
-      if (a.dy) c.load(static_cast<const T*>(a.dy) + row * a.D, dy);
+      float x[E], that[E], g[E], dr[E], dy[E], u[E], tinv = 0.f;
+      c.unpack(rt, that);
+      c.unpack(rx, x);
+      if (gate_rows(a))
+        c.unpack(rg, g);
+      else
+        c.weights(lw + kGateRow * C::kWidth, g);
+      c.unpack(ry, dy);
+      c.unpack(rr, dr);
+      fetch(next);
       if (a.post) tinv = normalise(that, c, red, a.rms, a.eps, fd);
-      // u, in its place of use: r below and dgate
-      float u[E];
-      if (a.t) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) u[i] = that[i];
-        if (a.post) affine(u, a.post_w, a.post_b, c);
-      } else {
-#pragma unroll
-        for (int i = 0; i < E; ++i) u[i] = 0.f;
-      }
+      for (int i = 0; i < E; ++i) u[i] = that[i];
+      if (a.post) affine(u, lw, kPostW, kPostB, c);
       if (a.dy) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = fmaf(a.gate_mode ? g[i] : 1.f, u[i], a.scale * x[i]);
+        for (int i = 0; i < E; ++i) x[i] = fmaf(g[i], u[i], a.scale * x[i]);
         const float rinv = normalise(x, c, red, a.rms, a.eps, fd);
 #pragma unroll
         for (int i = 0; i < E; ++i) {
           sum[kSumPreW][i] = fmaf(dy[i], x[i], sum[kSumPreW][i]);
           sum[kSumPreB][i] += dy[i];
         }
-        affine(dy, a.pre_w, nullptr, c);
-        norm_input_grad(dy, x, rinv, c, red, a.rms, fd);
+        times(dy, lw, kPreW, c);
+        norm_input_grad(dy, x, rinv, red, a.rms, fd);
 #pragma unroll
         for (int i = 0; i < E; ++i) dr[i] += dy[i];
       }
-      if (a.dx) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = a.scale * dr[i];
-        c.store(static_cast<T*>(a.dx) + row * a.D, x);
-      }
-      if (!a.t) continue;
+      for (int i = 0; i < E; ++i) x[i] = a.scale * dr[i];
+      c.store(dx, x);
       if (a.gate_mode) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) u[i] *= dr[i];
-        if (a.dgate && a.gate_mode == kGateToken) {
-          c.store(static_cast<T*>(a.dgate) + row * a.D, u);
+        for (int i = 0; i < E; ++i) {
+          u[i] *= dr[i];
+          dr[i] *= g[i];
+        }
+        if (token) {
+          c.store(dg, u);
         } else {
 #pragma unroll
           for (int i = 0; i < E; ++i) sum[kSumGate][i] += u[i];
         }
-#pragma unroll
-        for (int i = 0; i < E; ++i) dr[i] *= g[i];
       }
       if (a.post) {
 #pragma unroll
@@ -411,23 +510,26 @@ __global__ __launch_bounds__(kThreads<kTpr>) void k_norm_bwd(Norm a, NormPlan pl
           sum[kSumPostW][i] = fmaf(dr[i], that[i], sum[kSumPostW][i]);
           sum[kSumPostB][i] += dr[i];
         }
-        affine(dr, a.post_w, nullptr, c);
-        norm_input_grad(dr, that, tinv, c, red, a.rms, fd);
+        times(dr, lw, kPostW, c);
+        norm_input_grad(dr, that, tinv, red, a.rms, fd);
       }
-      if (a.dt) c.store(static_cast<T*>(a.dt) + row * a.D, dr);
+      c.store(dt, dr);
+      cur = next;
     }
     if (seq) {
-      block_sum(sum[kSumGate], gpart + it * a.D, buf, c);
+      block_sum<C, kRows>(sum[kSumGate], gpart + (long long)it * a.D, lw, c);
+      staged = false;  // the weights are gone
+      __syncthreads();
 #pragma unroll
       for (int i = 0; i < E; ++i) sum[kSumGate][i] = 0.f;
     }
   }
   float* part = a.ws + (long long)blockIdx.x * kSums * a.D;
-  if (a.dpre_w) block_sum(sum[kSumPreW], part + kSumPreW * a.D, buf, c);
-  if (a.dpre_b) block_sum(sum[kSumPreB], part + kSumPreB * a.D, buf, c);
-  if (a.dpost_w) block_sum(sum[kSumPostW], part + kSumPostW * a.D, buf, c);
-  if (a.dpost_b) block_sum(sum[kSumPostB], part + kSumPostB * a.D, buf, c);
-  if (a.dgate && a.gate_mode == kGateChannel) block_sum(sum[kSumGate], part + kSumGate * a.D, buf, c);
+  if (a.dpre_w) block_sum<C, kRows>(sum[kSumPreW], part + kSumPreW * a.D, lw, c);
+  if (a.dpre_b) block_sum<C, kRows>(sum[kSumPreB], part + kSumPreB * a.D, lw, c);
+  if (a.dpost_w) block_sum<C, kRows>(sum[kSumPostW], part + kSumPostW * a.D, lw, c);
+  if (a.dpost_b) block_sum<C, kRows>(sum[kSumPostB], part + kSumPostB * a.D, lw, c);
+  if (a.dgate && a.gate_mode == kGateChannel) block_sum<C, kRows>(sum[kSumGate], part + kSumGate * a.D, lw, c);
 }
 
 // 64 channels of one output a workgroup: 16 waves add every 16th record in
@@ -510,7 +612,7 @@ hipError_t run_norm(const Norm& a, hipStream_t s) {
     using S = decltype(shape);
     constexpr int kT = kThreads<S::kTpr>;
     const long long rows = (long long)a.B * a.n, per = kT / S::kTpr;
-    const unsigned blocks = (unsigned)std::min<long long>((rows + per - 1) / per, 8192);
+    const unsigned blocks = (unsigned)std::min<long long>((rows + per - 1) / per, kNormFwdBlocks);
     hipLaunchKernelGGL((k_norm<T, S::kVec, S::kPer, S::kTpr>), dim3(blocks), dim3(kT), 0, s, a);
     return hipGetLastError();
   });
