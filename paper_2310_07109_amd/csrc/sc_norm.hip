@@ -160,18 +160,19 @@ struct Cols {
 #pragma unroll
     for (int u = 0; u < kPer; ++u) B::store(r, at(u) * (int)sizeof(T), B::pack(z));
   }
-  // one of the weight rows in LDS
+  // access u of one of the weight rows in LDS, or all of it
+  SC_DEV void weight(const float* lds, int u, float* v) const {
+    if constexpr (kVec == 4) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(lds + at(u));
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = x[q];
+    } else {
+      *v = lds[at(u)];
+    }
+  }
   SC_DEV void weights(const float* lds, float* v) const {
 #pragma unroll
-    for (int u = 0; u < kPer; ++u) {
-      if constexpr (kVec == 4) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(lds + at(u));
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[4 * u + q] = x[q];
-      } else {
-        v[u] = lds[at(u)];
-      }
-    }
+    for (int u = 0; u < kPer; ++u) weight(lds, u, v + u * kVec);
   }
 };
 
@@ -179,12 +180,12 @@ struct Cols {
 // ones are 1 and 0, the channels past D are 0 (so that sums over them stay 0).
 enum { kPostW, kPostB, kPreW, kPreB, kGateRow, kWeights };
 template <int kWidth>
-SC_DEV void stage_weights(float* lds, const Norm& a) {
+SC_DEV void stage_weights(float* lds, const Norm& a, int count) {
   const float* src[kWeights] = {a.post_w, a.post_b, a.pre_w, a.pre_b,
                                 a.gate_mode == kGateChannel ? static_cast<const float*>(a.gate) : nullptr};
 #pragma unroll
   for (int k = 0; k < kWeights; ++k)
-    for (int i = threadIdx.x; i < kWidth; i += blockDim.x)
+    for (int i = k < count ? (int)threadIdx.x : kWidth; i < kWidth; i += blockDim.x)
       lds[k * kWidth + i] = i >= a.D ? 0.f : src[k] ? src[k][i] : k == kPostB || k == kPreB ? 0.f : 1.f;
   __syncthreads();
 }
@@ -281,7 +282,7 @@ __global__ __launch_bounds__(kThreads<kTpr>) void k_norm(Norm a) {
   };
   RowAt cur = row_at(a, blockIdx.x * kRows + slot, blockIdx.x * kRows + slot < rows);
   fetch(cur);
-  stage_weights<C::kWidth>(lw, a);
+  stage_weights<C::kWidth>(lw, a, kWeights);
   for (; cur.row < rows;) {
     const unsigned nrow = cur.row + step;  // below 2^31 + 2^24
     const RowAt next = row_at(a, nrow, nrow < rows);
@@ -379,8 +380,8 @@ struct NormPlan {
   int Bs, ns;       // sequences and rows of each, as the items see them
   int nch, blocks;  // parts of a sequence, blocks of the launch
 };
-SC_DEV __host__ bool norm_seq(const Norm& a) { return a.gate_mode == kGateSequence && a.dgate; }
-NormPlan norm_plan(const Norm& a, int rows_per_block, bool seq) {
+NormPlan norm_plan(const Norm& a, int rows_per_block) {
+  const bool seq = a.gate_mode == kGateSequence;
   NormPlan p;
   p.Bs = seq ? a.B : 1;
   p.ns = seq ? a.n : a.B * a.n;
@@ -410,28 +411,32 @@ SC_DEV void block_sum(const float (&v)[E], float* out, float* buf, const C& c) {
   }
 }
 
-template <typename T, int kVec, int kPer, int kTpr>
-__global__ __launch_bounds__(kThreads<kTpr>) __attribute__((amdgpu_waves_per_eu(2))) void k_norm_bwd(Norm a, NormPlan pl) {
+// kToken: a gate by token, read with the rows; else the gate's row (of ones, the
+// channels' or the sequence's) is in LDS.  Weights and gate are read from LDS
+// where they are used, u is made twice: at 16 channels a thread the sums, the rows
+// in flight and the row at hand leave no registers for them.
+template <typename T, int kVec, int kPer, int kTpr, bool kToken>
+__global__ __launch_bounds__(kThreads<kTpr>) __attribute__((amdgpu_waves_per_eu(2))) void k_norm_bwd(Norm a,
+                                                                                                     NormPlan pl) {
   constexpr int E = kVec * kPer, kRows = kThreads<kTpr> / kTpr;
   using C = Cols<T, kVec, kPer, kTpr>;
   __shared__ float slots[2 * kTpr / 64];
-  __shared__ __attribute__((aligned(16))) float lw[kWeights * C::kWidth];  // the row slots' sums at the end
-  static_assert(kRows <= kWeights, "sums of the row slots");
+  __shared__ __attribute__((aligned(16))) float lw[kWeights * C::kWidth], buf[kRows * C::kWidth];
   RowReduce<kTpr> red{slots};
   const C c{a.D, (int)threadIdx.x % kTpr};
   const float fd = (float)a.D;
   const unsigned slot = kTpr == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
-  const bool seq = norm_seq(a);
+  const bool seq = a.gate_mode == kGateSequence;
   float sum[kSums][E];
 #pragma unroll
   for (int k = 0; k < kSums; ++k)
 #pragma unroll
     for (int i = 0; i < E; ++i) sum[k][i] = 0.f;
-  typename C::Raw rx[kPer], rt[kPer], rg[kPer], rr[kPer], ry[kPer];
+  typename C::Raw rx[kPer], rt[kPer], rg[kToken ? kPer : 1], rr[kPer], ry[kPer];
   auto fetch = [&](const RowAt& r) {
     c.load(row_buffer(static_cast<const T*>(a.t), r.row, a.D, r.live && a.t), rt);
     c.load(row_buffer(static_cast<const T*>(a.x), r.row, a.D, r.live), rx);
-    if (gate_rows(a)) c.load(row_buffer(static_cast<const T*>(a.gate), gate_row(a, r), a.D, r.live), rg);
+    if constexpr (kToken) c.load(row_buffer(static_cast<const T*>(a.gate), r.row, a.D, r.live), rg);
     c.load(row_buffer(static_cast<const T*>(a.dy), r.row, a.D, r.live && a.dy), ry);
     c.load(row_buffer(static_cast<const T*>(a.dr), r.row, a.D, r.live && a.dr), rr);
   };
@@ -441,42 +446,67 @@ __global__ __launch_bounds__(kThreads<kTpr>) __attribute__((amdgpu_waves_per_eu(
   for (unsigned it = blockIdx.x; it < items; it += gridDim.x) {
     const unsigned bs = it / (unsigned)pl.nch, first = bs * (unsigned)pl.ns;
     const unsigned end = first + (unsigned)pl.ns;  // this item's rows: below 2^31
-    unsigned row = first + (it - bs * (unsigned)pl.nch) * kRows + slot;
+    const unsigned row = first + (it - bs * (unsigned)pl.nch) * kRows + slot;
     RowAt cur = row_at(a, row, row < end);
     fetch(cur);
-    if (!staged) stage_weights<C::kWidth>(lw, a);
+    if (seq) {
+      __syncthreads();  // the last item's rows are done
+      const T* g = static_cast<const T*>(a.gate) + (long long)bs * a.D;
+      for (int i = threadIdx.x; i < C::kWidth; i += blockDim.x) lw[kGateRow * C::kWidth + i] = i < a.D ? (float)g[i] : 0.f;
+      if (staged) __syncthreads();
+    }
+    if (!staged) stage_weights<C::kWidth>(lw, a, seq ? kGateRow : kWeights);
     staged = true;
     for (; cur.row < end;) {
       const RowAt next = row_at(a, cur.row + step, cur.row + step < end);
       const auto dx = row_buffer(static_cast<const T*>(a.dx), cur.row, a.D, a.dx);
       const auto dt = row_buffer(static_cast<const T*>(a.dt), cur.row, a.D, a.dt);
-      const bool token = a.dgate && a.gate_mode == kGateToken;
-      const auto dg = row_buffer(static_cast<const T*>(a.dgate), cur.row, a.D, token);
+      const auto dg = row_buffer(static_cast<const T*>(a.dgate), cur.row, a.D, kToken && a.dgate);
       if (!cur.live) {
         fetch(next);
         c.zero(dx);
         c.zero(dt);
-        if (token) c.zero(dg);
+        if (kToken) c.zero(dg);
         cur = next;
         continue;
       }
-      float x[E], that[E], g[E], dr[E], dy[E], u[E], tinv = 0.f;
+      float x[E], that[E], g[E], dr[E], dy[E], tinv = 0.f;
       c.unpack(rt, that);
       c.unpack(rx, x);
-      if (gate_rows(a))
-        c.unpack(rg, g);
-      else
-        c.weights(lw + kGateRow * C::kWidth, g);
+      if constexpr (kToken) c.unpack(rg, g);
       c.unpack(ry, dy);
       c.unpack(rr, dr);
       fetch(next);
       if (a.post) tinv = normalise(that, c, red, a.rms, a.eps, fd);
+      // u of access k, and the gate unless it came with the row
+      auto block = [&](int k, float (&u)[kVec]) {
+        float w[kVec], b[kVec];
 #pragma unroll
-      for (int i = 0; i < E; ++i) u[i] = that[i];
-      if (a.post) affine(u, lw, kPostW, kPostB, c);
+        for (int q = 0; q < kVec; ++q) u[q] = that[k * kVec + q];
+        if (a.post) {
+          c.weight(lw + kPostW * C::kWidth, k, w);
+          c.weight(lw + kPostB * C::kWidth, k, b);
+#pragma unroll
+          for (int q = 0; q < kVec; ++q) u[q] = fmaf(u[q], w[q], b[q]);
+        }
+      };
+      auto gate = [&](int k, float (&v)[kVec]) {
+        if constexpr (kToken) {
+#pragma unroll
+          for (int q = 0; q < kVec; ++q) v[q] = g[k * kVec + q];
+        } else {
+          c.weight(lw + kGateRow * C::kWidth, k, v);
+        }
+      };
       if (a.dy) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = fmaf(g[i], u[i], a.scale * x[i]);
+        for (int k = 0; k < kPer; ++k) {
+          float u[kVec], v[kVec];
+          block(k, u);
+          gate(k, v);
+#pragma unroll
+          for (int q = 0; q < kVec; ++q) x[k * kVec + q] = fmaf(v[q], u[q], a.scale * x[k * kVec + q]);
+        }
         const float rinv = normalise(x, c, red, a.rms, a.eps, fd);
 #pragma unroll
         for (int i = 0; i < E; ++i) {
@@ -493,16 +523,21 @@ __global__ __launch_bounds__(kThreads<kTpr>) __attribute__((amdgpu_waves_per_eu(
       c.store(dx, x);
       if (a.gate_mode) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-          u[i] *= dr[i];
-          dr[i] *= g[i];
-        }
-        if (token) {
-          c.store(dg, u);
-        } else {
+        for (int k = 0; k < kPer; ++k) {
+          float u[kVec], v[kVec];
+          block(k, u);
+          gate(k, v);
 #pragma unroll
-          for (int i = 0; i < E; ++i) sum[kSumGate][i] += u[i];
+          for (int q = 0; q < kVec; ++q) {
+            const int i = k * kVec + q;
+            if constexpr (kToken)
+              x[i] = u[q] * dr[i];
+            else
+              sum[kSumGate][i] = fmaf(u[q], dr[i], sum[kSumGate][i]);
+            dr[i] *= v[q];
+          }
         }
+        if constexpr (kToken) c.store(dg, x);
       }
       if (a.post) {
 #pragma unroll
@@ -516,20 +551,18 @@ __global__ __launch_bounds__(kThreads<kTpr>) __attribute__((amdgpu_waves_per_eu(
       c.store(dt, dr);
       cur = next;
     }
-    if (seq) {
-      block_sum<C, kRows>(sum[kSumGate], gpart + (long long)it * a.D, lw, c);
-      staged = false;  // the weights are gone
-      __syncthreads();
+    if (seq && a.dgate) {
+      block_sum<C, kRows>(sum[kSumGate], gpart + (long long)it * a.D, buf, c);
 #pragma unroll
       for (int i = 0; i < E; ++i) sum[kSumGate][i] = 0.f;
     }
   }
   float* part = a.ws + (long long)blockIdx.x * kSums * a.D;
-  if (a.dpre_w) block_sum<C, kRows>(sum[kSumPreW], part + kSumPreW * a.D, lw, c);
-  if (a.dpre_b) block_sum<C, kRows>(sum[kSumPreB], part + kSumPreB * a.D, lw, c);
-  if (a.dpost_w) block_sum<C, kRows>(sum[kSumPostW], part + kSumPostW * a.D, lw, c);
-  if (a.dpost_b) block_sum<C, kRows>(sum[kSumPostB], part + kSumPostB * a.D, lw, c);
-  if (a.dgate && a.gate_mode == kGateChannel) block_sum<C, kRows>(sum[kSumGate], part + kSumGate * a.D, lw, c);
+  if (a.dpre_w) block_sum<C, kRows>(sum[kSumPreW], part + kSumPreW * a.D, buf, c);
+  if (a.dpre_b) block_sum<C, kRows>(sum[kSumPreB], part + kSumPreB * a.D, buf, c);
+  if (a.dpost_w) block_sum<C, kRows>(sum[kSumPostW], part + kSumPostW * a.D, buf, c);
+  if (a.dpost_b) block_sum<C, kRows>(sum[kSumPostB], part + kSumPostB * a.D, buf, c);
+  if (a.dgate && a.gate_mode == kGateChannel) block_sum<C, kRows>(sum[kSumGate], part + kSumGate * a.D, buf, c);
 }
 
 // 64 channels of one output a workgroup: 16 waves add every 16th record in
@@ -539,7 +572,7 @@ template <typename T>
 __global__ __launch_bounds__(1024) void k_norm_sums(Norm a, NormPlan pl) {
   __shared__ float buf[16][64];
   const int lane = threadIdx.x & 63, k = blockIdx.x * 64 + lane, w = threadIdx.x >> 6;
-  const int count = kSums + (norm_seq(a) ? a.B : 0);
+  const int count = kSums + (a.gate_mode == kGateSequence && a.dgate ? a.B : 0);
   for (int o = blockIdx.y; o < count; o += gridDim.y) {
     float* out = o == kSumPreW    ? a.dpre_w
                  : o == kSumPreB  ? a.dpre_b
@@ -623,10 +656,12 @@ hipError_t run_norm_backward(const Norm& a, hipStream_t s) {
   return norm_shape(a.D, norm_vec(a), [&](auto shape) {
     using S = decltype(shape);
     constexpr int kT = kThreads<S::kTpr>, kRows = kT / S::kTpr;
-    const bool seq = norm_seq(a);
-    const NormPlan pl = norm_plan(a, kRows, seq);
-    hipLaunchKernelGGL((k_norm_bwd<T, S::kVec, S::kPer, S::kTpr>), dim3(pl.blocks), dim3(kT),
-                       kRows > 1 ? kRows * a.D * sizeof(float) : 0, s, a, pl);
+    const bool seq = a.gate_mode == kGateSequence && a.dgate;
+    const NormPlan pl = norm_plan(a, kRows);
+    if (a.gate_mode == kGateToken)
+      hipLaunchKernelGGL((k_norm_bwd<T, S::kVec, S::kPer, S::kTpr, true>), dim3(pl.blocks), dim3(kT), 0, s, a, pl);
+    else
+      hipLaunchKernelGGL((k_norm_bwd<T, S::kVec, S::kPer, S::kTpr, false>), dim3(pl.blocks), dim3(kT), 0, s, a, pl);
     if (a.dpre_w || a.dpre_b || a.dpost_w || a.dpost_b || (a.gate_mode == kGateChannel && a.dgate) || seq)
       hipLaunchKernelGGL(k_norm_sums<T>, dim3((a.D + 63) / 64, std::min(kSums + (seq ? a.B : 0), 32768)), dim3(1024), 0,
                          s, a, pl);
@@ -641,14 +676,14 @@ hipError_t launch_block_norm(const Norm& a, hipStream_t s) {
 }
 
 // The records of every block and, for a gate by sequence, of every item: the
-// most over what the tensors' alignment and a missing dgate may choose.
+// most over the rows per block that the tensors' alignment may choose.
 size_t block_norm_backward_floats(const Norm& a) {
   size_t most = 0;
-  for (int rows : {1, 4})
-    for (int seq = 0; seq <= (a.gate_mode == kGateSequence ? 1 : 0); ++seq) {
-      const NormPlan pl = norm_plan(a, rows, seq);
-      most = std::max(most, ((size_t)pl.blocks * kSums + (seq ? (size_t)pl.Bs * pl.nch : 0)) * a.D);
-    }
+  for (int rows : {1, 4}) {
+    const NormPlan pl = norm_plan(a, rows);
+    most = std::max(most,
+                    ((size_t)pl.blocks * kSums + (a.gate_mode == kGateSequence ? (size_t)pl.Bs * pl.nch : 0)) * a.D);
+  }
   return most;
 }
 
