@@ -4,22 +4,56 @@ from __future__ import annotations
 import ctypes
 
 from ._binding import (SC_ACT_NONE, SC_BF16, SC_F32, SC_GATE_CHANNEL, SC_GATE_NONE, SC_GATE_SEQUENCE, SC_I8,
-                       SC_NORM_LAYER, _check, _I8Weight, _LayerI8,
-                       _LinearDesc, _NormDesc, _min_bytes, _on_stream, _opt, _ptr, _stream, _tensor, _ws,
-                       load)
+                       SC_NORM_LAYER, _check, _I8Weight, _LayerI8, _LinearDesc, _min_bytes, _NormDesc, _on_stream,
+                       _opt, _ptr, _stream, _tensor, _ws, load)
 
 
-def _one_device(tensors, stream):
-    """The device of the tensors (None: absent), which is the stream's (default: the current one)."""
-    import torch
-    dev = tensors[0].device
-    for t in tensors:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors on {dev} and {t.device}")
-    at = torch.cuda.current_device() if stream is None else stream.device_index
-    if dev.index != at:
-        raise ValueError(f"tensors on {dev}, stream on device {at}")
-    return dev
+class _Call:
+    """Checks the tensors of one call and gives their addresses.  The checks are _tensor's, and that every tensor lies
+    on the device of the call's stream; the common case is settled by comparisons alone, since the smallest calls cost
+    less on the GPU than their marshalling does on the host (a norm of one row: 18 us a call with _tensor for each, 12
+    so, 4 of it the launch)."""
+
+    def __init__(self, stream, x):
+        import torch
+        if not (isinstance(x, torch.Tensor) and x.is_cuda):
+            _tensor(x, "x")  # raises
+        self.device = torch.cuda.current_device() if stream is None else stream.device_index
+        self.stream = torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream
+
+    def ptr(self, t, name, dtype, shape):
+        """Address of a required tensor."""
+        try:
+            if t.dtype is dtype and t.shape == shape and t.get_device() == self.device and t.is_contiguous():
+                return t.data_ptr()
+        except AttributeError:
+            pass
+        _tensor(t, name, dtype, shape)
+        raise ValueError(f"{name}: on {t.device}, the call's stream on device {self.device}")
+
+    def opt(self, t, name, dtype, shape):
+        """Address of an optional tensor."""
+        return None if t is None else self.ptr(t, name, dtype, shape)
+
+    def lengths(self, valid_len, B):
+        import torch
+        return None if valid_len is None else self.ptr(valid_len, "valid_len", torch.int32, (B,))
+
+    def workspace(self, t, nbytes):
+        """(address, bytes, tensor) of the given workspace or of a new one; the tensor is kept by the caller until the
+        call is enqueued."""
+        import torch
+        if t is None:
+            if nbytes == 0:
+                return None, 0, None
+            t = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            return t.data_ptr(), nbytes, t
+        _tensor(t, "workspace")
+        return self.ptr(t, "workspace", t.dtype, t.shape), t.numel() * t.element_size(), t
+
+    def new(self, dtype, shape):
+        import torch
+        return torch.empty(shape, dtype=dtype, device=self.device)
 
 
 def _float_type(code, what):
@@ -38,11 +72,6 @@ def _code(t, name):
     raise TypeError(f"{name}: expected torch.float32 or torch.bfloat16, got {t.dtype}")
 
 
-def _lengths(valid_len, B):
-    import torch
-    return None if valid_len is None else _tensor(valid_len, "valid_len", torch.int32, (B,))
-
-
 def sc_i8_pitch(K: int) -> int:
     """Bytes of a row of K 8-bit values."""
     return load().sc_i8_pitch(int(K))
@@ -53,16 +82,15 @@ def sc_quantize_rows_i8(x, valid_len=None, xq=None, scale=None, stream=None):
     """8-bit rows of x [B, n, K] (float32 or bf16).  Returns (xq int8 [B, n, pitch], scale float32 [B, n])."""
     import torch
     L = load()
-    code = _code(_tensor(x, "x"), "x")
+    call = _Call(stream, x)
+    code = _code(x, "x")
     B, n, K = x.shape
-    _lengths(valid_len, B)
     shape = (B, n, L.sc_i8_pitch(K))
-    dev = _one_device((x, valid_len, xq, scale), stream)
-    xq = torch.empty(shape, dtype=torch.int8, device=dev) if xq is None else _tensor(xq, "xq", torch.int8, shape)
-    scale = torch.empty((B, n), dtype=torch.float32, device=dev) if scale is None else \
-        _tensor(scale, "scale", torch.float32, (B, n))
-    _check(L.sc_quantize_rows_i8(B, n, K, _ptr(valid_len), code, _ptr(x), _ptr(xq), _ptr(scale), _stream(stream)),
-           "sc_quantize_rows_i8")
+    xq = call.new(torch.int8, shape) if xq is None else xq
+    scale = call.new(torch.float32, (B, n)) if scale is None else scale
+    _check(L.sc_quantize_rows_i8(B, n, K, call.lengths(valid_len, B), code, call.ptr(x, "x", x.dtype, x.shape),
+                                 call.ptr(xq, "xq", torch.int8, shape),
+                                 call.ptr(scale, "scale", torch.float32, (B, n)), call.stream), "sc_quantize_rows_i8")
     return xq, scale
 
 
@@ -71,14 +99,15 @@ def sc_quantize_weight_i8(w, wq=None, scale=None, stream=None):
     """8-bit weights of w [K, N] (float32 or bf16).  Returns (wq int8 [N, pitch(K)], scale float32 [N])."""
     import torch
     L = load()
-    code = _code(_tensor(w, "w"), "w")
+    call = _Call(stream, w)
+    code = _code(w, "w")
     K, N = w.shape
     shape = (N, L.sc_i8_pitch(K))
-    dev = _one_device((w, wq, scale), stream)
-    wq = torch.empty(shape, dtype=torch.int8, device=dev) if wq is None else _tensor(wq, "wq", torch.int8, shape)
-    scale = torch.empty((N,), dtype=torch.float32, device=dev) if scale is None else \
-        _tensor(scale, "scale", torch.float32, (N,))
-    _check(L.sc_quantize_weight_i8(K, N, code, _ptr(w), _ptr(wq), _ptr(scale), _stream(stream)),
+    wq = call.new(torch.int8, shape) if wq is None else wq
+    scale = call.new(torch.float32, (N,)) if scale is None else scale
+    _check(L.sc_quantize_weight_i8(K, N, code, call.ptr(w, "w", w.dtype, w.shape),
+                                   call.ptr(wq, "wq", torch.int8, shape),
+                                   call.ptr(scale, "scale", torch.float32, (N,)), call.stream),
            "sc_quantize_weight_i8")
     return wq, scale
 
@@ -108,31 +137,26 @@ def sc_linear_i8(desc: LinearDesc, x, wq, w_scale, bias=None, x_scale=None, out=
     wq, w_scale: as sc_quantize_weight_i8 returns them."""
     import torch
     L = load()
+    call = _Call(stream, x)
     B, n, K, N = desc.B, desc.n, desc.K, desc.N
-    _lengths(desc.valid_len, B)
     pitch = L.sc_i8_pitch(K)
     if desc.x_dtype == SC_I8:
-        _tensor(x, "x", torch.int8, (B, n, pitch))
-        _tensor(x_scale, "x_scale", torch.float32, (B, n))
+        px = call.ptr(x, "x", torch.int8, (B, n, pitch))
+        ps = call.ptr(x_scale, "x_scale", torch.float32, (B, n))
     else:
-        _tensor(x, "x", _float_type(desc.x_dtype, "x_dtype"), (B, n, K))
+        px, ps = call.ptr(x, "x", _float_type(desc.x_dtype, "x_dtype"), (B, n, K)), None
         if x_scale is not None:
             raise ValueError("x_scale: only with 8-bit rows")
-    _tensor(wq, "wq", torch.int8, (N, pitch))
-    _tensor(w_scale, "w_scale", torch.float32, (N,))
-    if bias is not None:
-        _tensor(bias, "bias", torch.float32, (N,))
-    dev = _one_device((x, x_scale, wq, w_scale, bias, out, workspace, desc.valid_len), stream)
+    pw = call.ptr(wq, "wq", torch.int8, (N, pitch))
+    pws = call.ptr(w_scale, "w_scale", torch.float32, (N,))
+    pb = call.opt(bias, "bias", torch.float32, (N,))
+    call.lengths(desc.valid_len, B)
     dt = _float_type(desc.out_dtype, "out_dtype")
-    out = torch.empty((B, n, N), dtype=dt, device=dev) if out is None else _tensor(out, "out", dt, (B, n, N))
-    cd = desc.c()
-    wsb = L.sc_linear_i8_workspace_size(ctypes.byref(cd))
-    if workspace is None:
-        workspace = _ws(wsb, dev) if wsb > 0 else None
-    else:
-        wsb = _tensor(workspace, "workspace").numel() * workspace.element_size()
-    _check(L.sc_linear_i8(ctypes.byref(cd), _ptr(x), _ptr(x_scale), _ptr(wq), _ptr(w_scale), _ptr(bias), _ptr(out),
-                          _ptr(workspace), wsb, _stream(stream)), "sc_linear_i8")
+    out = call.new(dt, (B, n, N)) if out is None else out
+    po = call.ptr(out, "out", dt, (B, n, N))
+    cd = ctypes.byref(desc.c())
+    work, wsb, keep = call.workspace(workspace, L.sc_linear_i8_workspace_size(cd))
+    _check(L.sc_linear_i8(cd, px, ps, pw, pws, pb, po, work, wsb, call.stream), "sc_linear_i8")
     return out
 
 
@@ -160,20 +184,17 @@ class NormDesc:
             _float_type(self.dtype, "dtype")
 
 
-def _norm_inputs(desc, x, t, gate, post_w, post_b, pre_w, pre_b):
+def _norm_inputs(stream, desc, x, t, gate, post_w, post_b, pre_w, pre_b):
+    """(call, shape, dtype, addresses) of what both directions read."""
     import torch
     shape, dt = (desc.B, desc.n, desc.D), _float_type(desc.dtype, "dtype")
-    _lengths(desc.valid_len, desc.B)
-    _tensor(x, "x", dt, shape)
-    if t is not None:
-        _tensor(t, "t", dt, shape)
-    if gate is not None:
-        gs, gt = desc.gate_form()
-        _tensor(gate, "gate", gt, gs)
-    for w, nm in ((post_w, "post_w"), (post_b, "post_b"), (pre_w, "pre_w"), (pre_b, "pre_b")):
-        if w is not None:
-            _tensor(w, nm, torch.float32, (desc.D,))
-    return shape, dt
+    call = _Call(stream, x)
+    call.lengths(desc.valid_len, desc.B)
+    gs, gt = desc.gate_form() if gate is not None else (None, None)
+    vec, f32 = (desc.D,), torch.float32
+    return call, shape, dt, (call.ptr(x, "x", dt, shape), call.opt(t, "t", dt, shape), call.opt(gate, "gate", gt, gs),
+                       call.opt(post_w, "post_w", f32, vec), call.opt(post_b, "post_b", f32, vec),
+                       call.opt(pre_w, "pre_w", f32, vec), call.opt(pre_b, "pre_b", f32, vec))
 
 
 @_on_stream
@@ -185,26 +206,17 @@ def sc_block_norm(desc: NormDesc, x, t=None, gate=None, post_w=None, post_b=None
     yscale).  Without desc.pre, y is skipped."""
     import torch
     L = load()
-    shape, dt = _norm_inputs(desc, x, t, gate, post_w, post_b, pre_w, pre_b)
-    for o, nm in ((r, "r"), (y, "y")):
-        if isinstance(o, torch.Tensor):
-            _tensor(o, nm, dt, shape)
-    rt = _opt(r, lambda: torch.empty(shape, dtype=dt, device=x.device))
-    yt = _opt(y, lambda: torch.empty(shape, dtype=dt, device=x.device)) if desc.pre or y is not True else None
-    yq = ys = None
+    call, shape, dt, ins = _norm_inputs(stream, desc, x, t, gate, post_w, post_b, pre_w, pre_b)
+    r = _opt(r, lambda: torch.empty_like(x))
+    y = _opt(y, lambda: torch.empty_like(x)) if desc.pre or y is not True else None
+    yq = ys = pq = ps = None
     if quantized:
         qshape = (desc.B, desc.n, L.sc_i8_pitch(desc.D))
-        if quantized is True:
-            yq = torch.empty(qshape, dtype=torch.int8, device=x.device)
-            ys = torch.empty(shape[:2], dtype=torch.float32, device=x.device)
-        else:
-            yq = _tensor(quantized[0], "yq", torch.int8, qshape)
-            ys = _tensor(quantized[1], "yscale", torch.float32, shape[:2])
-    _one_device((x, t, gate, post_w, post_b, pre_w, pre_b, rt, yt, yq, ys, desc.valid_len), stream)
-    _check(L.sc_block_norm(ctypes.byref(desc.c()), _ptr(x), _ptr(t), _ptr(gate), _ptr(post_w), _ptr(post_b),
-                           _ptr(pre_w), _ptr(pre_b), _ptr(rt), _ptr(yt), _ptr(yq), _ptr(ys), _stream(stream)),
-           "sc_block_norm")
-    return rt, yt, yq, ys
+        yq, ys = (call.new(torch.int8, qshape), call.new(torch.float32, shape[:2])) if quantized is True else quantized
+        pq, ps = call.ptr(yq, "yq", torch.int8, qshape), call.ptr(ys, "yscale", torch.float32, shape[:2])
+    _check(L.sc_block_norm(ctypes.byref(desc.c()), *ins, call.opt(r, "r", dt, shape), call.opt(y, "y", dt, shape), pq,
+                           ps, call.stream), "sc_block_norm")
+    return r, y, yq, ys
 
 
 def sc_block_norm_backward_workspace_size(desc: NormDesc) -> int:
@@ -220,41 +232,33 @@ def sc_block_norm_backward(desc: NormDesc, x, t=None, gate=None, post_w=None, po
     grads: optional dict of preallocated outputs; only those it names are computed."""
     import torch
     L = load()
-    shape, dt = _norm_inputs(desc, x, t, gate, post_w, post_b, pre_w, pre_b)
-    for g, nm in ((dr, "dr"), (dy, "dy")):
-        if g is not None:
-            _tensor(g, nm, dt, shape)
-    forms = {"dx": (x, shape, dt), "dt": (t, shape, dt), "dgate": (gate, None, None)}
-    if gate is not None:
-        forms["dgate"] = (gate, *desc.gate_form())
-    for nm, w in (("dpost_w", post_w), ("dpost_b", post_b), ("dpre_w", pre_w), ("dpre_b", pre_b)):
-        forms[nm] = (w, (desc.D,), torch.float32)
-    out = dict.fromkeys(forms)
-    if grads is None:
-        for nm, (src, s, ty) in forms.items():
-            if src is not None:
-                out[nm] = torch.empty(s, dtype=ty, device=x.device)
-    else:
-        for nm, g in grads.items():
-            if nm not in forms:
-                raise ValueError(f"grads: unknown output {nm}")
-            if g is not None:
-                if nm == "dgate" and gate is None:
-                    raise ValueError("dgate: there is no gate")
-                out[nm] = _tensor(g, nm, forms[nm][2], forms[nm][1])
-    dev = _one_device((x, t, gate, post_w, post_b, pre_w, pre_b, dr, dy, workspace, desc.valid_len, *out.values()),
-                      stream)
-    cd = desc.c()
-    wsb = L.sc_block_norm_backward_workspace_size(ctypes.byref(cd))
-    if workspace is None:
-        workspace = _ws(wsb, dev)
-    else:
-        wsb = _tensor(workspace, "workspace").numel() * workspace.element_size()
-    _check(L.sc_block_norm_backward(ctypes.byref(cd), _ptr(x), _ptr(t), _ptr(gate), _ptr(post_w), _ptr(post_b),
-                                    _ptr(pre_w), _ptr(pre_b), _ptr(dr), _ptr(dy), _ptr(out["dx"]), _ptr(out["dt"]),
-                                    _ptr(out["dgate"]), _ptr(out["dpost_w"]), _ptr(out["dpost_b"]),
-                                    _ptr(out["dpre_w"]), _ptr(out["dpre_b"]), _ptr(workspace), wsb,
-                                    _stream(stream)), "sc_block_norm_backward")
+    call, shape, dt, ins = _norm_inputs(stream, desc, x, t, gate, post_w, post_b, pre_w, pre_b)
+    pr, py = call.opt(dr, "dr", dt, shape), call.opt(dy, "dy", dt, shape)
+    gs, gt = desc.gate_form() if gate is not None else (None, None)
+    vec, f32 = (desc.D,), torch.float32
+    forms = (("dx", x, dt, shape), ("dt", t, dt, shape), ("dgate", gate, gt, gs), ("dpost_w", post_w, f32, vec),
+             ("dpost_b", post_b, f32, vec), ("dpre_w", pre_w, f32, vec), ("dpre_b", pre_b, f32, vec))
+    out, outs = {}, []
+    if grads is not None:
+        unknown = set(grads) - {f[0] for f in forms}
+        if unknown:
+            raise ValueError(f"grads: unknown outputs {sorted(unknown)}")
+        if gate is None and grads.get("dgate") is not None:
+            raise ValueError("dgate: there is no gate")
+    for nm, src, ty, s in forms:
+        if grads is not None:
+            g = grads.get(nm)
+            outs.append(call.opt(g, nm, ty, s))
+        elif src is None:
+            g = None
+            outs.append(None)
+        else:
+            g = call.new(ty, s)
+            outs.append(g.data_ptr())
+        out[nm] = g
+    cd = ctypes.byref(desc.c())
+    work, wsb, keep = call.workspace(workspace, L.sc_block_norm_backward_workspace_size(cd))
+    _check(L.sc_block_norm_backward(cd, *ins, pr, py, *outs, work, wsb, call.stream), "sc_block_norm_backward")
     return out
 
 
@@ -308,8 +312,10 @@ def sc_encoder_stack_i8(desc, x_in, layers, ffn_dim, thresholds, windows=None, k
         raise ValueError("thresholds and windows: one per layer")
     for i, y in enumerate(layers):
         y.check(f"layers[{i}]", D, F)
-    dev = _one_device((x_in, x_out, workspace, desc.valid_len, desc.global_pos,
-                       *(t for y in layers for t in y.tensors())), stream)
+    call = _Call(stream, x_in)
+    for t in (x_in, x_out, workspace, desc.valid_len, desc.global_pos, *(t for y in layers for t in y.tensors())):
+        call.opt(t, "argument", t if t is None else t.dtype, t if t is None else t.shape)
+    dev = x_in.device
     x_out = torch.empty_like(x_in) if x_out is None else x_out
     i32 = dict(dtype=torch.int32, device=dev)
     final_len, orig, kpl = torch.empty((B,), **i32), torch.empty((B, n), **i32), torch.empty((nl, B), **i32)

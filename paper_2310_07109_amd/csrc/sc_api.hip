@@ -757,7 +757,6 @@ sc_status check_stack_i8(const sc_attn_desc* d, int32_t n_layers, int32_t F) {
   if (D > 2048 || F > sc::kI8MaxK || d->B > sc::kPackMaxB || d->n * 3 * D * 2 >= (1LL << 32)) return SC_EUNSUPPORTED;
   const long long pf = sc::i8_pitch(F);
   if (bn * std::max(pd, pf) >= (1LL << 32) || F * pd >= (1LL << 32) || D * pf >= (1LL << 32)) return SC_EUNSUPPORTED;
-  if (sc::linear_tiles(bn, (int)std::max(3 * D, (long long)F)) >= (1LL << 24) - 8) return SC_EUNSUPPORTED;
   return SC_OK;
 }
 

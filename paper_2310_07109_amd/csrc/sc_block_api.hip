@@ -29,11 +29,9 @@ sc_status check_linear(const sc_linear_desc* d) {
   if (st != SC_OK) return st;
   if (d->K > sc::kI8MaxK) return SC_EUNSUPPORTED;
   if (d->valid_len && d->B > sc::kPackMaxB) return SC_EUNSUPPORTED;  // the packed rows' prefix table
-  // tile loads address the rows and the weights with 32-bit byte offsets; a
-  // launch has fewer than 2^32 threads
+  // tile loads address the rows and the weights with 32-bit byte offsets
   const long long rows = (long long)d->B * d->n, pitch = sc::i8_pitch(d->K);
   if (rows * pitch >= (1LL << 32) || d->N * pitch >= (1LL << 32)) return SC_EUNSUPPORTED;
-  if (sc::linear_tiles(rows, d->N) >= (1LL << 24) - 8) return SC_EUNSUPPORTED;
   return SC_OK;
 }
 
@@ -42,7 +40,8 @@ struct LinearWs {
   float* xs;
 };
 size_t carve_linear(const sc_linear_desc* d, void* base, LinearWs* w) {
-  if (d->x_dtype == SC_I8) return 0;
+  // no rows of its own: they come quantised, or stay in the launch
+  if (d->x_dtype == SC_I8 || sc::linear_few_ok((long long)d->B * d->n, d->K, d->N)) return 0;
   const size_t rows = (size_t)d->B * d->n;
   Carver c(base);
   LinearWs x;
@@ -157,19 +156,8 @@ sc_status linear_impl(const sc_linear_desc* d, const void* x, const float* x_sca
   hipStream_t s = static_cast<hipStream_t>(stream);
   sc::Linear l;
   std::memset(&l, 0, sizeof(l));
-  if (d->x_dtype == SC_I8) {
-    l.xq = static_cast<const int8_t*>(x);
-    l.xs = x_scale;
-  } else {
-    LinearWs w;
-    carve_linear(d, workspace, &w);
-    if (sc::launch_quant_rows(x, d->x_dtype == SC_F32, w.xq, w.xs, d->B, d->n, d->K, d->valid_len, nullptr, 1, s) !=
-        hipSuccess)
-      return SC_EHIP;
-    l.xq = w.xq;
-    l.xs = w.xs;
-    l.packed = 1;
-  }
+  l.xq = static_cast<const int8_t*>(x);
+  l.xs = x_scale;
   l.wq = wq;
   l.w_scale = w_scale;
   l.bias = bias;
@@ -181,6 +169,18 @@ sc_status linear_impl(const sc_linear_desc* d, const void* x, const float* x_sca
   l.len = d->valid_len;
   l.gelu = d->act == SC_ACT_GELU;
   l.out_f32 = d->out_dtype == SC_F32;
+  if (sc::linear_few_ok((long long)rows, d->K, d->N))
+    return sc::launch_linear_few(l, x, d->x_dtype, s) == hipSuccess ? SC_OK : SC_EHIP;
+  if (d->x_dtype != SC_I8) {
+    LinearWs w;
+    carve_linear(d, workspace, &w);
+    if (sc::launch_quant_rows(x, d->x_dtype == SC_F32, w.xq, w.xs, d->B, d->n, d->K, d->valid_len, nullptr, 1, s) !=
+        hipSuccess)
+      return SC_EHIP;
+    l.xq = w.xq;
+    l.xs = w.xs;
+    l.packed = 1;
+  }
   return sc::launch_linear_i8(l, s) == hipSuccess ? SC_OK : SC_EHIP;
 }
 

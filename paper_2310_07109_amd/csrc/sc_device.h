@@ -281,6 +281,12 @@ SC_DEV unsigned long long uniform64(unsigned long long v) {
          ((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(v >> 32)) << 32);
 }
 
+// A word of an array that the launch does not write, at a wave-uniform index: by a
+// scalar load, which does not wait for the rows in flight.
+SC_DEV int scalar_load(const int* p, long long i) {
+  return ((const __attribute__((address_space(4))) int*)p)[i];
+}
+
 SC_DEV int clampi(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
 
 }  // namespace sc

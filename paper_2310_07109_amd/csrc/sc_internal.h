@@ -193,7 +193,10 @@ struct Linear {
   int packed, skip_pad, gelu, out_f32;
 };
 hipError_t launch_linear_i8(const Linear& l, hipStream_t s);
-long long linear_tiles(long long rows, int N);  // workgroups of the product's grid
+// The product of few rows from x itself, quantised in the same launch (x_type as
+// SC_F32, SC_BF16, SC_I8; xq, and xs but for 8-bit rows, are not used).
+bool linear_few_ok(long long rows, int K, int N);
+hipError_t launch_linear_few(const Linear& l, const void* x, int x_type, hipStream_t s);
 
 // Block norms (sc_norm.hip).
 constexpr int kNormMaxD = 4096;

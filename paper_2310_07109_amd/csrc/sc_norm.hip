@@ -233,12 +233,6 @@ SC_DEV void times(float (&v)[E], const float* lds, int w, const C& c) {
   for (int i = 0; i < E; ++i) v[i] *= p[i];
 }
 
-// A word of an array that the launch does not write, at a wave-uniform index: by a
-// scalar load, which does not wait for the rows in flight.
-SC_DEV int scalar_load(const int* p, long long i) {
-  return ((const __attribute__((address_space(4))) int*)p)[i];
-}
-
 // A row's sequence and whether it is padding; all of it wave-uniform.
 struct RowAt {
   unsigned row;

@@ -678,7 +678,8 @@ def test_binding_refusals():
     with pytest.raises(TypeError, match="valid_len"):
         sc.sc_linear_i8(sc.LinearDesc(2, 8, 64, 32, valid_len=torch.ones(2, dtype=torch.int64, device=DEV)), x, w, s)
     with pytest.raises(sc.ScError, match="workspace"):
-        sc.sc_linear_i8(d, x, w, s, workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
+        sc.sc_linear_i8(sc.LinearDesc(2, 800, 64, 32), torch.zeros((2, 800, 64), dtype=torch.bfloat16, device=DEV), w, s,
+                        workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
     n = sc.NormDesc(2, 8, 64, gate=sc.SC_GATE_CHANNEL)
     with pytest.raises(TypeError, match="gate: expected torch.float32"):
         sc.sc_block_norm(n, x, x, gate=x[0, 0].contiguous())
