@@ -4,7 +4,7 @@
 //
 // k_quant_rows    the tokens' 8-bit rows (sc_quant.h), one wavefront a row.
 // k_quant_weight  the weights', once per model.
-// k_linear        the product on v_mfma_i32_32x32x32_i8: sums of up to 131072
+// k_linear        the product on v_mfma_i32_16x16x64_i8: sums of up to 131072
 //                 products of 127 x 127 fit an int32, so they are exact in any
 //                 order, and a row's result does not depend on the tile that
 //                 computed it.
@@ -20,7 +20,6 @@ namespace sc {
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) int i32x4;
-typedef __attribute__((ext_vector_type(16))) int i32x16;
 
 // -------------------------------------------------------- activations ----
 // gelu(v) = max(v, 0) - |v| Phi(-|v|), with Phi(-a) = exp2(P(a)): log2 Phi(-a)
@@ -272,8 +271,8 @@ struct LinearArgs {
 
 constexpr int kBK = 128;        // bytes of a row per K stage: whole lines (64-byte pieces halve the loads' rate)
 constexpr int kLinWgs = 256;    // one workgroup per CU, each taking tiles in turn
-constexpr int kLinLds = 147456; // stage buffers: 2 x 64, 3 x 48, 4 x 32 or 9 x 16 KB
-constexpr int kLinModes = 4;
+constexpr int kLinLds = 147456; // stage buffers: 3 x 48, 4 x 32 or 8 x 16 KB
+constexpr int kLinModes = 3;
 constexpr int kGroupM = 8;
 // k_linear_few: at most kFewRows rows of kFewK bytes, kFewWgs workgroups and
 // kFewWork bytes of rows over all of them.  us in a graph, bf16 rows, this kernel and
@@ -283,21 +282,20 @@ constexpr int kGroupM = 8;
 // and 17.1, 128 rows 13.8 and 18.8, 256 rows 23.8 and 19.3.  8-bit rows alike.
 constexpr int kFewRows = 512, kFewK = 4096, kFewWgs = 1024, kFewWork = 5 << 19;
 
-// Tile shapes: kKS waves share a part of the tile, each with its part of every stage.
+// Tile shapes: BM x BN, waves along M and N, stage buffers.
 template <int kM>
 struct LinTile;
 template <>
-struct LinTile<0> { static constexpr int kBM = 256, kBN = 256, kWgM = 2, kWgN = 4, kKS = 1; };
+struct LinTile<0> { static constexpr int kBM = 256, kBN = 128, kWgM = 4, kWgN = 2, kNBuf = 3; };
 template <>
-struct LinTile<1> { static constexpr int kBM = 256, kBN = 128, kWgM = 4, kWgN = 2, kKS = 1; };
+struct LinTile<1> { static constexpr int kBM = 128, kBN = 128, kWgM = 4, kWgN = 2, kNBuf = 4; };
 template <>
-struct LinTile<2> { static constexpr int kBM = 128, kBN = 128, kWgM = 4, kWgN = 2, kKS = 1; };
-template <>
-struct LinTile<3> { static constexpr int kBM = 64, kBN = 64, kWgM = 2, kWgN = 2, kKS = 2; };
+struct LinTile<2> { static constexpr int kBM = 64, kBN = 64, kWgM = 2, kWgN = 4, kNBuf = 8; };
 
 struct LinPlan {
   int mode, T, Nt;
 };
+constexpr int kStreamMin = 5;  // stages that linear_stream needs: its buffers and two
 // The mode with the least rounds of workgroups times the cost of a tile: of a stage
 // and of what stands beside the stages, in cycles.
 SC_DEV LinPlan lin_plan(int R, int N, int ns) {
@@ -305,13 +303,12 @@ SC_DEV LinPlan lin_plan(int R, int N, int ns) {
   long long best = 1LL << 62;
 #pragma unroll
   for (int m = 0; m < kLinModes; ++m) {
-    const int bm = m <= 1 ? 256 : m == 2 ? 128 : 64, bn = m == 0 ? 256 : m == 3 ? 64 : 128;
-    const int stage = m == 0 ? 2400 : m == 1 ? 1400 : m == 2 ? 800 : 450;
-    const int fixed = m == 0 ? 12000 : m == 1 ? 7000 : m == 2 ? 4500 : 3000;
+    const int bm = m == 0 ? 256 : m == 1 ? 128 : 64, bn = m == 2 ? 64 : 128;
+    const int stage = m == 0 ? 1300 : m == 1 ? 800 : 450, fixed = m == 0 ? 1500 : m == 1 ? 4500 : 3000;
     const int T = (R + bm - 1) / bm, Nt = (N + bn - 1) / bn;
     const long long rounds = ((long long)T * Nt + kLinWgs - 1) / kLinWgs;
-    const long long t = rounds * (ns * stage + fixed);
-    if (t < best) {
+    const long long t = rounds * (ns * stage + fixed) + (m == 0 ? 6000 : 0);
+    if (t < best && (m > 0 || ns >= kStreamMin)) {
       best = t;
       p.mode = m;
       p.T = T;
@@ -322,24 +319,17 @@ SC_DEV LinPlan lin_plan(int R, int N, int ns) {
 }
 
 // 128-byte rows in LDS, 16-byte units swizzled by bits 1-3 of the row: the fragment
-// reads of 32x32x32 products (lane l: row l % 32, unit l / 32 of a chunk's two) run at
-// 225 bytes per clock and CU (swizzled by bits 0-2: 126).
+// reads (lane l: row l % 16, unit l / 16 of a chunk's four) run at 226 bytes per clock
+// and CU, 64-byte rows swizzled by bits 2-3 at 121.
 SC_DEV int q_off(int row, int unit) { return row * kBK + 16 * (unit ^ ((row >> 1) & 7)); }
 
 SC_DEV i32x4 lds_read_q(unsigned addr) {
   return *(const __attribute__((address_space(3))) i32x4*)(size_t)addr;
 }
 
-// Orders a wavefront's LDS accesses across its lanes: without it the compiler may take
-// what a lane read before for what it reads after other lanes' writes.
-SC_DEV void wave_exchange() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // The row numbering (sc_pack.h) with a table of fixed size: the prefix sums of every
 // `per`-th sequence, the rest by a scan of at most per - 1 lengths.
-constexpr int kCoarse = 1024;
+constexpr int kCoarse = 512;
 struct Packed {
   const int* pre;  // LDS
   const int* len;
@@ -394,48 +384,65 @@ struct Packed {
   }
 };
 
-// A tile's rows and columns: in LDS, twice, the next tile's beside this one's.
+// A tile's rows and columns, in LDS.
 struct LinTables {
-  int grow[256], xrow[256];  // row of out (-1: none) and of xq
-  float xs[256], sw[256], sb[256];
+  int grow[256], xrow[256];  // row of out and of xq; rows past the last one repeat it
+  float xs[256], sw[128], sb[128];
 };
 
+// A workgroup's share of the tiles.  They go to the XCDs in contiguous ranges
+// (workgroup i runs on XCD i % 8), in groups of kGroupM row tiles by all column
+// tiles: what an XCD runs at a time shares rows and weights in its L2.
+struct LinShare {
+  long long item, last;
+  int T, Nt, step;
+  SC_DEV LinShare(const LinPlan& pl) : T(pl.T), Nt(pl.Nt), step(gridDim.x >> 3) {
+    const long long items = (long long)T * Nt;
+    const int xcd = blockIdx.x & 7;
+    last = items * (xcd + 1) / 8;
+    item = items * xcd / 8 + (blockIdx.x >> 3);
+  }
+  template <int kBM, int kBN>
+  SC_DEV void place(long long it, int& m0, int& n0) const {
+    const int per = kGroupM * Nt, gi = (int)(it / per), rem = (int)(it - (long long)gi * per);
+    const int gs = min(kGroupM, T - gi * kGroupM);
+    m0 = __builtin_amdgcn_readfirstlane((gi * kGroupM + rem % gs) * kBM);
+    n0 = __builtin_amdgcn_readfirstlane(rem / gs * kBN);
+  }
+};
+
+// What the tiles of one mode share: a wave's part of the loads, fragments, products
+// and results.
 template <int kM, typename O, bool kGelu>
-SC_DEV void linear_run(const LinearArgs& a, char* stage, LinTables* tab, const Packed& pk, int R, const LinPlan& pl) {
+struct LinWave {
   using S = LinTile<kM>;
-  constexpr int BM = S::kBM, BN = S::kBN, KS = S::kKS;
-  constexpr int WM = BM / S::kWgM, WN = BN / S::kWgN, FI = WM / 32, FJ = WN / 32;
-  constexpr int XL = BM / 64, WL = BN / 64, kDma = XL + WL;  // loads of a wave and stage, 8 rows each
-  constexpr int kStage = (BM + BN) * kBK, kNBuf = kLinLds / kStage < 8 ? kLinLds / kStage : 8;
-  constexpr int CH = 4 / KS;  // a wave's 32-byte chunks of a stage, one product each (even)
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), hi = lane >> 5,
-            lr = lane & 31;
-  const int wt = w / KS, ks = w % KS;
-  const int wm = (wt / S::kWgN) * WM, wn = (wt % S::kWgN) * WN;
-  const int ns = a.Kp / kBK;
-  const long long items = (long long)pl.T * pl.Nt;
-  // The tiles go to the XCDs in contiguous ranges (workgroup i runs on XCD i % 8), in
-  // groups of kGroupM row tiles by all column tiles: what an XCD runs at a time shares
-  // rows and weights in its L2.
-  const int xcd = blockIdx.x & 7;
-  const long long last = items * (xcd + 1) / 8;
-  long long item = items * xcd / 8 + (blockIdx.x >> 3);
-  if (item >= last) return;
-  auto place = [&](long long it, int& m0, int& n0) {
-    const int per = kGroupM * pl.Nt, gi = (int)(it / per), rem = (int)(it - (long long)gi * per);
-    const int gs = min(kGroupM, pl.T - gi * kGroupM);
-    m0 = __builtin_amdgcn_readfirstlane((gi * kGroupM + rem % gs) * BM);
-    n0 = __builtin_amdgcn_readfirstlane(rem / gs * BN);
-  };
-  // What thread tid brings into a tile's tables: row m0 + tid, column n0 + tid.
-  int b_gr = -1, b_xr = 0;
+  static constexpr int BM = S::kBM, BN = S::kBN, kNBuf = S::kNBuf;
+  static constexpr int WM = BM / S::kWgM, WN = BN / S::kWgN, FI = WM / 16, FJ = WN / 16, FH = FI / 2;
+  static constexpr int XL = BM / 64, WL = BN / 64, kDma = XL + WL;  // loads of a wave and stage, 8 rows each
+  static constexpr int kStage = (BM + BN) * kBK;
+  static_assert(kNBuf * kStage <= kLinLds && FI % 2 == 0, "stage buffers, halves of the rows");
+  const LinearArgs& a;
+  const Packed& pk;
+  const int R, tid, lane, w, g, lr, wm, wn;
+  const unsigned lds0, xa, wa;
+  unsigned xoff[XL], woff[WL];
+  i32x4 acc[FI][FJ];
+  i32x4 xf[2][FH], wf[2][FJ];  // the fragments of half a wave's rows, and of its columns, twice
+  int b_gr = 0, b_xr = 0;      // what this thread brings into a tile's tables
   float b_xs = 0.f, b_sw = 0.f, b_sb = 0.f;
-  auto bring = [&](int m0, int n0) {
+
+  SC_DEV LinWave(const LinearArgs& args, char* stage, const Packed& packed, int rows)
+      : a(args), pk(packed), R(rows), tid(threadIdx.x), lane(threadIdx.x & 63),
+        w(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), g(lane >> 4), lr(lane & 15),
+        wm((w / S::kWgN) * WM), wn((w % S::kWgN) * WN), lds0(lds_addr(stage)), xa(lds0 + q_off(wm + lr, g)),
+        wa(lds0 + BM * kBK + q_off(wn + lr, g)) {}
+
+  // Thread tid's row m0 + tid and column n0 + tid of a tile, and their way into its tables.
+  SC_DEV void bring(int m0, int n0) {
     if (tid < BM) {
-      const int p = min(m0 + tid, R - 1);  // rows past the last one read it again
-      const int gr = a.len ? pk.row(p) : p;
-      b_gr = m0 + tid < R ? gr : -1;
-      b_xr = a.packed ? p : gr;
+      const int p = min(m0 + tid, R - 1);
+      b_gr = a.len ? pk.row(p) : p;
+      b_xr = a.packed ? p : b_gr;
       b_xs = a.xs[b_xr];
     }
     if (tid < BN) {
@@ -443,8 +450,8 @@ SC_DEV void linear_run(const LinearArgs& a, char* stage, LinTables* tab, const P
       b_sw = a.ws[c];
       b_sb = a.bias ? a.bias[c] : 0.f;
     }
-  };
-  auto put = [&](LinTables& d) {
+  }
+  SC_DEV void put(LinTables& d) {
     if (tid < BM) {
       d.grow[tid] = b_gr;
       d.xrow[tid] = b_xr;
@@ -454,9 +461,8 @@ SC_DEV void linear_run(const LinearArgs& a, char* stage, LinTables* tab, const P
       d.sw[tid] = b_sw;
       d.sb[tid] = b_sb;
     }
-  };
-  unsigned xoff[XL], woff[WL];
-  auto offsets = [&](const LinTables& d, int n0) {
+  }
+  SC_DEV void offsets(const LinTables& d, int n0) {
 #pragma unroll
     for (int t = 0; t < XL; ++t) {
       const int R0 = (BM / 8) * w + 8 * t, swz = ((lane >> 4) & 3) | ((R0 >> 1) & 4);
@@ -467,179 +473,282 @@ SC_DEV void linear_run(const LinearArgs& a, char* stage, LinTables* tab, const P
       const int R0 = (BN / 8) * w + 8 * t, swz = ((lane >> 4) & 3) | ((R0 >> 1) & 4);
       woff[t] = (unsigned)min(n0 + R0 + (lane >> 3), a.N - 1) * (unsigned)a.Kp + 16u * ((lane & 7) ^ swz);
     }
-  };
-  const unsigned lds0 = lds_addr(stage);
-  auto issue = [&](int s, int bf) {
+  }
+  SC_DEV void issue(int s, int bf) const {  // stage s into buffer bf
     const int8_t *xb = a.xq + (size_t)s * kBK, *wb = a.wq + (size_t)s * kBK;
     const unsigned lx = lds0 + (unsigned)bf * kStage, lw = lx + BM * kBK;
 #pragma unroll
     for (int t = 0; t < XL; ++t) lds_dma16(xb, xoff[t], lx + ((BM / 8) * w + 8 * t) * kBK);
 #pragma unroll
     for (int t = 0; t < WL; ++t) lds_dma16(wb, woff[t], lw + ((BN / 8) * w + 8 * t) * kBK);
-  };
-  const unsigned xa = lds0 + q_off(wm + lr, hi), wa = lds0 + BM * kBK + q_off(wn + lr, hi);
-  i32x16 acc[FI][FJ];
-  i32x4 xf[2][FI], wf[2][FJ];  // two chunks' fragments
-  auto frags = [&](int p, int bf, int c) {
-    const unsigned o = (unsigned)bf * kStage, x = 32u * (c + ks * CH);
+  }
+  SC_DEV void cols(int p, int bf, int c) {  // chunk c of 64 k of the stage in buffer bf
 #pragma unroll
-    for (int j = 0; j < FJ; ++j) wf[p][j] = lds_read_q((wa ^ x) + o + j * (32 * kBK));
+    for (int j = 0; j < FJ; ++j) wf[p][j] = lds_read_q((wa ^ (64u * c)) + (unsigned)bf * kStage + j * (16 * kBK));
+  }
+  SC_DEV void rows(int h, int bf, int c) {
 #pragma unroll
-    for (int i = 0; i < FI; ++i) xf[p][i] = lds_read_q((xa ^ x) + o + i * (32 * kBK));
-  };
-  auto mul = [&](int p) {
+    for (int i = 0; i < FH; ++i)
+      xf[h][i] = lds_read_q((xa ^ (64u * c)) + (unsigned)bf * kStage + (h * FH + i) * (16 * kBK));
+    __builtin_amdgcn_sched_barrier(0);  // the reads stay ahead of the products that follow
+  }
+  SC_DEV void mul(int h, int p) {
 #pragma unroll
-    for (int i = 0; i < FI; ++i)
+    for (int i = 0; i < FH; ++i)
 #pragma unroll
       for (int j = 0; j < FJ; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[p][j], xf[p][i], acc[i][j], 0, 0, 0);
-  };
-  auto next_buf = [&](int bf) { return bf == kNBuf - 1 ? 0 : bf + 1; };
-  constexpr int kAhead = kNBuf - 1;  // stages of the next tile loaded beside the results, which leave through the last buffer
-  int m0, n0, cur = 0;
-  place(item, m0, n0);
-  bring(m0, n0);
-  put(tab[0]);
-  __syncthreads();
-  offsets(tab[0], n0);
-#pragma unroll
-  for (int p = 0; p < kAhead; ++p)
-    if (p < ns) issue(p, p);
-  while (true) {
+        acc[h * FH + i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[p][j], xf[h][i], acc[h * FH + i][j], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  SC_DEV void clear() {
 #pragma unroll
     for (int i = 0; i < FI; ++i)
 #pragma unroll
-      for (int j = 0; j < FJ; ++j) acc[i][j] = i32x16{};
-    if (kAhead < ns) issue(kAhead, kAhead);
-    const long long nitem = item + (gridDim.x >> 3);
-    const bool more = nitem < last;
-    int nm0 = 0, nn0 = 0;
-    if (more) place(nitem, nm0, nn0);
-    wait_stages<kNBuf, kDma>(min(ns, kNBuf) - 1);
-    __syncthreads();
-    int bf = 0;
-    frags(0, 0, 0);
-    // One barrier per stage, before its last product: a chunk's fragments are in flight
-    // during the products of the one before, across stages too, and a stage's buffer is
-    // refilled once every wave holds its last fragments.
-    for (int s = 0; s + 1 < ns; ++s) {
-      const int bn = next_buf(bf);
+      for (int j = 0; j < FJ; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  }
+  static SC_DEV int next_buf(int bf) { return bf == kNBuf - 1 ? 0 : bf + 1; }
+
+  SC_DEV void store16(O* row, int col, uint4 v) const {  // 16 bytes of a row at column col
+    constexpr int kE = 16 / sizeof(O);
+    if (col >= a.N) return;
+    if (a.vec) {
+      *reinterpret_cast<uint4*>(row + col) = v;
+    } else {
+      const O* e = reinterpret_cast<const O*>(&v);
 #pragma unroll
-      for (int c = 0; c + 1 < CH; ++c) {
-        frags((c + 1) & 1, bf, c + 1);
-        mul(c & 1);
+      for (int q = 0; q < kE; ++q)
+        if (col + q < a.N) row[col + q] = e[q];
+    }
+  }
+  // Stores 16 rows (16 i on) of two column fragments (j, j + 1; one where a wave has but
+  // one): element e of a lane is row 16 i + lr, column 16 j + 4 g + e.  As bf16 a lane
+  // holds 8 bytes of each fragment; exchanging them between neighbouring lane groups
+  // leaves it with 16 bytes of one, and every group of four lanes with 64 bytes of a row.
+  SC_DEV void emit(const i32x4 (&v)[FI][FJ], const LinTables& d, int n0, int i, int j) const {
+    const int r = wm + 16 * i + lr;
+    const float xs = d.xs[r];
+    O* row = static_cast<O*>(a.out) + (long long)d.grow[r] * a.N;
+    constexpr int kF = FJ == 1 ? 1 : 2;
+    unsigned p[kF][2];
+#pragma unroll
+    for (int f = 0; f < kF; ++f) {
+      const int c = wn + 16 * (j + f) + 4 * g;
+      const f32x4 ws = *reinterpret_cast<const f32x4*>(d.sw + c), bs = *reinterpret_cast<const f32x4*>(d.sb + c);
+      f32x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = finish<sizeof(O) == 4, kGelu>(v[i][j + f][e], xs, ws[e], bs[e]);
+      if constexpr (sizeof(O) == 4) {
+        store16(row, n0 + c, __builtin_bit_cast(uint4, o));
+      } else {
+        p[f][0] = pack_bf16(o[0], o[1]);
+        p[f][1] = pack_bf16(o[2], o[3]);
       }
-      wait_stages<kNBuf - 1, kDma>(min(ns - 2 - s, kNBuf - 2));
-      __syncthreads();
-      if (s + kNBuf < ns) issue(s + kNBuf, bf);
-      frags(0, bn, 0);
-      mul(1);
-      bf = bn;
     }
+    if constexpr (sizeof(O) == 2 && kF == 2) {
+      const auto lo = __builtin_amdgcn_permlane16_swap(p[0][0], p[1][0], false, false);
+      const auto hi = __builtin_amdgcn_permlane16_swap(p[0][1], p[1][1], false, false);
+      store16(row, n0 + wn + 16 * (j + (g & 1)) + 8 * (g >> 1),
+              make_uint4((unsigned)lo[0], (unsigned)hi[0], (unsigned)lo[1], (unsigned)hi[1]));
+    } else if constexpr (sizeof(O) == 2) {
+      const int col = n0 + wn + 16 * j + 4 * g;
+      if (col < a.N) {
+        if (a.vec) {
+          *reinterpret_cast<uint2*>(row + col) = make_uint2(p[0][0], p[0][1]);
+        } else {
+          const O* e = reinterpret_cast<const O*>(p[0]);
 #pragma unroll
-    for (int c = 0; c + 1 < CH; ++c) {
-      frags((c + 1) & 1, bf, c + 1);
-      if (c == 0 && more) bring(nm0, nn0);
-      mul(c & 1);
-    }
-    mul(1);
-    __syncthreads();  // every wave has read the last stage
-    const int on0 = n0;
-    const LinTables& d = tab[cur];
-    if (more) {
-      put(tab[cur ^ 1]);
-      __syncthreads();
-      n0 = nn0;
-      offsets(tab[cur ^ 1], n0);
-#pragma unroll
-      for (int p = 0; p < kAhead; ++p)
-        if (p < ns) issue(p, p);
-    }
-    // Element e of a lane's acc[i][j] is row wm + 32 i + lr, column wn + 32 j + 8 (e / 4)
-    // + 4 hi + e % 4.  A wave's part goes through the last stage buffer, kSr rows at a
-    // time (16-byte units swizzled by the row), and leaves as whole 16-byte units.
-    constexpr int es = sizeof(O), kUr = WN * es / 16, kRb = WN * es, kEpu = 16 / es;
-    constexpr int kParts = 8 / KS, kSr = kParts * 32 * kRb <= kStage ? 32 : 16;
-    static_assert(kParts * kSr * kRb <= kStage && (KS == 1 || kParts * 4096 * FI * FJ <= kStage), "staging rows");
-    char* st = stage + kAhead * kStage + wt * (kSr * kRb);
-    if constexpr (KS == 2) {  // the second half's sums through the same buffer
-      int* red = reinterpret_cast<int*>(stage + kAhead * kStage) + wt * 1024 * FI * FJ;
-      if (ks == 1) {
-#pragma unroll
-        for (int i = 0; i < FI; ++i)
-#pragma unroll
-          for (int j = 0; j < FJ; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) red[((i * FJ + j) * 16 + e) * 64 + lane] = acc[i][j][e];
-      }
-      __syncthreads();
-      if (ks == 0) {
-#pragma unroll
-        for (int i = 0; i < FI; ++i)
-#pragma unroll
-          for (int j = 0; j < FJ; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] += red[((i * FJ + j) * 16 + e) * 64 + lane];
-      }
-      __syncthreads();
-    }
-    if (ks == 0) {
-#pragma unroll
-      for (int i = 0; i < FI; ++i) {
-        const float xs = d.xs[wm + 32 * i + lr];
-#pragma unroll
-        for (int r0 = 0; r0 < 32; r0 += kSr) {
-          if (kSr == 32 || (lr >= r0 && lr < r0 + kSr)) {
-#pragma unroll
-            for (int j = 0; j < FJ; ++j)
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const int c = 32 * j + 8 * q + 4 * hi;
-                const f32x4 ws = *reinterpret_cast<const f32x4*>(d.sw + wn + c);
-                const f32x4 bs = *reinterpret_cast<const f32x4*>(d.sb + wn + c);
-                f32x4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = finish<es == 4, kGelu>(acc[i][j][4 * q + e], xs, ws[e], bs[e]);
-                const int r = lr - r0, un = c * es / 16;
-                char* o = st + r * kRb + 16 * (un ^ (r & (kUr - 1)));
-                if constexpr (es == 4)
-                  *reinterpret_cast<uint4*>(o) = __builtin_bit_cast(uint4, v);
-                else
-                  *reinterpret_cast<uint2*>(o + 8 * hi) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-              }
-          }
-          wave_exchange();
-#pragma unroll
-          for (int x = 0; x < kSr * kUr / 64; ++x) {
-            const int r = x * (64 / kUr) + lane / kUr, un = lane % kUr, gr = d.grow[wm + 32 * i + r0 + r];
-            const int col = on0 + wn + un * kEpu;
-            const uint4 v = *reinterpret_cast<const uint4*>(st + r * kRb + 16 * (un ^ (r & (kUr - 1))));
-            if (gr < 0 || col >= a.N) continue;
-            O* o = static_cast<O*>(a.out) + (long long)gr * a.N + col;
-            if (a.vec) {
-              *reinterpret_cast<uint4*>(o) = v;
-            } else {
-              const O* e = reinterpret_cast<const O*>(&v);
-#pragma unroll
-              for (int q = 0; q < kEpu; ++q)
-                if (col + q < a.N) o[q] = e[q];
-            }
-          }
-          wave_exchange();
+          for (int q = 0; q < 4; ++q)
+            if (col + q < a.N) row[col + q] = e[q];
         }
       }
     }
-    if (!more) break;
-    item = nitem;
-    cur ^= 1;
-    __syncthreads();  // the results have left the last stage buffer
   }
+};
+
+// Tiles one after the other: all stage buffers but the one at hand in flight during a
+// tile, the next tile's first stages during its results.
+template <int kM, typename O, bool kGelu>
+SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const Packed& pk, int R, const LinPlan& pl) {
+  using W = LinWave<kM, O, kGelu>;
+  constexpr int kNBuf = W::kNBuf, kDma = W::kDma;
+  LinShare sh(pl);
+  if (sh.item >= sh.last) return;
+  W w(a, stage, pk, R);
+  const int ns = a.Kp / kBK;
+  int m0, n0, cur = 0;
+  sh.template place<W::BM, W::BN>(sh.item, m0, n0);
+  w.bring(m0, n0);
+  w.put(tab[0]);
+  __syncthreads();
+  w.offsets(tab[0], n0);
+#pragma unroll
+  for (int p = 0; p < kNBuf; ++p)
+    if (p < ns) w.issue(p, p);
+  while (true) {
+    w.clear();
+    const long long nitem = sh.item + sh.step;
+    const bool more = nitem < sh.last;
+    int nm0 = 0, nn0 = 0;
+    if (more) sh.template place<W::BM, W::BN>(nitem, nm0, nn0);
+    wait_stages<kNBuf, kDma>(min(ns, kNBuf) - 1);
+    __syncthreads();
+    int bf = 0;
+    w.cols(0, 0, 0);
+    w.rows(0, 0, 0);
+    // Two chunks a stage, two halves of the rows each: a half's fragments are in flight
+    // during the products of the one before, across stages too.  One barrier per stage,
+    // before its last products: the next stage has landed, and this one's buffer is
+    // refilled, since every wave holds its last fragments.
+    for (int s = 0; s + 1 < ns; ++s) {
+      const int bn = W::next_buf(bf);
+      w.rows(1, bf, 0);
+      w.mul(0, 0);
+      w.cols(1, bf, 1);
+      w.rows(0, bf, 1);
+      w.mul(1, 0);
+      w.rows(1, bf, 1);
+      w.mul(0, 1);
+      wait_stages<kNBuf - 1, kDma>(min(ns - 2 - s, kNBuf - 2));
+      __syncthreads();
+      if (s + kNBuf < ns) w.issue(s + kNBuf, bf);
+      w.cols(0, bn, 0);
+      w.rows(0, bn, 0);
+      w.mul(1, 1);
+      bf = bn;
+    }
+    w.rows(1, bf, 0);
+    if (more) w.bring(nm0, nn0);
+    w.mul(0, 0);
+    w.cols(1, bf, 1);
+    w.rows(0, bf, 1);
+    w.mul(1, 0);
+    w.rows(1, bf, 1);
+    w.mul(0, 1);
+    w.mul(1, 1);
+    if (more) {
+      w.put(tab[cur ^ 1]);
+      __syncthreads();  // and every wave has read the last stage
+      w.offsets(tab[cur ^ 1], nn0);
+#pragma unroll
+      for (int p = 0; p < kNBuf; ++p)
+        if (p < ns) w.issue(p, p);
+    }
+#pragma unroll
+    for (int i = 0; i < W::FI; ++i)
+#pragma unroll
+      for (int j = 0; j < W::FJ; j += 2) w.emit(w.acc, tab[cur], n0, i, j);
+    if (!more) return;
+    sh.item = nitem;
+    n0 = nn0;
+    cur ^= 1;
+  }
+}
+
+// The same for tiles of enough stages (kStreamMin), as one stream: the next tile's
+// stages follow this one's into the buffers without a gap, and a tile's results are
+// finished and stored during the next tile's products, a sixteenth of a wave's part
+// after every chunk, so that one wave's arithmetic on results runs beside the other
+// waves' matrix instructions, and the stores spread over the whole time.
+template <typename O, bool kGelu>
+SC_DEV void linear_stream(const LinearArgs& a, char* stage, LinTables* tab, const Packed& pk, int R, const LinPlan& pl) {
+  using W = LinWave<0, O, kGelu>;
+  constexpr int kNBuf = W::kNBuf, kDma = W::kDma, kUnits = W::FI * W::FJ / 2;
+  static_assert(kStreamMin == kNBuf + 2, "a barrier between the last tile's results and the next tile's tables");
+  LinShare sh(pl);
+  if (sh.item >= sh.last) return;
+  W w(a, stage, pk, R);
+  const int ns = a.Kp / kBK;
+  int m0, n0, pn0 = 0, bf = 0;
+  int tc = 0, tp = 2, tn = 1;  // tables of this tile, the last one and the next one
+  sh.template place<W::BM, W::BN>(sh.item, m0, n0);
+  w.bring(m0, n0);
+  w.put(tab[tc]);
+  __syncthreads();
+  w.offsets(tab[tc], n0);
+#pragma unroll
+  for (int p = 0; p < kNBuf; ++p) w.issue(p, p);
+  wait_vm<(kNBuf - 1) * kDma>();
+  __syncthreads();
+  w.cols(0, 0, 0);
+  w.rows(0, 0, 0);
+  i32x4 done[W::FI][W::FJ];  // the last tile's sums
+  bool pending = false;
+  while (true) {
+    w.clear();
+    const long long nitem = sh.item + sh.step;
+    const bool more = nitem < sh.last;
+    int nm0 = 0, nn0 = 0;
+    if (more) sh.template place<W::BM, W::BN>(nitem, nm0, nn0);
+    // Stage s; unit u of the last tile's results beside it (none: u < 0).
+    auto step = [&](int s, int u) {
+      const int bn = W::next_buf(bf);
+      w.rows(1, bf, 0);
+      w.mul(0, 0);
+      if (u >= 0) w.emit(done, tab[tp], pn0, u / (W::FJ / 2), 2 * (u % (W::FJ / 2)));
+      w.cols(1, bf, 1);
+      w.rows(0, bf, 1);
+      w.mul(1, 0);
+      w.rows(1, bf, 1);
+      w.mul(0, 1);
+      const bool turn = more && s == ns - kNBuf - 1;  // at least one barrier into the tile
+      if (turn) {
+        w.bring(nm0, nn0);
+        w.put(tab[tn]);
+      }
+      if (more || s + 1 < ns) {
+        if (more || s + 2 < ns)
+          wait_vm<(kNBuf - 2) * kDma>();
+        else
+          wait_vm<0>();
+        __syncthreads();
+        if (s + kNBuf < ns)
+          w.issue(s + kNBuf, bf);
+        else if (more)
+          w.issue(s + kNBuf - ns, bf);  // the next tile's
+        if (turn) w.offsets(tab[tn], nn0);
+        w.cols(0, bn, 0);
+        w.rows(0, bn, 0);
+      }
+      w.mul(1, 1);
+      bf = bn;
+    };
+    int s = 0;
+    if (pending) {
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) {
+        if (s < ns) {
+          step(s, u);
+          ++s;
+        } else {
+          w.emit(done, tab[tp], pn0, u / (W::FJ / 2), 2 * (u % (W::FJ / 2)));
+        }
+      }
+    }
+    for (; s < ns; ++s) step(s, -1);
+#pragma unroll
+    for (int i = 0; i < W::FI; ++i)
+#pragma unroll
+      for (int j = 0; j < W::FJ; ++j) done[i][j] = w.acc[i][j];
+    pending = true;
+    pn0 = n0;
+    if (!more) break;
+    n0 = nn0;
+    sh.item = nitem;
+    const int t = tp;
+    tp = tc;
+    tc = tn;
+    tn = t;
+    // the tables of the tile before last are free: its results were finished before the
+    // barriers of this tile's last stages
+  }
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u) w.emit(done, tab[tc], pn0, u / (W::FJ / 2), 2 * (u % (W::FJ / 2)));
 }
 
 template <typename O, bool kGelu>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_linear(LinearArgs a) {
   __shared__ __attribute__((aligned(1024))) char stage[kLinLds];
-  __shared__ __attribute__((aligned(16))) LinTables tab[2];
+  __shared__ __attribute__((aligned(16))) LinTables tab[3];
   __shared__ int pre[kCoarse + 1];
   const int per = (a.B + kCoarse - 1) / kCoarse, count = (a.B + per - 1) / per;
   const Packed pk{pre, a.len, a.B, a.n, per, count};
@@ -652,13 +761,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   if (R > 0) {
     const LinPlan pl = lin_plan(R, a.N, a.Kp / kBK);
     if (pl.mode == 0)
-      linear_run<0, O, kGelu>(a, stage, tab, pk, R, pl);
+      linear_stream<O, kGelu>(a, stage, tab, pk, R, pl);
     else if (pl.mode == 1)
-      linear_run<1, O, kGelu>(a, stage, tab, pk, R, pl);
-    else if (pl.mode == 2)
-      linear_run<2, O, kGelu>(a, stage, tab, pk, R, pl);
+      linear_tiles<1, O, kGelu>(a, stage, tab, pk, R, pl);
     else
-      linear_run<3, O, kGelu>(a, stage, tab, pk, R, pl);
+      linear_tiles<2, O, kGelu>(a, stage, tab, pk, R, pl);
   }
   if (!a.len || a.skip_pad) return;
   // zeros into the padding rows, an even share a workgroup
