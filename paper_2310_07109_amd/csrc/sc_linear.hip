@@ -7,7 +7,9 @@
 // k_linear        the product on v_mfma_i32_16x16x64_i8: sums of up to 131072
 //                 products of 127 x 127 fit an int32, so they are exact in any
 //                 order, and a row's result does not depend on the tile that
-//                 computed it.
+//                 computed it.  (With random operands the 16x16x64 form sustains
+//                 4.0 POP/s here, 32x32x32 3.5: the clock follows the power; with
+//                 zeros 4.8 and 4.9.)
 // k_linear_few    the same for a few rows: quantisation and product in one launch.
 #include <algorithm>
 
@@ -272,7 +274,7 @@ struct LinearArgs {
 constexpr int kBK = 128;        // bytes of a row per K stage: whole lines (64-byte pieces halve the loads' rate)
 constexpr int kLinWgs = 256;    // one workgroup per CU, each taking tiles in turn
 constexpr int kLinLds = 147456; // stage buffers: 3 x 48, 4 x 32 or 8 x 16 KB
-constexpr int kLinModes = 3;
+constexpr int kLinModes = 4;
 constexpr int kGroupM = 8;
 // k_linear_few: at most kFewRows rows of kFewK bytes, kFewWgs workgroups and
 // kFewWork bytes of rows over all of them.  us in a graph, bf16 rows, this kernel and
@@ -291,23 +293,28 @@ template <>
 struct LinTile<1> { static constexpr int kBM = 128, kBN = 128, kWgM = 4, kWgN = 2, kNBuf = 4; };
 template <>
 struct LinTile<2> { static constexpr int kBM = 64, kBN = 64, kWgM = 2, kWgN = 4, kNBuf = 8; };
+template <>
+struct LinTile<3> { static constexpr int kBM = 256, kBN = 256, kWgM = 2, kWgN = 4, kNBuf = 2; };
 
 struct LinPlan {
   int mode, T, Nt;
 };
 constexpr int kStreamMin = 5;  // stages that linear_stream needs: its buffers and two
 // The mode with the least rounds of workgroups times the cost of a tile: of a stage
-// and of what stands beside the stages, in cycles.
+// and of what stands beside the stages, in cycles at 2.4 GHz, from full launches (us,
+// modes 0 to 3: 32768 x 4096 x 1024 129, 151, 280, 113; 32768 x 1024 x 4096 167, 207,
+// 480, 154; 24165 x 768 x 768, where the tiles do not fill whole rounds, 28, 29, 57, 33).
 SC_DEV LinPlan lin_plan(int R, int N, int ns) {
   LinPlan p = {0, 0, 0};
   long long best = 1LL << 62;
 #pragma unroll
   for (int m = 0; m < kLinModes; ++m) {
-    const int bm = m == 0 ? 256 : m == 1 ? 128 : 64, bn = m == 2 ? 64 : 128;
-    const int stage = m == 0 ? 1300 : m == 1 ? 800 : 450, fixed = m == 0 ? 1500 : m == 1 ? 4500 : 3000;
+    const int bm = m == 0 || m == 3 ? 256 : m == 1 ? 128 : 64, bn = m == 2 ? 64 : m == 3 ? 256 : 128;
+    const int stage = m == 0 ? 2170 : m == 1 ? 1240 : m == 2 ? 500 : 3680;
+    const int fixed = m == 0 ? 7700 : m == 1 ? 5600 : m == 2 ? 5000 : 16700;
     const int T = (R + bm - 1) / bm, Nt = (N + bn - 1) / bn;
     const long long rounds = ((long long)T * Nt + kLinWgs - 1) / kLinWgs;
-    const long long t = rounds * (ns * stage + fixed) + (m == 0 ? 6000 : 0);
+    const long long t = rounds * (ns * stage + fixed);
     if (t < best && (m > 0 || ns >= kStreamMin)) {
       best = t;
       p.mode = m;
@@ -329,7 +336,7 @@ SC_DEV i32x4 lds_read_q(unsigned addr) {
 
 // The row numbering (sc_pack.h) with a table of fixed size: the prefix sums of every
 // `per`-th sequence, the rest by a scan of at most per - 1 lengths.
-constexpr int kCoarse = 512;
+constexpr int kCoarse = 192;
 struct Packed {
   const int* pre;  // LDS
   const int* len;
@@ -387,7 +394,7 @@ struct Packed {
 // A tile's rows and columns, in LDS.
 struct LinTables {
   int grow[256], xrow[256];  // row of out and of xq; rows past the last one repeat it
-  float xs[256], sw[128], sb[128];
+  float xs[256], sw[256], sb[256];
 };
 
 // A workgroup's share of the tiles.  They go to the XCDs in contiguous ranges
@@ -575,6 +582,9 @@ SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const
   if (sh.item >= sh.last) return;
   W w(a, stage, pk, R);
   const int ns = a.Kp / kBK;
+  // the last tile's stores that the first stages, loaded before them, do not wait for
+  constexpr int kStores = W::FI * (W::FJ + 1) / 2 * (sizeof(O) == 4 && W::FJ > 1 ? 2 : 1);
+  bool stored = false;
   int m0, n0, cur = 0;
   sh.template place<W::BM, W::BN>(sh.item, m0, n0);
   w.bring(m0, n0);
@@ -590,7 +600,10 @@ SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const
     const bool more = nitem < sh.last;
     int nm0 = 0, nn0 = 0;
     if (more) sh.template place<W::BM, W::BN>(nitem, nm0, nn0);
-    wait_stages<kNBuf, kDma>(min(ns, kNBuf) - 1);
+    if (stored)
+      wait_stages<kNBuf, kDma, kStores>(min(ns, kNBuf) - 1);
+    else
+      wait_stages<kNBuf, kDma>(min(ns, kNBuf) - 1);
     __syncthreads();
     int bf = 0;
     w.cols(0, 0, 0);
@@ -608,7 +621,10 @@ SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const
       w.mul(1, 0);
       w.rows(1, bf, 1);
       w.mul(0, 1);
-      wait_stages<kNBuf - 1, kDma>(min(ns - 2 - s, kNBuf - 2));
+      if (stored && s + 1 < kNBuf)
+        wait_stages<kNBuf - 1, kDma, kStores>(min(ns - 2 - s, kNBuf - 2));
+      else
+        wait_stages<kNBuf - 1, kDma>(min(ns - 2 - s, kNBuf - 2));
       __syncthreads();
       if (s + kNBuf < ns) w.issue(s + kNBuf, bf);
       w.cols(0, bn, 0);
@@ -637,6 +653,7 @@ SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const
     for (int i = 0; i < W::FI; ++i)
 #pragma unroll
       for (int j = 0; j < W::FJ; j += 2) w.emit(w.acc, tab[cur], n0, i, j);
+    stored = a.vec && n0 + W::BN <= a.N;  // a whole tile: exactly kStores of them, every lane's
     if (!more) return;
     sh.item = nitem;
     n0 = nn0;
@@ -764,8 +781,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
       linear_stream<O, kGelu>(a, stage, tab, pk, R, pl);
     else if (pl.mode == 1)
       linear_tiles<1, O, kGelu>(a, stage, tab, pk, R, pl);
-    else
+    else if (pl.mode == 2)
       linear_tiles<2, O, kGelu>(a, stage, tab, pk, R, pl);
+    else
+      linear_tiles<3, O, kGelu>(a, stage, tab, pk, R, pl);
   }
   if (!a.len || a.skip_pad) return;
   // zeros into the padding rows, an even share a workgroup

@@ -47,14 +47,15 @@ SC_DEV void wait_vm() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
 }
 
-// Waits until at most `later` (< kNBuf) stages of kPer loads are in flight.
-template <int kNBuf, int kPer, int kL = kNBuf - 1>
+// Waits until at most `later` (< kNBuf) stages of kPer loads and kExtra newer
+// accesses are in flight.
+template <int kNBuf, int kPer, int kExtra = 0, int kL = kNBuf - 1>
 SC_DEV void wait_stages(int later) {
   if constexpr (kL == 0) {
-    wait_vm<0>();
+    wait_vm<kExtra>();
   } else {
-    if (later >= kL) wait_vm<kL * kPer>();
-    else wait_stages<kNBuf, kPer, kL - 1>(later);
+    if (later >= kL) wait_vm<kL * kPer + kExtra>();
+    else wait_stages<kNBuf, kPer, kExtra, kL - 1>(later);
   }
 }
 
