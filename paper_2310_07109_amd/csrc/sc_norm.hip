@@ -177,16 +177,45 @@ struct Cols {
 };
 
 // Both norms' weights and a gate by channel in LDS, a row of kWidth each: absent
-// ones are 1 and 0, the channels past D are 0 (so that sums over them stay 0).
+// ones are 1 and 0, the channels past D are 0 (so that sums over them stay 0).  The
+// row slots share the rows, and a slot's loads are all in flight together (one at a
+// time they took 40 round trips at 1111 channels: 25 us of a backward launch).
 enum { kPostW, kPostB, kPreW, kPreB, kGateRow, kWeights };
-template <int kWidth>
+template <int kVec, int kPer, int kTpr>
 SC_DEV void stage_weights(float* lds, const Norm& a, int count) {
+  using C = Cols<float, kVec, kPer, kTpr>;
+  constexpr int kRows = kThreads<kTpr> / kTpr, kMine = (kWeights + kRows - 1) / kRows;
+  const C c{a.D, (int)threadIdx.x % kTpr};
+  const int slot = kRows > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kTpr) : 0;
   const float* src[kWeights] = {a.post_w, a.post_b, a.pre_w, a.pre_b,
                                 a.gate_mode == kGateChannel ? static_cast<const float*>(a.gate) : nullptr};
+  typename C::Raw raw[kMine][kPer];
 #pragma unroll
-  for (int k = 0; k < kWeights; ++k)
-    for (int i = k < count ? (int)threadIdx.x : kWidth; i < kWidth; i += blockDim.x)
-      lds[k * kWidth + i] = i >= a.D ? 0.f : src[k] ? src[k][i] : k == kPostB || k == kPreB ? 0.f : 1.f;
+  for (int m = 0; m < kMine; ++m) {
+    const float* p = nullptr;
+#pragma unroll
+    for (int k = 0; k < kWeights; ++k)
+      if (k == slot + m * kRows && k < count) p = src[k];
+    c.load(row_buffer(p, 0, a.D, p != nullptr), raw[m]);
+  }
+#pragma unroll
+  for (int m = 0; m < kMine; ++m) {
+    const int k = slot + m * kRows;
+    if (k >= count) continue;
+    bool have = false;
+#pragma unroll
+    for (int i = 0; i < kWeights; ++i)
+      if (i == k) have = src[i] != nullptr;
+    const float absent = k == kPostB || k == kPreB ? 0.f : 1.f;
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      float v[kVec];
+      C::B::unpack(raw[m][u], v);
+#pragma unroll
+      for (int q = 0; q < kVec; ++q)
+        lds[k * C::kWidth + c.at(u) + q] = have || !c.in(u) ? v[q] : absent;
+    }
+  }
   __syncthreads();
 }
 
@@ -265,6 +294,9 @@ __global__ __launch_bounds__(kThreads<kTpr>) void k_norm(Norm a) {
   const float fd = (float)a.D;
   const int Dp = (a.D + kI8Pitch - 1) / kI8Pitch * kI8Pitch;
   const unsigned rows = (unsigned)a.B * (unsigned)a.n, step = gridDim.x * kRows;
+  // Slot i's row of round k is k step + (i + k turn) mod step: without the turn a slot
+  // whose place in the sequences is padding in one round would be so in every round.
+  const unsigned turn = (unsigned)(0.382f * (float)step) / kRows * kRows;
   const unsigned slot = kTpr == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
   typename C::Raw rx[kPer], rt[kPer], rg[kPer];
   auto fetch = [&](const RowAt& r) {
@@ -274,12 +306,18 @@ __global__ __launch_bounds__(kThreads<kTpr>) void k_norm(Norm a) {
     c.load(row_buffer(static_cast<const T*>(a.t), r.row, a.D, r.live && a.t), rt);
     if (gate_rows(a)) c.load(row_buffer(static_cast<const T*>(a.gate), gate_row(a, r), a.D, r.live), rg);
   };
-  RowAt cur = row_at(a, blockIdx.x * kRows + slot, blockIdx.x * kRows + slot < rows);
+  unsigned place = blockIdx.x * kRows + slot, round = 0;  // round: its first row
+  RowAt cur = row_at(a, place, place < rows);
   fetch(cur);
-  stage_weights<C::kWidth>(lw, a, kWeights);
-  for (; cur.row < rows;) {
-    const unsigned nrow = cur.row + step;  // below 2^31 + 2^24
-    const RowAt next = row_at(a, nrow, nrow < rows);
+  stage_weights<kVec, kPer, kTpr>(lw, a, kWeights);
+  while (round < rows) {
+    round += step;  // below 2^31 + 2^24
+    place = place + turn < step ? place + turn : place + turn - step;
+    const RowAt next = row_at(a, round + place, round + place < rows);
+    if (cur.row >= rows) {  // the last round is not whole
+      cur = next;
+      continue;
+    }
     const long long row = cur.row;
     const auto r = row_buffer(static_cast<const T*>(a.r), row, a.D, a.r);
     const auto y = row_buffer(static_cast<const T*>(a.y), row, a.D, a.y);
@@ -426,7 +464,7 @@ __global__ __launch_bounds__(kThreads<kTpr>) __attribute__((amdgpu_waves_per_eu(
   for (int k = 0; k < kSums; ++k)
 #pragma unroll
     for (int i = 0; i < E; ++i) sum[k][i] = 0.f;
-  typename C::Raw rx[kPer], rt[kPer], rg[kToken ? kPer : 1], rr[kPer], ry[kPer];
+  typename C::Raw rx[kPer], rt[kPer], rg[kPer], rr[kPer], ry[kPer];
   auto fetch = [&](const RowAt& r) {
     c.load(row_buffer(static_cast<const T*>(a.t), r.row, a.D, r.live && a.t), rt);
     c.load(row_buffer(static_cast<const T*>(a.x), r.row, a.D, r.live), rx);
@@ -445,11 +483,15 @@ __global__ __launch_bounds__(kThreads<kTpr>) __attribute__((amdgpu_waves_per_eu(
     fetch(cur);
     if (seq) {
       __syncthreads();  // the last item's rows are done
-      const T* g = static_cast<const T*>(a.gate) + (long long)bs * a.D;
-      for (int i = threadIdx.x; i < C::kWidth; i += blockDim.x) lw[kGateRow * C::kWidth + i] = i < a.D ? (float)g[i] : 0.f;
+      if (threadIdx.x < kTpr) {
+        typename C::Raw rg[kPer];
+        c.load(row_buffer(static_cast<const T*>(a.gate), bs, a.D, true), rg);
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) C::B::unpack(rg[u], lw + kGateRow * C::kWidth + c.at(u));
+      }
       if (staged) __syncthreads();
     }
-    if (!staged) stage_weights<C::kWidth>(lw, a, seq ? kGateRow : kWeights);
+    if (!staged) stage_weights<kVec, kPer, kTpr>(lw, a, seq ? kGateRow : kWeights);
     staged = true;
     for (; cur.row < end;) {
       const RowAt next = row_at(a, cur.row + step, cur.row + step < end);
