@@ -556,7 +556,7 @@ struct StackWs {
   float *t, *scores, *partials;
   float* split;  // slabs of the split reductions of the output and second feed-forward products
   int *len_a, *len_b, *gp_a, *gp_b, *orig_a, *orig_b, *keep_idx, *new_index;
-  // 8-bit stack: rows quantised for a product (packed) and by a norm (in place), and their scales
+  // 8-bit stack: rows quantised for a product and by a norm, and their scales
   int8_t *xq, *yq;
   float *xs, *ys;
   AttnArgs attn;
@@ -789,8 +789,8 @@ sc_status run_stack_i8(const sc_attn_desc* d, int32_t n_layers, const int32_t* w
   Launches chk;
   StackRows rows = stack_rows(d, w, chk, s);
   __bf16* t = reinterpret_cast<__bf16*>(w.t);
-  // out = lin(wt, v): 8-bit rows of the survivors (len), packed or in place
-  auto linear = [&](const int8_t* q, const float* qs, int packed, const sc_i8_weight& wt, void* out, int K, int N,
+  // out = lin(wt, v), v given as 8-bit rows, on the rows of len
+  auto linear = [&](const int8_t* q, const float* qs, const sc_i8_weight& wt, void* out, int K, int N,
                     const int* len, int gelu) {
     sc::Linear a;
     std::memset(&a, 0, sizeof(a));
@@ -805,13 +805,12 @@ sc_status run_stack_i8(const sc_attn_desc* d, int32_t n_layers, const int32_t* w
     a.K = K;
     a.N = N;
     a.len = len;
-    a.packed = packed;
     a.skip_pad = 1;
     a.gelu = gelu;
     chk(sc::launch_linear_i8(a, s));
   };
   auto quantise = [&](const void* v, int K, const int* len, const int* xidx) {
-    chk(sc::launch_quant_rows(v, 0, w.xq, w.xs, B, n, K, len, xidx, 1, s));
+    chk(sc::launch_quant_rows(v, 0, w.xq, w.xs, B, n, K, len, xidx, 0, nullptr, 0, s));
   };
   // y = LayerNorm(res_scale x + gate t) w + b on the survivors, and its 8-bit rows in place
   auto norm = [&](const void* x, const int* xidx, const float* gate, const float* lw, const float* lb, void* y,
@@ -845,18 +844,18 @@ sc_status run_stack_i8(const sc_attn_desc* d, int32_t n_layers, const int32_t* w
     // the norm that ends a layer leaves the next one's rows quantised
     if (l == 0) {
       quantise(cur, D, rows.len_cur, nullptr);
-      linear(w.xq, w.xs, 1, y.qkv, w.qkv, D, 3 * D, rows.len_cur, 0);
+      linear(w.xq, w.xs, y.qkv, w.qkv, D, 3 * D, rows.len_cur, 0);
     } else {
-      linear(w.yq, w.ys, 0, y.qkv, w.qkv, D, 3 * D, rows.len_cur, 0);
+      linear(w.yq, w.ys, y.qkv, w.qkv, D, 3 * D, rows.len_cur, 0);
     }
     attend_and_prune(d, w, rows, windows ? windows[l] : d->window, l, thresholds[l], keep_global, kept_per_layer, chk,
                      s);
     quantise(w.o, D, rows.len_nxt, w.keep_idx);
-    linear(w.xq, w.xs, 1, y.o, t, D, D, rows.len_nxt, 0);
+    linear(w.xq, w.xs, y.o, t, D, D, rows.len_nxt, 0);
     norm(cur, w.keep_idx, y.gate1, y.ln1_w, y.ln1_b, w.x1, true);
-    linear(w.yq, w.ys, 0, y.w1, w.h, D, F, rows.len_nxt, 1);
+    linear(w.yq, w.ys, y.w1, w.h, D, F, rows.len_nxt, 1);
     quantise(w.h, F, rows.len_nxt, nullptr);
-    linear(w.xq, w.xs, 1, y.w2, t, F, D, rows.len_nxt, 0);
+    linear(w.xq, w.xs, y.w2, t, F, D, rows.len_nxt, 0);
     norm(w.x1, nullptr, y.gate2, y.ln2_w, y.ln2_b, nxt, l + 1 < n_layers);
     cur = nxt;
     rows.next();

@@ -132,7 +132,7 @@ sc_status quantize_rows_impl(int32_t B, int32_t n, int32_t K, const int32_t* val
   if (overlaps(xq, qb, x, xb) || overlaps(scale, sb, x, xb) || overlaps(xq, qb, scale, sb)) return SC_EINVAL;
   if (valid_len && (overlaps(xq, qb, valid_len, 4 * (size_t)B) || overlaps(scale, sb, valid_len, 4 * (size_t)B)))
     return SC_EINVAL;
-  return sc::launch_quant_rows(x, dtype == SC_F32, xq, scale, B, n, K, valid_len, nullptr, 0,
+  return sc::launch_quant_rows(x, dtype == SC_F32, xq, scale, B, n, K, valid_len, nullptr, 1, nullptr, 0,
                                static_cast<hipStream_t>(stream)) == hipSuccess
              ? SC_OK
              : SC_EHIP;
@@ -174,12 +174,12 @@ sc_status linear_impl(const sc_linear_desc* d, const void* x, const float* x_sca
   if (d->x_dtype != SC_I8) {
     LinearWs w;
     carve_linear(d, workspace, &w);
-    if (sc::launch_quant_rows(x, d->x_dtype == SC_F32, w.xq, w.xs, d->B, d->n, d->K, d->valid_len, nullptr, 1, s) !=
-        hipSuccess)
+    if (sc::launch_quant_rows(x, d->x_dtype == SC_F32, w.xq, w.xs, d->B, d->n, d->K, d->valid_len, nullptr, 0, out,
+                              (long long)N * elem_size(d->out_dtype), s) != hipSuccess)
       return SC_EHIP;
+    l.skip_pad = 1;  // they are zero already
     l.xq = w.xq;
     l.xs = w.xs;
-    l.packed = 1;
   }
   return sc::launch_linear_i8(l, s) == hipSuccess ? SC_OK : SC_EHIP;
 }

@@ -152,6 +152,13 @@ SC_DEV void lds_dma16(const void* base, unsigned voff, unsigned lds) {
                : "v"(voff), "s"(base), "s"(lds)
                : "memory", "m0");
 }
+// The same for 4 bytes a lane, at lds + 4 i.
+SC_DEV void lds_dma4(const void* base, unsigned voff, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+               :
+               : "v"(voff), "s"(base), "s"(lds)
+               : "memory", "m0");
+}
 SC_DEV void wait_dma() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Workgroups are dispatched round-robin over the 8 XCDs (each with its own

@@ -176,13 +176,14 @@ hipError_t launch_validate_desc(const int* valid_len, const int* gpos, int B, in
 constexpr int kI8Pitch = 128;
 constexpr int kI8MaxK = 131072;  // 127 x 127 x K fits an int32
 inline int i8_pitch(int K) { return (K + kI8Pitch - 1) / kI8Pitch * kI8Pitch; }
-// packed: row p of xq and scale is the p-th surviving row of x, read through
-// xidx when given; else rows keep their places and padding rows become zeros.
+// Rows keep their places; row j of sequence b is x's row xidx[b, j] when given.
+// zero_pad: padding rows become zeros, else they are left as they are.  zero_out: rows
+// of zero_bytes, of which the padding ones are zeroed, or null.
 hipError_t launch_quant_rows(const void* x, int f32, int8_t* xq, float* scale, int B, int n, int K, const int* len,
-                             const int* xidx, int packed, hipStream_t s);
+                             const int* xidx, int zero_pad, void* zero_out, long long zero_bytes, hipStream_t s);
 hipError_t launch_quant_weight(const void* w, int f32, int8_t* wq, float* scale, int K, int N, hipStream_t s);
 struct Linear {
-  const int8_t* xq;  // [rows, pitch] (packed: the surviving rows; else [B, n, pitch])
+  const int8_t* xq;  // [B, n, pitch]
   const float* xs;
   const int8_t* wq;  // [N, pitch]
   const float* w_scale;
@@ -190,7 +191,7 @@ struct Linear {
   void* out;          // [B, n, N]
   int B, n, K, N;
   const int* len;  // or null
-  int packed, skip_pad, gelu, out_f32;
+  int skip_pad, gelu, out_f32;
 };
 hipError_t launch_linear_i8(const Linear& l, hipStream_t s);
 // The product of few rows from x itself, quantised in the same launch (x_type as

@@ -170,57 +170,82 @@ SC_DEV float quant_long(__amdgpu_buffer_rsrc_t row, int Kp, Dst dst, int lane) {
   return r.scale;
 }
 
-// Rows dealt round-robin over the launch's waves.  packed: row p of the output
-// is the p-th surviving row (pack_seq), read through xidx; else rows keep their
-// places and padding rows become zeros.  The next row's loads are in flight while
-// a row is quantised.
+// Rows of a product's output that are padding: zeroed by the launch that quantises its
+// input, beside its reads.
+struct ZeroRows {
+  char* out;        // or null
+  long long bytes;  // of a row
+  SC_DEV void fill(unsigned row, int lane) const {
+    char* p = out + row * bytes;
+    if (((reinterpret_cast<uintptr_t>(out) | (uintptr_t)bytes) & 15) == 0) {
+      for (long long c = 16 * lane; c < bytes; c += 1024) *reinterpret_cast<uint4*>(p + c) = make_uint4(0, 0, 0, 0);
+    } else {
+      for (long long c = 2 * lane; c < bytes; c += 128) *reinterpret_cast<unsigned short*>(p + c) = 0;
+    }
+  }
+};
+
+// Rows dealt round-robin over the launch's waves; the next row's loads are in flight
+// while a row is quantised.  Row j of sequence b goes to row b n + j, from row xidx[b,
+// j] of the sequence when given.  zero_pad: padding rows become zeros (else they are
+// left as they are).
 template <typename T, bool kVec, int kUnits>
 __global__ __launch_bounds__(256) void k_quant_rows(const T* __restrict__ x, int8_t* __restrict__ xq,
                                                     float* __restrict__ scale, int B, int n, int K, int Kp,
                                                     const int* __restrict__ len, const int* __restrict__ xidx,
-                                                    int packed) {
-  extern __shared__ int pre[];
+                                                    int zero_pad, ZeroRows zero) {
   const int lane = threadIdx.x & 63;
-  unsigned rows = (unsigned)B * (unsigned)n;
-  if (packed && len) {
-    pack_prefix(pre, len, B, n);
-    __syncthreads();
-    rows = __builtin_amdgcn_readfirstlane(pre[B]);
-  }
-  const unsigned step = gridDim.x * 4;
-  auto buffer = [&](unsigned p) {
-    long long from = p;
-    bool live = p < rows;
-    if (live && packed) {
-      if (len) {
-        const int b = __builtin_amdgcn_readfirstlane(pack_seq(pre, B, (int)p));
-        from = (long long)b * n + ((int)p - __builtin_amdgcn_readfirstlane(pre[b]));
-      }
-      if (xidx) from = from / n * n + clampi(scalar_load(xidx, from), 0, n - 1);
-    } else if (live && len) {
-      const unsigned b = p / (unsigned)n;
-      live = (int)(p - b * n) < clampi(scalar_load(len, b), 0, n);
-    }
-    return row_buffer(x + from * K, K, live);
+  const unsigned rows = (unsigned)B * (unsigned)n, step = gridDim.x * 4;
+  // Round k takes place (i + k turn) mod step, as k_norm does.
+  const unsigned turn = (unsigned)(0.382f * (float)step);
+  struct Row {
+    unsigned p;
+    bool exists, live;
+    __amdgpu_buffer_rsrc_t buf;
   };
-  unsigned p = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (p >= rows) return;
+  auto at = [&](unsigned p) {
+    Row r;
+    r.p = p;
+    r.exists = r.live = p < rows;
+    long long from = p;
+    if (r.live && (len || xidx)) {
+      const unsigned b = p / (unsigned)n;
+      if (len) r.live = (int)(p - b * n) < clampi(scalar_load(len, b), 0, n);
+      if (xidx && r.live) from = (long long)b * n + clampi(scalar_load(xidx, p), 0, n - 1);
+    }
+    r.buf = row_buffer(x + from * K, K, r.live);
+    return r;
+  };
+  unsigned place = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), round = 0;
+  auto advance = [&]() {
+    round += step;
+    place = place + turn < step ? place + turn : place + turn - step;
+  };
+  Row cur = at(place);
   if constexpr (kUnits > 0) {
     RowHeld<T, kVec, kUnits> next;
-    next.load(buffer(p), lane);
-    for (; p < rows; p += step) {
+    next.load(cur.buf, lane);
+    while (round < rows) {
+      advance();
       const RowHeld<T, kVec, kUnits> row = next;
-      next.load(buffer(p + step), lane);
-      int8_t* d = xq + (long long)p * Kp;
-      const float s = row.quant(Kp, [&](int c, uint2 v) { *reinterpret_cast<uint2*>(d + c) = v; }, lane);
-      if (lane == 0) scale[p] = s;
+      const Row nrow = at(round + place);
+      next.load(nrow.buf, lane);
+      if (cur.exists && (cur.live || zero_pad)) {
+        int8_t* d = xq + (long long)cur.p * Kp;
+        const float s = row.quant(Kp, [&](int c, uint2 v) { *reinterpret_cast<uint2*>(d + c) = v; }, lane);
+        if (lane == 0) scale[cur.p] = s;
+      }
+      if (zero.out && cur.exists && !cur.live) zero.fill(cur.p, lane);
+      cur = nrow;
     }
   } else {
-    for (; p < rows; p += step) {
-      int8_t* d = xq + (long long)p * Kp;
-      const float s = quant_long<T, kVec>(buffer(p), Kp, [&](int c, uint2 v) { *reinterpret_cast<uint2*>(d + c) = v; },
+    for (; round < rows; advance(), cur = at(round + place)) {
+      if (zero.out && cur.exists && !cur.live) zero.fill(cur.p, lane);
+      if (!cur.exists || (!cur.live && !zero_pad)) continue;
+      int8_t* d = xq + (long long)cur.p * Kp;
+      const float s = quant_long<T, kVec>(cur.buf, Kp, [&](int c, uint2 v) { *reinterpret_cast<uint2*>(d + c) = v; },
                                           lane);
-      if (lane == 0) scale[p] = s;
+      if (lane == 0) scale[cur.p] = s;
     }
   }
 }
@@ -266,7 +291,6 @@ struct LinearArgs {
   void* out;
   int B, n, N, Kp;
   const int* len;
-  int packed;    // xq and xs hold the surviving rows alone, in order
   int skip_pad;  // padding rows of out are left as they are
   int vec;       // rows of out are whole 16-byte units
 };
@@ -336,7 +360,7 @@ SC_DEV i32x4 lds_read_q(unsigned addr) {
 
 // The row numbering (sc_pack.h) with a table of fixed size: the prefix sums of every
 // `per`-th sequence, the rest by a scan of at most per - 1 lengths.
-constexpr int kCoarse = 192;
+constexpr int kCoarse = 512;
 struct Packed {
   const int* pre;  // LDS
   const int* len;
@@ -393,7 +417,7 @@ struct Packed {
 
 // A tile's rows and columns, in LDS.
 struct LinTables {
-  int grow[256], xrow[256];  // row of out and of xq; rows past the last one repeat it
+  int row[256];  // of xq and out; rows past the last one repeat it
   float xs[256], sw[256], sb[256];
 };
 
@@ -435,8 +459,6 @@ struct LinWave {
   unsigned xoff[XL], woff[WL];
   i32x4 acc[FI][FJ];
   i32x4 xf[2][FH], wf[2][FJ];  // the fragments of half a wave's rows, and of its columns, twice
-  int b_gr = 0, b_xr = 0;      // what this thread brings into a tile's tables
-  float b_xs = 0.f, b_sw = 0.f, b_sb = 0.f;
 
   SC_DEV LinWave(const LinearArgs& args, char* stage, const Packed& packed, int rows)
       : a(args), pk(packed), R(rows), tid(threadIdx.x), lane(threadIdx.x & 63),
@@ -444,36 +466,28 @@ struct LinWave {
         wm((w / S::kWgN) * WM), wn((w % S::kWgN) * WN), lds0(lds_addr(stage)), xa(lds0 + q_off(wm + lr, g)),
         wa(lds0 + BM * kBK + q_off(wn + lr, g)) {}
 
-  // Thread tid's row m0 + tid and column n0 + tid of a tile, and their way into its tables.
-  SC_DEV void bring(int m0, int n0) {
-    if (tid < BM) {
-      const int p = min(m0 + tid, R - 1);
-      b_gr = a.len ? pk.row(p) : p;
-      b_xr = a.packed ? p : b_gr;
-      b_xs = a.xs[b_xr];
+  // Fills a tile's tables: rows m0 + tid, columns n0 + tid.  The scales come by direct
+  // loads, in order with the stages': a wait for a stage loaded later covers them.
+  SC_DEV void bring(LinTables& d, int m0, int n0) const {
+    if (w < BM / 64) {
+      const int p = min(m0 + tid, R - 1), row = a.len ? pk.row(p) : p;
+      d.row[tid] = row;
+      lds_dma4(a.xs, 4u * (unsigned)row, lds_addr(&d.xs[64 * w]));
     }
-    if (tid < BN) {
-      const int c = min(n0 + tid, a.N - 1);
-      b_sw = a.ws[c];
-      b_sb = a.bias ? a.bias[c] : 0.f;
-    }
-  }
-  SC_DEV void put(LinTables& d) {
-    if (tid < BM) {
-      d.grow[tid] = b_gr;
-      d.xrow[tid] = b_xr;
-      d.xs[tid] = b_xs;
-    }
-    if (tid < BN) {
-      d.sw[tid] = b_sw;
-      d.sb[tid] = b_sb;
+    if (w < BN / 64) {
+      const unsigned c = 4u * (unsigned)min(n0 + tid, a.N - 1);
+      lds_dma4(a.ws, c, lds_addr(&d.sw[64 * w]));
+      if (a.bias)
+        lds_dma4(a.bias, c, lds_addr(&d.sb[64 * w]));
+      else
+        d.sb[tid] = 0.f;
     }
   }
   SC_DEV void offsets(const LinTables& d, int n0) {
 #pragma unroll
     for (int t = 0; t < XL; ++t) {
       const int R0 = (BM / 8) * w + 8 * t, swz = ((lane >> 4) & 3) | ((R0 >> 1) & 4);
-      xoff[t] = (unsigned)d.xrow[R0 + (lane >> 3)] * (unsigned)a.Kp + 16u * ((lane & 7) ^ swz);
+      xoff[t] = (unsigned)d.row[R0 + (lane >> 3)] * (unsigned)a.Kp + 16u * ((lane & 7) ^ swz);
     }
 #pragma unroll
     for (int t = 0; t < WL; ++t) {
@@ -534,7 +548,7 @@ struct LinWave {
   SC_DEV void emit(const i32x4 (&v)[FI][FJ], const LinTables& d, int n0, int i, int j) const {
     const int r = wm + 16 * i + lr;
     const float xs = d.xs[r];
-    O* row = static_cast<O*>(a.out) + (long long)d.grow[r] * a.N;
+    O* row = static_cast<O*>(a.out) + (long long)d.row[r] * a.N;
     constexpr int kF = FJ == 1 ? 1 : 2;
     unsigned p[kF][2];
 #pragma unroll
@@ -587,8 +601,7 @@ SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const
   bool stored = false;
   int m0, n0, cur = 0;
   sh.template place<W::BM, W::BN>(sh.item, m0, n0);
-  w.bring(m0, n0);
-  w.put(tab[0]);
+  w.bring(tab[0], m0, n0);
   __syncthreads();
   w.offsets(tab[0], n0);
 #pragma unroll
@@ -604,7 +617,8 @@ SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const
       wait_stages<kNBuf, kDma, kStores>(min(ns, kNBuf) - 1);
     else
       wait_stages<kNBuf, kDma>(min(ns, kNBuf) - 1);
-    __syncthreads();
+    __syncthreads();  // and the last tile's results have left its tables
+    if (more) w.bring(tab[cur ^ 1], nm0, nn0);
     int bf = 0;
     w.cols(0, 0, 0);
     w.rows(0, 0, 0);
@@ -633,7 +647,6 @@ SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const
       bf = bn;
     }
     w.rows(1, bf, 0);
-    if (more) w.bring(nm0, nn0);
     w.mul(0, 0);
     w.cols(1, bf, 1);
     w.rows(0, bf, 1);
@@ -642,8 +655,7 @@ SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const
     w.mul(0, 1);
     w.mul(1, 1);
     if (more) {
-      w.put(tab[cur ^ 1]);
-      __syncthreads();  // and every wave has read the last stage
+      __syncthreads();  // every wave has read the last stage
       w.offsets(tab[cur ^ 1], nn0);
 #pragma unroll
       for (int p = 0; p < kNBuf; ++p)
@@ -678,8 +690,7 @@ SC_DEV void linear_stream(const LinearArgs& a, char* stage, LinTables* tab, cons
   int m0, n0, pn0 = 0, bf = 0;
   int tc = 0, tp = 2, tn = 1;  // tables of this tile, the last one and the next one
   sh.template place<W::BM, W::BN>(sh.item, m0, n0);
-  w.bring(m0, n0);
-  w.put(tab[tc]);
+  w.bring(tab[tc], m0, n0);
   __syncthreads();
   w.offsets(tab[tc], n0);
 #pragma unroll
@@ -707,17 +718,15 @@ SC_DEV void linear_stream(const LinearArgs& a, char* stage, LinTables* tab, cons
       w.mul(1, 0);
       w.rows(1, bf, 1);
       w.mul(0, 1);
-      const bool turn = more && s == ns - kNBuf - 1;  // at least one barrier into the tile
-      if (turn) {
-        w.bring(nm0, nn0);
-        w.put(tab[tn]);
-      }
+      const bool turn = more && s == ns - kNBuf - 1;  // not the first stage
       if (more || s + 1 < ns) {
         if (more || s + 2 < ns)
           wait_vm<(kNBuf - 2) * kDma>();
         else
           wait_vm<0>();
         __syncthreads();
+        // a barrier into the tile the results of the one before last have left their tables
+        if (more && s == 0) w.bring(tab[tn], nm0, nn0);
         if (s + kNBuf < ns)
           w.issue(s + kNBuf, bf);
         else if (more)
@@ -810,20 +819,19 @@ hipError_t run_linear(const LinearArgs& a, hipStream_t s) {
 
 template <typename T, bool kVec>
 hipError_t run_quant(const void* x, int8_t* xq, float* scale, int B, int n, int K, int Kp, const int* len,
-                     const int* xidx, int packed, hipStream_t s) {
+                     const int* xidx, int zero_pad, ZeroRows z, hipStream_t s) {
   const long long rows = (long long)B * n;
-  const dim3 grid((unsigned)std::min<long long>((rows + 3) / 4, 4096));
-  const size_t lds = packed && len ? sizeof(int) * (B + 1) : 0;
+  const dim3 grid((unsigned)std::min<long long>((rows + 3) / 4, 2048)), block(256);
   const T* xt = static_cast<const T*>(x);
   if (Kp <= 1024)
-    hipLaunchKernelGGL((k_quant_rows<T, kVec, 2>), grid, dim3(256), lds, s, xt, xq, scale, B, n, K, Kp, len, xidx,
-                       packed);
+    hipLaunchKernelGGL((k_quant_rows<T, kVec, 2>), grid, block, 0, s, xt, xq, scale, B, n, K, Kp, len, xidx, zero_pad,
+                       z);
   else if (Kp <= 4096)
-    hipLaunchKernelGGL((k_quant_rows<T, kVec, 8>), grid, dim3(256), lds, s, xt, xq, scale, B, n, K, Kp, len, xidx,
-                       packed);
+    hipLaunchKernelGGL((k_quant_rows<T, kVec, 8>), grid, block, 0, s, xt, xq, scale, B, n, K, Kp, len, xidx, zero_pad,
+                       z);
   else
-    hipLaunchKernelGGL((k_quant_rows<T, kVec, 0>), grid, dim3(256), lds, s, xt, xq, scale, B, n, K, Kp, len, xidx,
-                       packed);
+    hipLaunchKernelGGL((k_quant_rows<T, kVec, 0>), grid, block, 0, s, xt, xq, scale, B, n, K, Kp, len, xidx, zero_pad,
+                       z);
   return hipGetLastError();
 }
 
@@ -913,14 +921,15 @@ __global__ __launch_bounds__(256) void k_linear_few(LinearArgs a, const T* __res
 }  // namespace
 
 hipError_t launch_quant_rows(const void* x, int f32, int8_t* xq, float* scale, int B, int n, int K, const int* len,
-                             const int* xidx, int packed, hipStream_t s) {
+                             const int* xidx, int zero_pad, void* zero_out, long long zero_bytes, hipStream_t s) {
   const int Kp = i8_pitch(K);
+  const ZeroRows z = {static_cast<char*>(zero_out), zero_bytes};
   const bool vec = K % 8 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
   if (f32)
-    return vec ? run_quant<float, true>(x, xq, scale, B, n, K, Kp, len, xidx, packed, s)
-               : run_quant<float, false>(x, xq, scale, B, n, K, Kp, len, xidx, packed, s);
-  return vec ? run_quant<__bf16, true>(x, xq, scale, B, n, K, Kp, len, xidx, packed, s)
-             : run_quant<__bf16, false>(x, xq, scale, B, n, K, Kp, len, xidx, packed, s);
+    return vec ? run_quant<float, true>(x, xq, scale, B, n, K, Kp, len, xidx, zero_pad, z, s)
+               : run_quant<float, false>(x, xq, scale, B, n, K, Kp, len, xidx, zero_pad, z, s);
+  return vec ? run_quant<__bf16, true>(x, xq, scale, B, n, K, Kp, len, xidx, zero_pad, z, s)
+             : run_quant<__bf16, false>(x, xq, scale, B, n, K, Kp, len, xidx, zero_pad, z, s);
 }
 
 hipError_t launch_quant_weight(const void* w, int f32, int8_t* wq, float* scale, int K, int N, hipStream_t s) {
@@ -948,7 +957,6 @@ LinearArgs linear_args(const Linear& l) {
   a.N = l.N;
   a.Kp = i8_pitch(l.K);
   a.len = l.len;
-  a.packed = l.packed;
   a.skip_pad = l.skip_pad;
   const size_t es = l.out_f32 ? 4 : 2;
   a.vec = (size_t)l.N * es % 16 == 0 && reinterpret_cast<uintptr_t>(l.out) % 16 == 0;
