@@ -78,13 +78,27 @@ SC_DEV __amdgpu_buffer_rsrc_t row_buffer(const T* row, int K, bool live) {
 }
 
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+// Global accesses of 16 and 8 bytes at any element's address (rows of odd length).
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+typedef __attribute__((ext_vector_type(2), aligned(2))) unsigned u32x2_any;
 
-// Eight elements from column c on; zeros at and beyond K.  kVec: K is a multiple of
-// 8 and the row 16-byte aligned.
+// Zeros into n bytes at p (a multiple of 2), by one wavefront.
+SC_DEV void zero_bytes(char* p, long long n, int lane) {
+  for (long long c = 16 * lane; c < n; c += 1024) {
+    if (c + 16 <= n) {
+      *reinterpret_cast<u32x4_any*>(p + c) = u32x4_any{0, 0, 0, 0};
+    } else {
+      for (long long i = c; i < n; i += 2) *reinterpret_cast<unsigned short*>(p + i) = 0;
+    }
+  }
+}
+
+// Eight elements from column c on; zeros at and beyond K.  kVec: rows start at dwords
+// (the hardware checks every dword of an access against the buffer's end).
 template <typename T, bool kVec>
 struct Unit8 {
   static constexpr int kWords = (int)sizeof(T) * 2;
-  unsigned w[kVec || sizeof(T) == 4 ? kWords : 8];
+  unsigned w[kVec ? kWords : 8];
   SC_DEV void load(__amdgpu_buffer_rsrc_t row, int c) {
     if constexpr (kVec) {
 #pragma unroll
@@ -94,13 +108,9 @@ struct Unit8 {
         for (int q = 0; q < 4; ++q) w[4 * i + q] = v[q];
       }
     } else {
+      static_assert(sizeof(T) == 2, "dwords are aligned");
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (sizeof(T) == 4)
-          w[i] = __builtin_amdgcn_raw_buffer_load_b32(row, (c + i) * 4, 0, 0);
-        else
-          w[i] = __builtin_amdgcn_raw_buffer_load_b16(row, (c + i) * 2, 0, 0);
-      }
+      for (int i = 0; i < 8; ++i) w[i] = __builtin_amdgcn_raw_buffer_load_b16(row, (c + i) * 2, 0, 0);
     }
   }
   SC_DEV float at(int i) const {
@@ -175,14 +185,7 @@ SC_DEV float quant_long(__amdgpu_buffer_rsrc_t row, int Kp, Dst dst, int lane) {
 struct ZeroRows {
   char* out;        // or null
   long long bytes;  // of a row
-  SC_DEV void fill(unsigned row, int lane) const {
-    char* p = out + row * bytes;
-    if (((reinterpret_cast<uintptr_t>(out) | (uintptr_t)bytes) & 15) == 0) {
-      for (long long c = 16 * lane; c < bytes; c += 1024) *reinterpret_cast<uint4*>(p + c) = make_uint4(0, 0, 0, 0);
-    } else {
-      for (long long c = 2 * lane; c < bytes; c += 128) *reinterpret_cast<unsigned short*>(p + c) = 0;
-    }
-  }
+  SC_DEV void fill(unsigned row, int lane) const { zero_bytes(out + row * bytes, bytes, lane); }
 };
 
 // Rows dealt round-robin over the launch's waves; the next row's loads are in flight
@@ -292,7 +295,6 @@ struct LinearArgs {
   int B, n, N, Kp;
   const int* len;
   int skip_pad;  // padding rows of out are left as they are
-  int vec;       // rows of out are whole 16-byte units
 };
 
 constexpr int kBK = 128;        // bytes of a row per K stage: whole lines (64-byte pieces halve the loads' rate)
@@ -529,15 +531,20 @@ struct LinWave {
   }
   static SC_DEV int next_buf(int bf) { return bf == kNBuf - 1 ? 0 : bf + 1; }
 
-  SC_DEV void store16(O* row, int col, uint4 v) const {  // 16 bytes of a row at column col
+  // 16 bytes of a row at column col, at any element's address: element by element, rows of
+  // odd length took 32768 x 1024 x 4095 from 290 to 396 us, 24165 x 768 x 1111 from 57 to
+  // 96, for 32768 x 1024 x 4096 with GELU 190 against 196 (registers).  The barrier keeps
+  // the compiler from running several fragments' results ahead.
+  SC_DEV void store16(O* row, int col, uint4 v) const {
     constexpr int kE = 16 / sizeof(O);
+    __builtin_amdgcn_sched_barrier(0);
     if (col >= a.N) return;
-    if (a.vec) {
-      *reinterpret_cast<uint4*>(row + col) = v;
+    if (col + kE <= a.N) {
+      *reinterpret_cast<u32x4_any*>(row + col) = __builtin_bit_cast(u32x4_any, v);
     } else {
       const O* e = reinterpret_cast<const O*>(&v);
 #pragma unroll
-      for (int q = 0; q < kE; ++q)
+      for (int q = 0; q < kE - 1; ++q)
         if (col + q < a.N) row[col + q] = e[q];
     }
   }
@@ -547,6 +554,7 @@ struct LinWave {
   // leaves it with 16 bytes of one, and every group of four lanes with 64 bytes of a row.
   SC_DEV void emit(const i32x4 (&v)[FI][FJ], const LinTables& d, int n0, int i, int j) const {
     const int r = wm + 16 * i + lr;
+    __builtin_amdgcn_sched_barrier(0);
     const float xs = d.xs[r];
     O* row = static_cast<O*>(a.out) + (long long)d.row[r] * a.N;
     constexpr int kF = FJ == 1 ? 1 : 2;
@@ -572,15 +580,13 @@ struct LinWave {
               make_uint4((unsigned)lo[0], (unsigned)hi[0], (unsigned)lo[1], (unsigned)hi[1]));
     } else if constexpr (sizeof(O) == 2) {
       const int col = n0 + wn + 16 * j + 4 * g;
-      if (col < a.N) {
-        if (a.vec) {
-          *reinterpret_cast<uint2*>(row + col) = make_uint2(p[0][0], p[0][1]);
-        } else {
-          const O* e = reinterpret_cast<const O*>(p[0]);
+      if (col + 4 <= a.N) {
+        *reinterpret_cast<u32x2_any*>(row + col) = u32x2_any{p[0][0], p[0][1]};
+      } else {
+        const O* e = reinterpret_cast<const O*>(p[0]);
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (col + q < a.N) row[col + q] = e[q];
-        }
+        for (int q = 0; q < 3; ++q)
+          if (col + q < a.N) row[col + q] = e[q];
       }
     }
   }
@@ -665,7 +671,7 @@ SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const
     for (int i = 0; i < W::FI; ++i)
 #pragma unroll
       for (int j = 0; j < W::FJ; j += 2) w.emit(w.acc, tab[cur], n0, i, j);
-    stored = a.vec && n0 + W::BN <= a.N;  // a whole tile: exactly kStores of them, every lane's
+    stored = n0 + W::BN <= a.N;  // a whole tile: exactly kStores of them, every lane's
     if (!more) return;
     sh.item = nitem;
     n0 = nn0;
@@ -801,13 +807,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   const long long lo = P * blockIdx.x / gridDim.x, end = P * (blockIdx.x + 1) / gridDim.x;
   const int lane = threadIdx.x & 63;
   for (long long q = lo + (threadIdx.x >> 6); q < end; q += 8) {
-    O* o = static_cast<O*>(a.out) + pk.pad_row(q) * a.N;
-    if (a.vec) {
-      for (int c = lane; c < a.N / (16 / (int)sizeof(O)); c += 64)
-        reinterpret_cast<uint4*>(o)[c] = make_uint4(0, 0, 0, 0);
-    } else {
-      for (int c = lane; c < a.N; c += 64) o[c] = (O)0.f;
-    }
+    zero_bytes(reinterpret_cast<char*>(static_cast<O*>(a.out) + pk.pad_row(q) * a.N), a.N * (long long)sizeof(O), lane);
   }
 }
 
@@ -924,10 +924,8 @@ hipError_t launch_quant_rows(const void* x, int f32, int8_t* xq, float* scale, i
                              const int* xidx, int zero_pad, void* zero_out, long long zero_bytes, hipStream_t s) {
   const int Kp = i8_pitch(K);
   const ZeroRows z = {static_cast<char*>(zero_out), zero_bytes};
-  const bool vec = K % 8 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
-  if (f32)
-    return vec ? run_quant<float, true>(x, xq, scale, B, n, K, Kp, len, xidx, zero_pad, z, s)
-               : run_quant<float, false>(x, xq, scale, B, n, K, Kp, len, xidx, zero_pad, z, s);
+  const bool vec = K % 2 == 0 && reinterpret_cast<uintptr_t>(x) % 4 == 0;
+  if (f32) return run_quant<float, true>(x, xq, scale, B, n, K, Kp, len, xidx, zero_pad, z, s);
   return vec ? run_quant<__bf16, true>(x, xq, scale, B, n, K, Kp, len, xidx, zero_pad, z, s)
              : run_quant<__bf16, false>(x, xq, scale, B, n, K, Kp, len, xidx, zero_pad, z, s);
 }
@@ -958,8 +956,6 @@ LinearArgs linear_args(const Linear& l) {
   a.Kp = i8_pitch(l.K);
   a.len = l.len;
   a.skip_pad = l.skip_pad;
-  const size_t es = l.out_f32 ? 4 : 2;
-  a.vec = (size_t)l.N * es % 16 == 0 && reinterpret_cast<uintptr_t>(l.out) % 16 == 0;
   return a;
 }
 
@@ -993,9 +989,9 @@ bool linear_few_ok(long long rows, int K, int N) {
 }
 
 hipError_t launch_linear_few(const Linear& l, const void* x, int x_type, hipStream_t s) {
-  const bool vec = l.K % 8 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
+  const bool vec = l.K % 2 == 0 && reinterpret_cast<uintptr_t>(x) % 4 == 0;
   if (x_type == 2) return run_few<int8_t, true>(l, x, s);
-  if (x_type == 0) return vec ? run_few<float, true>(l, x, s) : run_few<float, false>(l, x, s);
+  if (x_type == 0) return run_few<float, true>(l, x, s);
   return vec ? run_few<__bf16, true>(l, x, s) : run_few<__bf16, false>(l, x, s);
 }
 

@@ -125,7 +125,9 @@ struct Bits<__bf16, 1> {
 
 // One row of a tensor as a buffer of its D elements: accesses beyond it load zeros
 // and store nothing, so the channels past D need no branch, nor does an absent
-// tensor (a buffer of no elements).  With a branch around each access the compiler
+// tensor (a buffer of no elements).  The hardware checks every dword of an access, and
+// needs no more than dword alignment, so rows that end inside an access are fine.
+// With a branch around each access the compiler
 // waited for every load on its own (backward of 32768 x 1024: 229 us).
 template <typename T>
 SC_DEV __amdgpu_buffer_rsrc_t row_buffer(const T* base, long long row, int D, bool present) {
@@ -142,7 +144,7 @@ struct Cols {
   static constexpr int kWidth = kVec * kPer * kTpr, kPerThread = kPer;
   int D, t;  // t: thread of the row
   SC_DEV int at(int u) const { return (u * kTpr + t) * kVec; }
-  SC_DEV bool in(int u) const { return at(u) < D; }
+  SC_DEV bool in(int u, int q) const { return at(u) + q < D; }
   SC_DEV void load(__amdgpu_buffer_rsrc_t r, Raw (&v)[kPer]) const {
 #pragma unroll
     for (int u = 0; u < kPer; ++u) v[u] = B::load(r, at(u) * (int)sizeof(T));
@@ -213,7 +215,7 @@ SC_DEV void stage_weights(float* lds, const Norm& a, int count) {
       C::B::unpack(raw[m][u], v);
 #pragma unroll
       for (int q = 0; q < kVec; ++q)
-        lds[k * C::kWidth + c.at(u) + q] = have || !c.in(u) ? v[q] : absent;
+        lds[k * C::kWidth + c.at(u) + q] = have || !c.in(u, q) ? v[q] : absent;
     }
   }
   __syncthreads();
@@ -230,11 +232,9 @@ SC_DEV float normalise(float (&v)[E], const C& c, R& red, bool rms, float eps, f
     for (int i = 0; i < E; ++i) s += v[i];
     const float mean = red.sum(s) / fd;  // divided: a constant row has no deviation
 #pragma unroll
-    for (int u = 0; u < kPer; ++u) {
-      const float m = c.in(u) ? mean : 0.f;
+    for (int u = 0; u < kPer; ++u)
 #pragma unroll
-      for (int q = 0; q < kVec; ++q) v[u * kVec + q] -= m;
-    }
+      for (int q = 0; q < kVec; ++q) v[u * kVec + q] -= c.in(u, q) ? mean : 0.f;
   }
   float s = 0.f;
 #pragma unroll
@@ -644,11 +644,11 @@ struct NormShape {
   static constexpr int kVec = kV, kPer = kP, kTpr = kT;
 };
 
-// Calls f with the shape for D: a wavefront per row up to 1024 channels (256 where
-// rows are not aligned), a workgroup beyond.
-template <typename F>
+// Calls f with the shape for D: a wavefront per row up to 1024 channels (256 for bf16
+// rows of odd length or address, an element an access), a workgroup beyond.
+template <typename T, typename F>
 hipError_t norm_shape(int D, bool vec, F&& f) {
-  if (vec) {
+  if (sizeof(T) == 4 || vec) {
     if (D <= 256) return f(NormShape<4, 1, 64>{});
     if (D <= 512) return f(NormShape<4, 2, 64>{});
     if (D <= 768) return f(NormShape<4, 3, 64>{});
@@ -656,28 +656,29 @@ hipError_t norm_shape(int D, bool vec, F&& f) {
     if (D <= 2048) return f(NormShape<4, 2, 256>{});
     return f(NormShape<4, 2, 512>{});
   }
-  if (D <= 256) return f(NormShape<1, 4, 64>{});
-  if (D <= 1024) return f(NormShape<1, 4, 256>{});
-  if (D <= 2048) return f(NormShape<1, 8, 256>{});
-  return f(NormShape<1, 8, 512>{});
+  if constexpr (sizeof(T) == 2) {
+    if (D <= 256) return f(NormShape<1, 4, 64>{});
+    if (D <= 1024) return f(NormShape<1, 4, 256>{});
+    if (D <= 2048) return f(NormShape<1, 8, 256>{});
+    return f(NormShape<1, 8, 512>{});
+  }
+  return hipErrorInvalidValue;  // not reached
 }
 
-// Every row of every tensor starts at a multiple of an access of four.
+// Rows of four elements an access: every row of every tensor starts at a dword.
+// (yq is 16-byte aligned.)
 bool norm_vec(const Norm& a) {
-  const uintptr_t e = a.f32 ? 16 : 8;
+  if (a.f32) return true;
   uintptr_t all = 0;
   for (const void* p : {a.x, a.t, (const void*)a.r, (const void*)a.y, a.dr, a.dy, (const void*)a.dx, (const void*)a.dt})
-    all |= reinterpret_cast<uintptr_t>(p) & (e - 1);
-  for (const float* p : {a.post_w, a.post_b, a.pre_w, a.pre_b}) all |= reinterpret_cast<uintptr_t>(p) & 15;
-  for (const void* p : {a.gate, (const void*)a.dgate})
-    all |= reinterpret_cast<uintptr_t>(p) & (a.gate_mode == kGateChannel ? 15 : e - 1);
-  all |= reinterpret_cast<uintptr_t>(a.yq) & 3;
-  return a.D % 4 == 0 && all == 0;
+    all |= reinterpret_cast<uintptr_t>(p) & 3;
+  if (a.gate_mode != kGateChannel) all |= (reinterpret_cast<uintptr_t>(a.gate) | reinterpret_cast<uintptr_t>(a.dgate)) & 3;
+  return a.D % 2 == 0 && all == 0;
 }
 
 template <typename T>
 hipError_t run_norm(const Norm& a, hipStream_t s) {
-  return norm_shape(a.D, norm_vec(a), [&](auto shape) {
+  return norm_shape<T>(a.D, norm_vec(a), [&](auto shape) {
     using S = decltype(shape);
     constexpr int kT = kThreads<S::kTpr>;
     const long long rows = (long long)a.B * a.n, per = kT / S::kTpr;
@@ -689,7 +690,7 @@ hipError_t run_norm(const Norm& a, hipStream_t s) {
 
 template <typename T>
 hipError_t run_norm_backward(const Norm& a, hipStream_t s) {
-  return norm_shape(a.D, norm_vec(a), [&](auto shape) {
+  return norm_shape<T>(a.D, norm_vec(a), [&](auto shape) {
     using S = decltype(shape);
     constexpr int kT = kThreads<S::kTpr>, kRows = kT / S::kTpr;
     const bool seq = a.gate_mode == kGateSequence && a.dgate;
