@@ -23,7 +23,8 @@
  * (device int32 [B]; values outside are clamped), or n without valid_len
  * (NULL).  Output rows of padding are zero, and padding rows of inputs are not
  * read into any result.  Every result is deterministic, and a row's result
- * depends neither on the other rows nor on the batch.
+ * depends neither on the other rows nor on the batch.  Tensors are aligned to
+ * their elements, 8-bit rows and workspaces to 16 bytes.
  */
 #ifndef SC_BLOCK_H_
 #define SC_BLOCK_H_
@@ -53,7 +54,7 @@ int64_t sc_i8_pitch(int64_t K);
  *   xq     int8 [B, n, sc_i8_pitch(K)];  scale  float32 [B, n].
  *   Padding rows: zeros, scale 0.
  * Errors: SC_EINVAL (null or overlapping buffers, sizes below 1, dtype, xq not
- * 16-byte aligned), SC_EUNSUPPORTED (B n >= 2^31).
+ * 16-byte aligned), SC_EUNSUPPORTED (B n >= 2^31, K >= 2^29).
  */
 sc_status sc_quantize_rows_i8(int32_t B, int32_t n, int32_t K, const int32_t *valid_len, int32_t dtype,
                               const void *x, int8_t *xq, float *scale, void *stream);
@@ -84,7 +85,8 @@ size_t sc_linear_i8_workspace_size(const sc_linear_desc *desc);
 /*
  * out[b,j,:] = act(x_scale[b,j] * w_scale[:] * (xq[b,j,:] . wq[:,:]^T) + bias[:])
  * for j < valid_len[b], 0 for the padding rows.  The sum of products is exact
- * (int32; K <= 131072), everything after it float32, rounded once to out_dtype.
+ * (int32; K <= 131072, integers from -127 to 127), everything after it float32,
+ * rounded once to out_dtype.
  *   x        SC_I8: the 8-bit rows [B, n, sc_i8_pitch(K)] (16-byte aligned), with
  *            x_scale float32 [B, n].  SC_F32, SC_BF16: [B, n, K], quantised in
  *            the call as by sc_quantize_rows_i8; x_scale must be NULL.
@@ -197,8 +199,10 @@ size_t sc_encoder_stack_i8_workspace_size(const sc_attn_desc *desc, int32_t n_la
  *   h   = bf16(GELU(lin(w1, x1)))
  *   x   = bf16(LayerNorm(res_scale x1 + gate2 * bf16(lin(w2, h))) ln2_w + ln2_b)
  *   layers  HOST array of n_layers; ffn_dim >= 1; res_scale finite.
- * Every other argument and error as for sc_encoder_stack; x_out rows at or
- * beyond final_len are left untouched, as there.
+ * bf16, not causal, D = H d <= 2048, ffn_dim <= 131072, B <= 8192 and n D <
+ * 2^32 / 6, and the limits of sc_linear_i8 for every product, or
+ * SC_EUNSUPPORTED.  Every other argument and error as for sc_encoder_stack;
+ * x_out rows at or beyond final_len are left untouched, as there.
  */
 sc_status sc_encoder_stack_i8(const sc_attn_desc *desc, int32_t n_layers, const int32_t *windows, const void *x_in,
                               const sc_layer_i8 *layers, int32_t ffn_dim, const float *thresholds,

@@ -779,6 +779,7 @@ sc_status run_stack_i8(const sc_attn_desc* d, int32_t n_layers, const int32_t* w
   }
   const size_t need = carve_stack(d, F, true, nullptr, nullptr);
   if (!workspace || ws_bytes < need) return SC_EWORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return SC_EINVAL;  // it holds 8-bit rows
   const size_t bn = (size_t)d->B * d->n, xb = bn * d->H * d->d * 2;
   if (overlaps(x_out, xb, x_in, xb) || overlaps(x_out, xb, workspace, need) || overlaps(x_in, xb, workspace, need))
     return SC_EINVAL;

@@ -127,6 +127,7 @@ sc_status quantize_rows_impl(int32_t B, int32_t n, int32_t K, const int32_t* val
   if (K < 1 || K > INT32_MAX - sc::kI8Pitch || !float_type(dtype) || !x || !xq || !scale) return SC_EINVAL;
   const sc_status st = check_rows(B, n);
   if (st != SC_OK) return st;
+  if (K >= 1 << 29) return SC_EUNSUPPORTED;  // 32-bit byte offsets inside a row
   const size_t rows = (size_t)B * n, xb = rows * K * elem_size(dtype), qb = rows * sc::i8_pitch(K), sb = rows * 4;
   if (!aligned(xq, 16)) return SC_EINVAL;
   if (overlaps(xq, qb, x, xb) || overlaps(scale, sb, x, xb) || overlaps(xq, qb, scale, sb)) return SC_EINVAL;
@@ -147,6 +148,7 @@ sc_status linear_impl(const sc_linear_desc* d, const void* x, const float* x_sca
   if (!aligned(wq, 16) || (d->x_dtype == SC_I8 && !aligned(x, 16))) return SC_EINVAL;
   const size_t need = carve_linear(d, nullptr, nullptr);
   if (need > 0 && (!workspace || ws_bytes < need)) return SC_EWORKSPACE;
+  if (need > 0 && !aligned(workspace, 16)) return SC_EINVAL;  // it holds 8-bit rows
   const size_t rows = (size_t)d->B * d->n, pitch = sc::i8_pitch(d->K), N = d->N;
   const Span in_x{x, d->x_dtype == SC_I8 ? rows * pitch : rows * d->K * elem_size(d->x_dtype)};
   const Span o{out, rows * N * elem_size(d->out_dtype)}, ws{workspace, need};

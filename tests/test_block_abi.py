@@ -215,3 +215,19 @@ def test_stack_i8_refusals():
     assert need > 0 and sc.sc_encoder_stack_i8_workspace_size(stack_desc(), 1, 0) == 0
     assert call(work=None) == B.SC_EWORKSPACE
     assert call(wb=need - 1) == B.SC_EWORKSPACE
+
+
+def test_workspace_alignment_and_long_rows_refused():
+    """Workspaces that 8-bit rows lie in start at 16 bytes; rows whose byte offsets pass 32 bits are not quantised."""
+    L = sc.load()
+    d = sc.LinearDesc(2, 800, 100, 64)
+    for off, want in ((4, B.SC_EINVAL), (8, B.SC_EINVAL)):
+        assert L.sc_linear_i8(ctypes.byref(d.c()), A[0], None, A[1], A[2], None, A[3], A[4] + off, 1 << 30,
+                              None) == want, off
+        arr = (B._LayerI8 * 1)(layer_i8())
+        assert L.sc_encoder_stack_i8(ctypes.byref(stack_desc().c()), 1, None, A[1], arr, 64, (ctypes.c_float * 1)(0.0),
+                                     1, ctypes.c_float(1e-5), ctypes.c_float(1.0), A[4], A[5], None, None, A[6] + off,
+                                     1 << 32, None) == want, off
+    for K in (1 << 29, (1 << 31) - 129):
+        for dt in (sc.SC_F32, sc.SC_BF16):
+            assert L.sc_quantize_rows_i8(1, 1, K, None, dt, A[0], A[8], A[16], None) == B.SC_EUNSUPPORTED, (K, dt)
