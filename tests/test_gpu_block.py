@@ -50,7 +50,7 @@ def off_by_one(t):
 
 
 def assert_close(got, want, tol, what):
-    got = got.double().cpu()
+    got = got.double().to(want.device)
     assert got.shape == want.shape, what
     bad = ~((got - want).abs() <= tol)
     assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} off, worst " \
@@ -150,12 +150,13 @@ def linear_case(B, n, K, N, lens, x_type, bias, seed):
 
 
 def linear_reference(x, L, wq, ws, bias, K, gelu, out_type):
-    """(outputs, tolerance) in float64."""
+    """(outputs, tolerance) in float64, on x's device."""
     B, n, _ = x.shape
-    m = valid_mask(L, n)
+    m = valid_mask(L, n).to(x.device)
+    wq, ws, bias = wq.to(x.device), ws.to(x.device), None if bias is None else bias.to(x.device)
     q, s = exact_quant(torch.where(m[..., None], x.float(), 0.0))
-    acc = q @ wq[:, :K].double().cpu().t()
-    p = acc * s.double()[..., None] * ws.double().cpu()
+    acc = (q.reshape(B * n, K) @ wq[:, :K].double().t()).reshape(B, n, -1)
+    p = acc * s.double()[..., None] * ws.double()
     v = p if bias is None else p + bias.double()
     tol = 3 * U * p.abs() + U * v.abs()
     if gelu:
@@ -170,8 +171,7 @@ def linear_reference(x, L, wq, ws, bias, K, gelu, out_type):
     else:
         out = v
     tol = tol + TYPES[out_type][2] * (out.abs() + tol) + 1e-44
-    zero = torch.zeros((), dtype=torch.float64)
-    return torch.where(m[..., None], out, zero), torch.where(m[..., None], tol, zero)
+    return torch.where(m[..., None], out, 0.0), torch.where(m[..., None], tol, 0.0)
 
 
 LINEAR = [
@@ -214,6 +214,54 @@ def test_linear(case):
     again = sc.sc_linear_i8(d, xd if x_type == "i8" else off_by_one(xd), wq, off_by_one(ws),
                             bias=None if b is None else off_by_one(b), x_scale=xs, out=off_by_one(out.clone()))
     assert torch.equal(again, out)
+
+
+# Several tiles a workgroup, and every form of them: tiles of 256 x 128 with 5, 6 and 9 stages (fewer and more than a
+# tile has parts of results), of 256 x 256 and of 128 x 128; sequences by the thousand.
+LINEAR_MANY = [
+    (5, 6600, 640, 300, None, "bf16", "bf16", True, True),
+    (4, 8250, 640, 770, (8250, 8249, 0, 8000), "bf16", "bf16", False, True),
+    (1, 20000, 768, 769, None, "f32", "f32", False, True),
+    (3, 11000, 1100, 304, (11000, 10990, 10500), "i8", "bf16", True, False),
+    (3, 11000, 130, 1030, (11000, 10990, 10500), "i8", "bf16", True, True),
+    (2, 16500, 257, 520, None, "bf16", "f32", False, False),
+    (2, 10000, 768, 1153, (10000, 9999), "bf16", "bf16", False, True),
+    (1, 33000, 257, 300, None, "f32", "f32", True, True),
+    (1500, 2, 300, 136, (2, 0, 1), "bf16", "bf16", False, True),
+    (8192, 1, 64, 200, (1, 0, 0, 1, 1), "f32", "bf16", True, True),
+    (5000, 7, 200, 333, (7, 0, 3, 1, 6, 7, 2), "i8", "f32", False, True),
+    (1025, 40, 128, 72, (40, 17, 0, 39), "i8", "bf16", False, False),
+]
+
+
+@pytest.mark.parametrize("case", LINEAR_MANY, ids=lambda c: "-".join(str(v) for v in c[:4]) + f"-{c[5]}-{c[6]}")
+def test_linear_many_rows(case):
+    B, n, K, N, lens, x_type, out_type, gelu, has_bias = case
+    L_dev, L, x, wq, ws, bias = linear_case(B, n, K, N, lens, x_type, has_bias, seed=B * n + K)
+    d = sc.LinearDesc(B, n, K, N, valid_len=L_dev, out_dtype=TYPES[out_type][1],
+                      x_dtype=sc.SC_I8 if x_type == "i8" else TYPES[x_type][1],
+                      act=sc.SC_ACT_GELU if gelu else sc.SC_ACT_NONE)
+    xd, b, xs = x.to(DEV), None if bias is None else bias.to(DEV), None
+    want, tol = linear_reference(xd, L, wq, ws, b, K, gelu, out_type)
+    if x_type == "i8":
+        xd, xs = sc.sc_quantize_rows_i8(xd)
+    out = torch.full((B, n, N), float("nan"), dtype=TYPES[out_type][0], device=DEV)
+    sc.sc_linear_i8(d, xd, wq, ws, bias=b, x_scale=xs, out=out)
+    assert_close(out, want, tol, "out")
+
+
+def test_linear_offsets_past_32_bits():
+    """2.2e9 outputs: the last rows are those of a call of their own; padding behind them is zero."""
+    B, n, K, N = 2, 500000, 64, 2200
+    x = torch.randn((B, n, K), generator=gen(1)).to(torch.bfloat16).to(DEV)
+    wq, ws = sc.sc_quantize_weight_i8(torch.randn((K, N), generator=gen(2)).to(DEV))
+    lens = torch.tensor([n, n - 50], dtype=torch.int32, device=DEV)
+    out = sc.sc_linear_i8(sc.LinearDesc(B, n, K, N, valid_len=lens), x, wq, ws)
+    for lo, hi in ((0, 70), (n - 90, n)):
+        for b in range(B):
+            part = sc.sc_linear_i8(sc.LinearDesc(1, hi - lo, K, N), x[b:b + 1, lo:hi].contiguous(), wq, ws)[0]
+            part[max(0, int(lens[b]) - lo):] = 0
+            assert torch.equal(out[b, lo:hi], part), (b, lo)
 
 
 @pytest.mark.parametrize("x_type", ["bf16", "i8"])
@@ -524,6 +572,26 @@ def test_norm_backward(case):
     odd = {k: None if v is None else off_by_one(v) for k, v in a.items()}
     check_grads(sc.sc_block_norm_backward(d, **odd, dr=off_by_one(gr), dy=off_by_one(gy) if d.pre else None), want,
                 case, "odd addresses")
+
+
+def test_norm_offsets_past_32_bits():
+    """2.2e9 elements, forward and backward, and 8-bit rows of them: the last rows are those of a call of their own."""
+    n, D, last = 2150000, 1024, 9
+    x, t = (torch.empty((1, n, D), dtype=torch.bfloat16, device=DEV).normal_() for _ in range(2))
+    w = torch.linspace(0.5, 1.5, D, device=DEV)
+
+    def run(xx, tt):
+        d = sc.NormDesc(1, xx.shape[1], D, post=True, gate=sc.SC_GATE_CHANNEL)
+        a = dict(gate=w, post_w=w, pre_w=w)
+        r, y = sc.sc_block_norm(d, xx, tt, **a)[:2]
+        dx, dt = torch.empty_like(xx), torch.empty_like(tt)
+        sc.sc_block_norm_backward(d, xx, tt, dr=r, dy=y, grads=dict(dx=dx, dt=dt), **a)
+        return r[:, -last:].clone(), y[:, -last:].clone(), dx[:, -last:].clone(), dt[:, -last:].clone()
+    whole, part = run(x, t), run(x[:, -last:].contiguous(), t[:, -last:].contiguous())
+    for a, b in zip(whole, part):
+        assert torch.equal(a, b)
+    for a, b in zip(sc.sc_quantize_rows_i8(x), sc.sc_quantize_rows_i8(x[:, -last:].contiguous())):
+        assert torch.equal(a[:, -last:], b)
 
 
 @pytest.mark.parametrize("kind", ["layer", "rms"])
