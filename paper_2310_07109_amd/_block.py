@@ -253,7 +253,7 @@ def sc_block_norm_backward(desc: NormDesc, x, t=None, gate=None, post_w=None, po
             g = None
             outs.append(None)
         else:
-            g = call.new(ty, s)
+            g = torch.empty_like(src)  # of that type and shape
             outs.append(g.data_ptr())
         out[nm] = g
     cd = ctypes.byref(desc.c())

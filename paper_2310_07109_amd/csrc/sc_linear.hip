@@ -806,9 +806,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   const long long P = (long long)a.B * a.n - R;
   const long long lo = P * blockIdx.x / gridDim.x, end = P * (blockIdx.x + 1) / gridDim.x;
   const int lane = threadIdx.x & 63;
-  for (long long q = lo + (threadIdx.x >> 6); q < end; q += 8) {
-    zero_bytes(reinterpret_cast<char*>(static_cast<O*>(a.out) + pk.pad_row(q) * a.N), a.N * (long long)sizeof(O), lane);
-  }
+  const long long bytes = a.N * (long long)sizeof(O);
+  for (long long q = lo + (threadIdx.x >> 6); q < end; q += 8)
+    zero_bytes(static_cast<char*>(a.out) + pk.pad_row(q) * bytes, bytes, lane);
 }
 
 template <typename O, bool kGelu>
@@ -913,7 +913,6 @@ __global__ __launch_bounds__(256) void k_linear_few(LinearArgs a, const T* __res
   if (m >= rows || col >= a.N) return;
   const int sum = red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid];
   const bool on = live(m);
-  if (!on && a.skip_pad) return;
   const float v = on ? finish<sizeof(O) == 4, kGelu>(sum, ss[r], a.ws[col], a.bias ? a.bias[col] : 0.f) : 0.f;
   store_out(static_cast<O*>(a.out) + m * a.N + col, v);
 }
@@ -921,9 +920,9 @@ __global__ __launch_bounds__(256) void k_linear_few(LinearArgs a, const T* __res
 }  // namespace
 
 hipError_t launch_quant_rows(const void* x, int f32, int8_t* xq, float* scale, int B, int n, int K, const int* len,
-                             const int* xidx, int zero_pad, void* zero_out, long long zero_bytes, hipStream_t s) {
+                             const int* xidx, int zero_pad, void* zero_out, long long zero_row, hipStream_t s) {
   const int Kp = i8_pitch(K);
-  const ZeroRows z = {static_cast<char*>(zero_out), zero_bytes};
+  const ZeroRows z = {static_cast<char*>(zero_out), zero_row};
   const bool vec = K % 2 == 0 && reinterpret_cast<uintptr_t>(x) % 4 == 0;
   if (f32) return run_quant<float, true>(x, xq, scale, B, n, K, Kp, len, xidx, zero_pad, z, s);
   return vec ? run_quant<__bf16, true>(x, xq, scale, B, n, K, Kp, len, xidx, zero_pad, z, s)

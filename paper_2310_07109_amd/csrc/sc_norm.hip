@@ -103,14 +103,10 @@ struct Bits<__bf16, 4> {
   SC_DEV static Raw pack(const float* f) { return Raw{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])}; }
 };
 template <>
-struct Bits<float, 1> {
+struct Bits<float, 1> {  // weights, beside bf16 rows an element an access
   using Raw = unsigned;
   SC_DEV static Raw load(__amdgpu_buffer_rsrc_t r, int off) { return __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0); }
-  SC_DEV static void store(__amdgpu_buffer_rsrc_t r, int off, Raw v) {
-    __builtin_amdgcn_raw_buffer_store_b32(v, r, off, 0, 0);
-  }
   SC_DEV static void unpack(Raw v, float* f) { *f = __builtin_bit_cast(float, v); }
-  SC_DEV static Raw pack(const float* f) { return __builtin_bit_cast(unsigned, *f); }
 };
 template <>
 struct Bits<__bf16, 1> {
@@ -127,8 +123,8 @@ struct Bits<__bf16, 1> {
 // and store nothing, so the channels past D need no branch, nor does an absent
 // tensor (a buffer of no elements).  The hardware checks every dword of an access, and
 // needs no more than dword alignment, so rows that end inside an access are fine.
-// With a branch around each access the compiler
-// waited for every load on its own (backward of 32768 x 1024: 229 us).
+// With a branch around each access the compiler waited for every load on its own
+// (backward of 32768 x 1024: 229 us).
 template <typename T>
 SC_DEV __amdgpu_buffer_rsrc_t row_buffer(const T* base, long long row, int D, bool present) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base) + row * D, 0, present ? D * (int)sizeof(T) : 0,
