@@ -302,13 +302,15 @@ constexpr int kLinWgs = 256;    // one workgroup per CU, each taking tiles in tu
 constexpr int kLinLds = 147456; // stage buffers: 3 x 48, 4 x 32 or 8 x 16 KB
 constexpr int kLinModes = 4;
 constexpr int kGroupM = 8;
-// k_linear_few: at most kFewRows rows of kFewK bytes, kFewWgs workgroups and
-// kFewWork bytes of rows over all of them.  us in a graph, bf16 rows, this kernel and
-// the two launches of the others: K 512 N 1536 1 row 3.9 and 6.5, 128 rows 6.0 and
-// 7.4, 256 rows 8.6 and 7.5; K 768 N 2304 64 rows 6.6 and 8.3, 128 rows 8.7 and 8.2;
-// K 1024 N 4096 64 rows 7.9 and 9.0, 128 rows 12.6 and 9.1; K 4096 N 1024 1 row 9.3
-// and 17.1, 128 rows 13.8 and 18.8, 256 rows 23.8 and 19.3.  8-bit rows alike.
-constexpr int kFewRows = 512, kFewK = 4096, kFewWgs = 1024, kFewWork = 5 << 19;
+// k_linear_few: at most kFewRows rows of kFewK bytes, and at most the workgroups that the
+// CUs hold at once: four a CU up to 1024 bytes a row, two beyond (70 KB of LDS).  us in a
+// graph, bf16 rows, this kernel and the two launches of the others: K 512 N 2048 1 row
+// 4.1 and 7.1, 128 rows (1024 workgroups) 7.0 and 8.1, 192 rows 8.7 and 8.2; K 1024 N
+// 4096 64 rows (1024) 8.2 and 9.5, 96 rows 10.2 and 9.4; K 2304 N 768 64 rows 8.6 and
+// 12.2, 128 rows (384) 11.8 and 12.4, 192 rows (576) 16.1 and 12.7; K 4096 N 1024 1 row
+// 9.5 and 15.3, 128 rows (512) 13.9 and 16.5, 192 rows 19.4 and 16.8.  8-bit rows alike
+// (K 1024 N 4096 64 rows 5.4 and 6.8, K 2304 N 768 192 rows 12.1 and 9.2).
+constexpr int kFewRows = 512, kFewK = 4096;
 
 // Tile shapes: BM x BN, waves along M and N, stage buffers.
 template <int kM>
@@ -328,8 +330,9 @@ struct LinPlan {
 constexpr int kStreamMin = 5;  // stages that linear_stream needs: its buffers and two
 // The mode with the least rounds of workgroups times the cost of a tile: of a stage
 // and of what stands beside the stages, in cycles at 2.4 GHz, from full launches (us,
-// modes 0 to 3: 32768 x 4096 x 1024 129, 151, 280, 113; 32768 x 1024 x 4096 167, 207,
-// 480, 154; 24165 x 768 x 768, where the tiles do not fill whole rounds, 28, 29, 57, 33).
+// modes 0 to 3, random operands: 32768 x 4096 x 1024 164, 178, 334, 121; 32768 x 1024 x
+// 4096 179, 215, 498, 160; 24165 x 768 x 768, where the tiles do not fill whole rounds,
+// 29, 29, 60, 32).
 SC_DEV LinPlan lin_plan(int R, int N, int ns) {
   LinPlan p = {0, 0, 0};
   long long best = 1LL << 62;
@@ -983,8 +986,7 @@ hipError_t run_few(const Linear& l, const void* x, hipStream_t s) {
 
 bool linear_few_ok(long long rows, int K, int N) {
   if (rows > kFewRows || i8_pitch(K) > kFewK) return false;
-  const long long wgs = (rows + 15) / 16 * ((N + 15) / 16);
-  return wgs <= kFewWgs && wgs * i8_pitch(K) <= kFewWork;
+  return (rows + 15) / 16 * ((N + 15) / 16) <= (i8_pitch(K) <= 1024 ? 4 * kLinWgs : 2 * kLinWgs);
 }
 
 hipError_t launch_linear_few(const Linear& l, const void* x, int x_type, hipStream_t s) {
