@@ -302,14 +302,16 @@ constexpr int kLinWgs = 256;    // one workgroup per CU, each taking tiles in tu
 constexpr int kLinLds = 147456; // stage buffers: 3 x 48, 4 x 32 or 8 x 16 KB
 constexpr int kLinModes = 4;
 constexpr int kGroupM = 8;
-// k_linear_few: at most kFewRows rows of kFewK bytes, and at most the workgroups that the
-// CUs hold at once: four a CU up to 1024 bytes a row, two beyond (70 KB of LDS).  us in a
-// graph, bf16 rows, this kernel and the two launches of the others: K 512 N 2048 1 row
-// 4.1 and 7.1, 128 rows (1024 workgroups) 7.0 and 8.1, 192 rows 8.7 and 8.2; K 1024 N
-// 4096 64 rows (1024) 8.2 and 9.5, 96 rows 10.2 and 9.4; K 2304 N 768 64 rows 8.6 and
-// 12.2, 128 rows (384) 11.8 and 12.4, 192 rows (576) 16.1 and 12.7; K 4096 N 1024 1 row
-// 9.5 and 15.3, 128 rows (512) 13.9 and 16.5, 192 rows 19.4 and 16.8.  8-bit rows alike
-// (K 1024 N 4096 64 rows 5.4 and 6.8, K 2304 N 768 192 rows 12.1 and 9.2).
+// k_linear_few: at most kFewRows rows of kFewK bytes, and at most five workgroups a CU up
+// to 1024 bytes a row, two beyond (what 70 KB of LDS each let a CU hold).  us in a graph,
+// bf16 rows, this kernel and the two launches of the others: K 512 N 2048 1 row 4.1 and
+// 7.1, 128 rows (1024 workgroups) 7.0 and 8.1, 192 rows (1536) 8.7 and 8.2; K 768 N 2304
+// 128 rows (1152) 8.9 and 8.9, and one launch and a workspace less on the host (a call
+// 10 us instead of 15); K 1024 N 4096 64 rows (1024) 8.2 and 9.5, 96 rows (1536) 10.2 and
+// 9.4; K 2304 N 768 64 rows 8.6 and 12.2, 128 rows (384) 11.8 and 12.4, 192 rows (576)
+// 16.1 and 12.7; K 4096 N 1024 1 row 9.5 and 15.3, 128 rows (512) 13.9 and 16.5, 192 rows
+// 19.4 and 16.8.  8-bit rows alike (K 768 N 2304 128 rows 5.9 and 6.3, 192 rows 7.2 and
+// 6.3; K 2304 N 768 192 rows 12.1 and 9.2).
 constexpr int kFewRows = 512, kFewK = 4096;
 
 // Tile shapes: BM x BN, waves along M and N, stage buffers.
@@ -986,7 +988,7 @@ hipError_t run_few(const Linear& l, const void* x, hipStream_t s) {
 
 bool linear_few_ok(long long rows, int K, int N) {
   if (rows > kFewRows || i8_pitch(K) > kFewK) return false;
-  return (rows + 15) / 16 * ((N + 15) / 16) <= (i8_pitch(K) <= 1024 ? 4 * kLinWgs : 2 * kLinWgs);
+  return (rows + 15) / 16 * ((N + 15) / 16) <= (i8_pitch(K) <= 1024 ? 5 * kLinWgs : 2 * kLinWgs);
 }
 
 hipError_t launch_linear_few(const Linear& l, const void* x, int x_type, hipStream_t s) {
