@@ -11,6 +11,12 @@
 //                 4.0 POP/s here, 32x32x32 3.5: the clock follows the power; with
 //                 zeros 4.8 and 4.9.)
 // k_linear_few    the same for a few rows: quantisation and product in one launch.
+//
+// 32768 x 4096 x 1024 on 8-bit rows: 116 us, 2.4 POP/s (a library's 8192^3: 2.0), at
+// 1.8 GHz under load, the matrix units busy 0.62 of the cycles.  32768 x 1024 x 4096
+// with GELU: 21 us of quantising (HBM rate) and 182, 0.36 of the cycles: a tile has few
+// stages there, and the arithmetic on its results (14 instructions each, an exponential
+// among them) and 268 MB of stores stand beside them.
 #include <algorithm>
 
 #include "sc_device.h"
