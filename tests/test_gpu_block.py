@@ -777,3 +777,88 @@ def test_debug_library_refuses_bad_lengths():
             assert torch.equal(y, sc.sc_block_norm(d, x, r=False)[1])
         else:
             assert (y == -7.0).all()
+
+
+@pytest.mark.parametrize("n", [8, 300])
+def test_batch_without_a_row(n):
+    """Every sequence is empty: outputs and gradients are zeros, whatever the inputs hold (few rows and many)."""
+    B, D = 5, 200
+    lens = torch.zeros(B, dtype=torch.int32, device=DEV)
+    x = torch.full((B, n, D), float("nan"), dtype=torch.bfloat16, device=DEV)
+    wq, ws = sc.sc_quantize_weight_i8(torch.randn((D, 72), generator=gen(1)).to(DEV))
+    xq, xs = sc.sc_quantize_rows_i8(x, valid_len=lens)
+    assert not xq.any() and not xs.any()
+    for a, code, scale in ((x, sc.SC_BF16, None), (torch.full_like(xq, 77), sc.SC_I8, torch.full_like(xs, float("nan")))):
+        out = torch.full((B, n, 72), float("nan"), dtype=torch.bfloat16, device=DEV)
+        sc.sc_linear_i8(sc.LinearDesc(B, n, D, 72, valid_len=lens, x_dtype=code), a, wq, ws, x_scale=scale, out=out)
+        assert not out.any()
+    for gate, shape, dt in ((sc.SC_GATE_CHANNEL, (D,), torch.float32), (sc.SC_GATE_SEQUENCE, (B, D), torch.bfloat16),
+                            (sc.SC_GATE_TOKEN, (B, n, D), torch.bfloat16)):
+        d = sc.NormDesc(B, n, D, valid_len=lens, post=True, gate=gate)
+        w = torch.ones(D, device=DEV)
+        a = dict(gate=torch.ones(shape, dtype=dt, device=DEV), post_w=w, post_b=w, pre_w=w, pre_b=w)
+        assert not any(t.any() for t in sc.sc_block_norm(d, x, x.clone(), quantized=True, **a))
+        grads = sc.sc_block_norm_backward(d, x, x.clone(), dr=x, dy=x, **a)
+        assert len(grads) == 7 and not any(t.any() for t in grads.values())
+
+
+def norm_and_products(lens, B, n, seed):
+    """A block of norm, products and the norm's gradients; a function of the streams' and lengths' present state."""
+    D, F = 192, 640
+    g = gen(seed)
+    x, t = (torch.randn((B, n, D), generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+    w1, w2 = (sc.sc_quantize_weight_i8(torch.randn(s, generator=g).to(DEV)) for s in ((D, F), (F, D)))
+    v = torch.linspace(0.5, 1.5, D, device=DEV)
+
+    def run():
+        d = sc.NormDesc(B, n, D, valid_len=lens, post=True, gate=sc.SC_GATE_CHANNEL)
+        a = dict(gate=v, post_w=v, pre_w=v)
+        r, y, yq, ys = sc.sc_block_norm(d, x, t, quantized=True, **a)
+        h = sc.sc_linear_i8(sc.LinearDesc(B, n, D, F, valid_len=lens, x_dtype=sc.SC_I8, act=sc.SC_ACT_GELU), yq, *w1,
+                            x_scale=ys)
+        o = sc.sc_linear_i8(sc.LinearDesc(B, n, F, D, valid_len=lens), h, *w2)
+        return [r, y, h, o, *(z for z in sc.sc_block_norm_backward(d, x, t, dr=r, dy=o, **a).values() if z is not None)]
+    return run
+
+
+def test_two_streams_at_once():
+    """Ten rounds on two streams, each with its own tensors and workspaces: the bits of one call alone."""
+    runs = [norm_and_products(torch.tensor([n, 3, 0, n - 1], dtype=torch.int32, device=DEV), 4, n, n) for n in (700, 40)]
+    want = [run() for run in runs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in runs]
+    got = [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(runs[i]())
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        for outs in g:
+            assert all(torch.equal(a, b) for a, b in zip(outs, w))
+
+
+@pytest.mark.parametrize("n", [20, 900])
+def test_replays_follow_the_lengths(n):
+    """Captured once; the lengths change in place between the replays (to none and to all rows among them)."""
+    B = 3
+    lens = torch.tensor([n, 1, n // 2], dtype=torch.int32, device=DEV)
+    run = norm_and_products(lens, B, n, n)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = run()
+    for new in ([n, 1, n // 2], [0, 0, 0], [n, n, n], [2, n - 3, 0], [n, 1, n // 2]):
+        lens.copy_(torch.tensor(new, dtype=torch.int32))
+        want = run()
+        torch.cuda.synchronize()
+        for o in outs:
+            o.fill_(-3)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), new
