@@ -313,7 +313,9 @@ def sc_encoder_stack_i8(desc, x_in, layers, ffn_dim, thresholds, windows=None, k
     for i, y in enumerate(layers):
         y.check(f"layers[{i}]", D, F)
     call = _Call(stream, x_in)
-    for t in (x_in, x_out, workspace, desc.valid_len, desc.global_pos, *(t for y in layers for t in y.tensors())):
+    call.lengths(desc.valid_len, B)
+    call.opt(desc.global_pos, "global_pos", torch.int32, (B, desc.G))
+    for t in (x_in, x_out, workspace, *(t for y in layers for t in y.tensors())):
         call.opt(t, "argument", t if t is None else t.dtype, t if t is None else t.shape)
     dev = x_in.device
     x_out = torch.empty_like(x_in) if x_out is None else x_out

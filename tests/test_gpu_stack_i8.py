@@ -127,3 +127,24 @@ def test_stack_i8_captured():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_stack_i8_binding_refusals():
+    """Tensors of another type, shape or place never reach the library."""
+    B, n, H, F = 2, 64, 2, 200
+    x, layers = make(B, n, H, F, 1, seed=5)
+    vl = torch.tensor([64, 7], dtype=torch.int32, device=DEV)
+    gp = torch.zeros((B, 1), dtype=torch.int32, device=DEV)
+
+    def call(x=x, vl=vl, gp=gp, layers=layers, F=F, th=(0.0,), **kw):
+        return sc.sc_encoder_stack_i8(sc.Desc(B, n, H, 32, vl, gp), x, layers, F, th, **kw)
+    call()
+    q, s, b = layers[0].products["qkv"]
+    with_qkv = lambda *w: [sc.LayerI8(w, *(layers[0].products[k] for k in ("o", "w1", "w2")))]  # noqa: E731
+    for bad in (dict(vl=vl.long()), dict(vl=vl[:1]), dict(vl=vl.cpu()), dict(gp=gp.long()), dict(gp=gp[:1]),
+                dict(x=x.float()), dict(x=x[:, :63]), dict(x=x.cpu()), dict(F=F + 1), dict(th=(0.0, 0.0)),
+                dict(layers=with_qkv(q.t(), s, b)), dict(layers=with_qkv(q, s[1:], b)), dict(layers=with_qkv(q, s.half(), b)),
+                dict(layers=with_qkv(q, s, b.cpu())), dict(x_out=x[:1]), dict(windows=[32, 32]),
+                dict(workspace=torch.empty(16, dtype=torch.uint8, device=DEV))):
+        with pytest.raises((TypeError, ValueError)):
+            call(**bad)
