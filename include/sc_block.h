@@ -70,7 +70,7 @@ sc_status sc_quantize_weight_i8(int32_t K, int32_t N, int32_t dtype, const void 
                                 void *stream);
 
 #define SC_ACT_NONE 0
-#define SC_ACT_GELU 1 /* v * Phi(v) */
+#define SC_ACT_GELU 1 /* v * Phi(v), float32 before the store: within 2.4e-7, and 3e-5 of the value down to v = -9 */
 
 typedef struct sc_linear_desc {
   int32_t B, n, K, N;        /* rows as above, K inputs, N outputs per row */

@@ -31,45 +31,36 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 
 // -------------------------------------------------------- activations ----
 // gelu(v) = max(v, 0) - |v| Phi(-|v|), with Phi(-a) = exp2(P(a)): log2 Phi(-a)
-// is close to a parabola, so a short polynomial (fitted here, minimax in the
+// is close to a parabola, so a polynomial (fitted here on [0, 9], minimax in the
 // relative error of Phi) replaces the rational form and its reciprocal, and a
 // negative leading coefficient lets it run on to 0 beyond the fitted range.
-// Stored as bf16: degree 5 on [0, 5], relative error 1.6e-4 there, a twelfth of
-// half a bf16 step.  Stored as float32: degree 12 on [0, 9], absolute error
-// 2.4e-7.  NaN stays NaN; |v| beyond 16 is cut for the product with Phi = 0.
-template <bool kF32>
+// Absolute error 2.4e-7; of a negative value 1e-6 relative down to -3, 2.5e-6 to
+// -5, 3e-5 to -9, where it is 1e-18.  One form for both output types: what is
+// stored as bf16 is the float32 value rounded once (degree 5 has 1.6e-4 relative and
+// 1 % beyond -5, and is 7 instructions of 21 shorter).  NaN stays NaN; |v| beyond
+// 16 is cut for the product with Phi = 0.
 SC_DEV float gelu_exp2(float v) {
   const float a = __builtin_elementwise_minimum(fabsf(v), 16.f);  // without the quieting that fminf needs
-  float p;
-  if constexpr (kF32) {
-    p = -4.266044115186496e-11f;
-    p = fmaf(p, a, 2.5370372469524227e-09f);
-    p = fmaf(p, a, -6.685024089847502e-08f);
-    p = fmaf(p, a, 1.0232761269435287e-06f);
-    p = fmaf(p, a, -9.952474101737607e-06f);
-    p = fmaf(p, a, 6.172758003231138e-05f);
-    p = fmaf(p, a, -0.00020646034681703895f);
-    p = fmaf(p, a, -0.00019499764312058687f);
-    p = fmaf(p, a, 0.007243024185299873f);
-    p = fmaf(p, a, -0.05268990248441696f);
-    p = fmaf(p, a, -0.45911744236946106f);
-    p = fmaf(p, a, -1.1511205434799194f);
-    p = fmaf(p, a, -0.9999995827674866f);
-  } else {
-    p = -0.0002699175092857331f;
-    p = fmaf(p, a, 0.005297347437590361f);
-    p = fmaf(p, a, -0.046319346874952316f);
-    p = fmaf(p, a, -0.46690741181373596f);
-    p = fmaf(p, a, -1.1477890014648438f);
-    p = fmaf(p, a, -1.0002282857894897f);
-  }
+  float p = -4.266044115186496e-11f;
+  p = fmaf(p, a, 2.5370372469524227e-09f);
+  p = fmaf(p, a, -6.685024089847502e-08f);
+  p = fmaf(p, a, 1.0232761269435287e-06f);
+  p = fmaf(p, a, -9.952474101737607e-06f);
+  p = fmaf(p, a, 6.172758003231138e-05f);
+  p = fmaf(p, a, -0.00020646034681703895f);
+  p = fmaf(p, a, -0.00019499764312058687f);
+  p = fmaf(p, a, 0.007243024185299873f);
+  p = fmaf(p, a, -0.05268990248441696f);
+  p = fmaf(p, a, -0.45911744236946106f);
+  p = fmaf(p, a, -1.1511205434799194f);
+  p = fmaf(p, a, -0.9999995827674866f);
   return fmaf(-a, fast_exp2(p), vmax(v, 0.f));
 }
 
-template <bool kF32, bool kGelu>
+template <bool kGelu>
 SC_DEV float finish(int acc, float sx, float sw, float bias) {
   const float v = fmaf((float)acc * sx, sw, bias);
-  return kGelu ? gelu_exp2<kF32>(v) : v;
+  return kGelu ? gelu_exp2(v) : v;
 }
 
 SC_DEV void store_out(float* p, float v) { *p = v; }
@@ -576,7 +567,7 @@ struct LinWave {
       const f32x4 ws = *reinterpret_cast<const f32x4*>(d.sw + c), bs = *reinterpret_cast<const f32x4*>(d.sb + c);
       f32x4 o;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = finish<sizeof(O) == 4, kGelu>(v[i][j + f][e], xs, ws[e], bs[e]);
+      for (int e = 0; e < 4; ++e) o[e] = finish<kGelu>(v[i][j + f][e], xs, ws[e], bs[e]);
       if constexpr (sizeof(O) == 4) {
         store16(row, n0 + c, __builtin_bit_cast(uint4, o));
       } else {
@@ -924,7 +915,7 @@ __global__ __launch_bounds__(256) void k_linear_few(LinearArgs a, const T* __res
   if (m >= rows || col >= a.N) return;
   const int sum = red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid];
   const bool on = live(m);
-  const float v = on ? finish<sizeof(O) == 4, kGelu>(sum, ss[r], a.ws[col], a.bias ? a.bias[col] : 0.f) : 0.f;
+  const float v = on ? finish<kGelu>(sum, ss[r], a.ws[col], a.bias ? a.bias[col] : 0.f) : 0.f;
   store_out(static_cast<O*>(a.out) + m * a.N + col, v);
 }
 

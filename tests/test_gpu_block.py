@@ -862,3 +862,24 @@ def test_replays_follow_the_lengths(n):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), new
+
+
+@pytest.mark.parametrize("N", [20000, 32768], ids=["few rows", "tiles"])
+@pytest.mark.parametrize("out_type", ["bf16", "f32"])
+def test_gelu_is_float32_rounded_once(N, out_type):
+    """GELU of given arguments (the bias of a product of zeros), whatever the output's type within the error e that the
+    head of this file counts for float32: a bf16 output lies between the roundings of gelu - e and gelu + e, since
+    rounding never swaps two values."""
+    v = torch.linspace(-8, 8, N, dtype=torch.float64).float()
+    d = sc.LinearDesc(1, 1, 1, N, x_dtype=sc.SC_F32, out_dtype=TYPES[out_type][1], act=sc.SC_ACT_GELU)
+    wq = torch.zeros((N, 128), dtype=torch.int8, device=DEV)
+    out = sc.sc_linear_i8(d, torch.ones((1, 1, 1), device=DEV), wq, torch.ones(N, device=DEV), bias=v.to(DEV))[0, 0].cpu()
+    z = v.double()
+    a = z.abs()
+    tail = a * 0.5 * torch.special.erfc(a / math.sqrt(2))
+    own = torch.where(a < 3, 1e-6, torch.where(a < 5, 2.5e-6, 3e-5)) * tail
+    want = gelu64(z)
+    e = own + 2.0 ** -23 * tail + U * want.abs() + 1e-44
+    lo, hi = ((want + s * e).float().to(out.dtype).double() for s in (-1, 1))
+    bad = ~((lo <= out.double()) & (out.double() <= hi))
+    assert not bad.any(), f"{int(bad.sum())} of {N} off, the first at {float(z[bad][0])}"
