@@ -456,6 +456,10 @@ struct LinWave {
   static constexpr int XL = BM / 64, WL = BN / 64, kDma = XL + WL;  // loads of a wave and stage, 8 rows each
   static constexpr int kStage = (BM + BN) * kBK;
   static_assert(kNBuf * kStage <= kLinLds && FI % 2 == 0, "stage buffers, halves of the rows");
+  // What a wave stores of a whole tile, in instructions: emit for 16 rows and up to two
+  // column fragments at a time, one store of a lane's results each (bf16) or one a fragment
+  // (float32).
+  static constexpr int kEmits = FI * ((FJ + 1) / 2), kStores = sizeof(O) == 4 ? FI * FJ : kEmits;
   const LinearArgs& a;
   const Packed& pk;
   const int R, tid, lane, w, g, lr, wm, wn;
@@ -604,8 +608,12 @@ SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const
   if (sh.item >= sh.last) return;
   W w(a, stage, pk, R);
   const int ns = a.Kp / kBK;
-  // the last tile's stores that the first stages, loaded before them, do not wait for
-  constexpr int kStores = W::FI * (W::FJ + 1) / 2 * (sizeof(O) == 4 && W::FJ > 1 ? 2 : 1);
+  // The last tile's stores that the first stages, loaded before them, do not wait for.  A
+  // count above the stores issued would let a stage be read before it has landed; below, it
+  // only waits longer.
+  constexpr int kStores = W::kStores;
+  static_assert(kStores == (kM == 1 ? 4 : kM == 2 ? 2 : 16) * (sizeof(O) == 4 && kM != 2 ? 2 : 1),
+                "128 x 128, 64 x 64 and 256 x 256 tiles: a wave's stores, 16 bytes a lane (64 x 64 bf16: 8)");
   bool stored = false;
   int m0, n0, cur = 0;
   sh.template place<W::BM, W::BN>(sh.item, m0, n0);
@@ -673,7 +681,7 @@ SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const
     for (int i = 0; i < W::FI; ++i)
 #pragma unroll
       for (int j = 0; j < W::FJ; j += 2) w.emit(w.acc, tab[cur], n0, i, j);
-    stored = n0 + W::BN <= a.N;  // a whole tile: exactly kStores of them, every lane's
+    stored = n0 + W::BN <= a.N;  // a whole tile: every lane's kStores stores
     if (!more) return;
     sh.item = nitem;
     n0 = nn0;
@@ -689,7 +697,7 @@ SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const
 template <typename O, bool kGelu>
 SC_DEV void linear_stream(const LinearArgs& a, char* stage, LinTables* tab, const Packed& pk, int R, const LinPlan& pl) {
   using W = LinWave<0, O, kGelu>;
-  constexpr int kNBuf = W::kNBuf, kDma = W::kDma, kUnits = W::FI * W::FJ / 2;
+  constexpr int kNBuf = W::kNBuf, kDma = W::kDma, kUnits = W::kEmits;
   static_assert(kStreamMin == kNBuf + 2, "a barrier between the last tile's results and the next tile's tables");
   LinShare sh(pl);
   if (sh.item >= sh.last) return;

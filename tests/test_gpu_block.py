@@ -883,3 +883,28 @@ def test_gelu_is_float32_rounded_once(N, out_type):
     lo, hi = ((want + s * e).float().to(out.dtype).double() for s in (-1, 1))
     bad = ~((lo <= out.double()) & (out.double() <= hi))
     assert not bad.any(), f"{int(bad.sum())} of {N} off, the first at {float(z[bad][0])}"
+
+
+# Rounds of whole tiles one after the other, so that stages of a tile load while the last one's results are stored: two
+# and five rounds of 128 x 128 tiles (4 and 16 stages), three of 256 x 256 (two stages, and one).
+ROUNDS = [(3000, 512, 1536), (9389, 2048, 2048), (20000, 256, 2048), (17000, 128, 2048)]
+
+
+@pytest.mark.parametrize("out_type", ["bf16", "f32"])
+@pytest.mark.parametrize("n,K,N", ROUNDS)
+def test_linear_rounds_of_whole_tiles(n, K, N, out_type):
+    """Every row of a call of several rounds is that of a call of few rows, which has no stages; twice."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(n)
+    xq = torch.randint(-127, 128, (1, n, K), dtype=torch.int8, device=DEV, generator=g)
+    wq = torch.randint(-127, 128, (N, K), dtype=torch.int8, device=DEV, generator=g)
+    xs, ws = (torch.rand(s, device=DEV, generator=g) + 0.5 for s in ((1, n), (N,)))
+    bias = torch.randn(N, device=DEV, generator=g)
+    few = (5 if K <= 1024 else 2) * 256 // (N // 16) * 16  # rows of the one-launch form
+
+    def run(lo, hi):
+        d = sc.LinearDesc(1, hi - lo, K, N, x_dtype=sc.SC_I8, out_dtype=TYPES[out_type][1])
+        return sc.sc_linear_i8(d, xq[:, lo:hi], wq, ws, bias=bias, x_scale=xs[:, lo:hi])[0]
+    want = torch.cat([run(lo, min(n, lo + few)) for lo in range(0, n, few)])
+    for _ in range(2):
+        assert torch.equal(run(0, n), want)
