@@ -790,7 +790,7 @@ sc_status run_stack_i8(const sc_attn_desc* d, int32_t n_layers, const int32_t* w
   Launches chk;
   StackRows rows = stack_rows(d, w, chk, s);
   __bf16* t = reinterpret_cast<__bf16*>(w.t);
-  auto few = [&](int K, int N) { return sc::linear_few_ok((long long)B * n, K, N); };
+  auto few = [&](int K, int N, int type) { return sc::linear_few_ok((long long)B * n, K, N, type); };
   // out = lin(wt, v), v given as 8-bit rows (or, for few rows, as bf16 ones: x), on the
   // rows of len
   auto linear = [&](const int8_t* q, const float* qs, const sc_i8_weight& wt, void* out, int K, int N,
@@ -810,7 +810,7 @@ sc_status run_stack_i8(const sc_attn_desc* d, int32_t n_layers, const int32_t* w
     a.len = len;
     a.skip_pad = 1;
     a.gelu = gelu;
-    if (few(K, N))
+    if (few(K, N, x ? SC_BF16 : SC_I8))
       chk(x ? sc::launch_linear_few(a, x, SC_BF16, s) : sc::launch_linear_few(a, q, SC_I8, s));
     else
       chk(sc::launch_linear_i8(a, s));
@@ -860,7 +860,7 @@ sc_status run_stack_i8(const sc_attn_desc* d, int32_t n_layers, const int32_t* w
     linear(w.xq, w.xs, y.o, t, D, D, rows.len_nxt, 0);
     norm(cur, w.keep_idx, y.gate1, y.ln1_w, y.ln1_b, w.x1, true);
     linear(w.yq, w.ys, y.w1, w.h, D, F, rows.len_nxt, 1);
-    if (!few(F, D)) quantise(w.h, F, rows.len_nxt, nullptr);
+    if (!few(F, D, SC_BF16)) quantise(w.h, F, rows.len_nxt, nullptr);
     linear(w.xq, w.xs, y.w2, t, F, D, rows.len_nxt, 0, w.h);
     norm(w.x1, nullptr, y.gate2, y.ln2_w, y.ln2_b, nxt, l + 1 < n_layers);
     cur = nxt;

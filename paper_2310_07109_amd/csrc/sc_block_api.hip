@@ -41,7 +41,7 @@ struct LinearWs {
 };
 size_t carve_linear(const sc_linear_desc* d, void* base, LinearWs* w) {
   // no rows of its own: they come quantised, or stay in the launch
-  if (d->x_dtype == SC_I8 || sc::linear_few_ok((long long)d->B * d->n, d->K, d->N)) return 0;
+  if (d->x_dtype == SC_I8 || sc::linear_few_ok((long long)d->B * d->n, d->K, d->N, d->x_dtype)) return 0;
   const size_t rows = (size_t)d->B * d->n;
   Carver c(base);
   LinearWs x;
@@ -171,7 +171,7 @@ sc_status linear_impl(const sc_linear_desc* d, const void* x, const float* x_sca
   l.len = d->valid_len;
   l.gelu = d->act == SC_ACT_GELU;
   l.out_f32 = d->out_dtype == SC_F32;
-  if (sc::linear_few_ok((long long)rows, d->K, d->N))
+  if (sc::linear_few_ok((long long)rows, d->K, d->N, d->x_dtype))
     return sc::launch_linear_few(l, x, d->x_dtype, s) == hipSuccess ? SC_OK : SC_EHIP;
   if (d->x_dtype != SC_I8) {
     LinearWs w;

@@ -196,7 +196,7 @@ struct Linear {
 hipError_t launch_linear_i8(const Linear& l, hipStream_t s);
 // The product of few rows from x itself, quantised in the same launch (x_type as
 // SC_F32, SC_BF16, SC_I8; xq, and xs but for 8-bit rows, are not used).
-bool linear_few_ok(long long rows, int K, int N);
+bool linear_few_ok(long long rows, int K, int N, int x_type);
 hipError_t launch_linear_few(const Linear& l, const void* x, int x_type, hipStream_t s);
 
 // Block norms (sc_norm.hip).

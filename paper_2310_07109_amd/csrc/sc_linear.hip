@@ -299,16 +299,25 @@ constexpr int kLinWgs = 256;    // one workgroup per CU, each taking tiles in tu
 constexpr int kLinLds = 147456; // stage buffers: 3 x 48, 4 x 32 or 8 x 16 KB
 constexpr int kLinModes = 4;
 constexpr int kGroupM = 8;
-// k_linear_few: at most kFewRows rows of kFewK bytes, and at most five workgroups a CU up
-// to 1024 bytes a row, two beyond (what 70 KB of LDS each let a CU hold).  us in a graph,
-// bf16 rows, this kernel and the two launches of the others: K 512 N 2048 1 row 4.1 and
-// 7.1, 128 rows (1024 workgroups) 7.0 and 8.1, 192 rows (1536) 8.7 and 8.2; K 768 N 2304
-// 128 rows (1152) 8.9 and 8.9, and one launch and a workspace less on the host (a call
-// 10 us instead of 15); K 1024 N 4096 64 rows (1024) 8.2 and 9.5, 96 rows (1536) 10.2 and
-// 9.4; K 2304 N 768 64 rows 8.6 and 12.2, 128 rows (384) 11.8 and 12.4, 192 rows (576)
-// 16.1 and 12.7; K 4096 N 1024 1 row 9.5 and 15.3, 128 rows (512) 13.9 and 16.5, 192 rows
-// 19.4 and 16.8.  8-bit rows alike (K 768 N 2304 128 rows 5.9 and 6.3, 192 rows 7.2 and
-// 6.3; K 2304 N 768 192 rows 12.1 and 9.2).
+// k_linear_few: at most kFewRows rows of kFewK bytes, and at most as many workgroups a CU
+// as few_per_cu gives.  Every workgroup quantises its 16 rows again, so the limit falls with
+// the cost of that.  us in a graph, this kernel and the two launches of the others:
+//   bf16 and 8-bit rows, up to 1024 bytes: five.  K 512 N 2048 1 row 4.1 and 7.1, 128 rows
+//     (1024 workgroups) 7.0 and 8.1, 192 rows (1536) 8.7 and 8.2; K 768 N 2304 128 rows
+//     (1152) 8.9 and 8.9, and one launch and a workspace less on the host (a call 10 us
+//     instead of 15); K 1024 N 4096 64 rows (1024) 8.2 and 9.5, 96 rows (1536) 10.2 and 9.4.
+//   the same beyond: two, what 70 KB of LDS each let a CU hold.  K 2304 N 768 64 rows 8.6 and
+//     12.2, 128 rows (384) 11.8 and 12.4, 192 rows (576) 16.1 and 12.7; K 4096 N 1024 1 row
+//     9.5 and 15.3, 128 rows (512) 13.9 and 16.5, 192 rows 19.4 and 16.8.  8-bit rows alike
+//     (K 768 N 2304 128 rows 5.9 and 6.3, 192 rows 7.2 and 6.3; K 2304 N 768 192 rows 12.1
+//     and 9.2).
+//   float32 rows, up to 1024 bytes: three.  K 1023 N 4096 48 rows (768) 9.2 and 9.5, 64 rows
+//     (1024) 10.6 and 9.7; K 767 N 2304 96 rows (864) 10.2 and 9.0.  Beyond: one.  K 4095
+//     N 1024 64 rows (256) 17.7 and 18.2, 96 rows (384) 20.8 and 18.4.
+//   bf16 rows of odd length, an element a load: one.  K 767 N 768 64 rows (192) 6.8 and 9.0,
+//     96 rows (288) 10.2 and 9.0; K 2303 N 768 1 row 12.4 and 14.0, 64 rows (192) 16.2 and
+//     15.8, 96 rows (288) 28.7 and 15.9.  Rows of even length at an odd address cost as much
+//     and keep the limit of their type: sizes alone decide, since the workspace goes by them.
 constexpr int kFewRows = 512, kFewK = 4096;
 
 // Tile shapes: BM x BN, waves along M and N, stage buffers.
@@ -889,7 +898,8 @@ __global__ __launch_bounds__(256) void k_linear_few(LinearArgs a, const T* __res
       if (lane == 0) ss[r] = on ? a.xs[m0 + r] : 0.f;
     }
   } else {
-    constexpr int kAtOnce = kUnits == 2 || (kVec && sizeof(T) == 2) ? 4 : 2;  // rows held at once, as registers allow
+    // rows held at once, as registers allow (an element a load: 272 with two, one workgroup a CU)
+    constexpr int kAtOnce = kUnits == 2 || (kVec && sizeof(T) == 2) ? 4 : kVec ? 2 : 1;
 #pragma unroll
     for (int r0 = 0; r0 < 4; r0 += kAtOnce) {
       RowHeld<T, kVec, kUnits> h[kAtOnce];
@@ -991,9 +1001,18 @@ hipError_t run_few(const Linear& l, const void* x, hipStream_t s) {
 }
 }  // namespace
 
-bool linear_few_ok(long long rows, int K, int N) {
+namespace {
+int few_per_cu(int K, int x_type) {
+  const bool longer = i8_pitch(K) > 1024;
+  if (x_type == 1 && K % 2 != 0) return 1;
+  if (x_type == 0) return longer ? 1 : 3;
+  return longer ? 2 : 5;
+}
+}  // namespace
+
+bool linear_few_ok(long long rows, int K, int N, int x_type) {
   if (rows > kFewRows || i8_pitch(K) > kFewK) return false;
-  return (rows + 15) / 16 * ((N + 15) / 16) <= (i8_pitch(K) <= 1024 ? 5 * kLinWgs : 2 * kLinWgs);
+  return (rows + 15) / 16 * ((N + 15) / 16) <= few_per_cu(K, x_type) * kLinWgs;
 }
 
 hipError_t launch_linear_few(const Linear& l, const void* x, int x_type, hipStream_t s) {

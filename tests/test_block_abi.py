@@ -231,3 +231,15 @@ def test_workspace_alignment_and_long_rows_refused():
     for K in (1 << 29, (1 << 31) - 129):
         for dt in (sc.SC_F32, sc.SC_BF16):
             assert L.sc_quantize_rows_i8(1, 1, K, None, dt, A[0], A[8], A[16], None) == B.SC_EUNSUPPORTED, (K, dt)
+
+
+@pytest.mark.parametrize("x_dtype,n,K,N,one_launch", [
+    (sc.SC_BF16, 128, 768, 2304, True), (sc.SC_BF16, 128, 2304, 768, True), (sc.SC_BF16, 192, 2304, 768, False),
+    (sc.SC_BF16, 64, 767, 768, True), (sc.SC_BF16, 96, 767, 768, False),        # an element a load
+    (sc.SC_BF16, 64, 2303, 768, True), (sc.SC_BF16, 96, 2303, 768, False), (sc.SC_BF16, 32, 4095, 4096, False),
+    (sc.SC_F32, 48, 1023, 4096, True), (sc.SC_F32, 64, 1023, 4096, False),
+    (sc.SC_F32, 64, 4095, 1024, True), (sc.SC_F32, 96, 4095, 1024, False)])
+def test_rows_quantised_in_the_products_launch(x_dtype, n, K, N, one_launch):
+    """Where every workgroup quantises its rows for itself no rows are kept in a workspace: as long as that is faster for
+    rows of the type and length."""
+    assert (sc.sc_linear_i8_workspace_size(sc.LinearDesc(1, n, K, N, x_dtype=x_dtype)) == 0) == one_launch

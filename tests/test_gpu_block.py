@@ -908,3 +908,24 @@ def test_linear_rounds_of_whole_tiles(n, K, N, out_type):
     want = torch.cat([run(lo, min(n, lo + few)) for lo in range(0, n, few)])
     for _ in range(2):
         assert torch.equal(run(0, n), want)
+
+
+@pytest.mark.parametrize("x_type,K,N", [("bf16", 767, 768), ("bf16", 1111, 1040), ("bf16", 2303, 300), ("f32", 1023, 4096),
+                                        ("f32", 2303, 768)])
+def test_linear_rows_around_the_one_launch_limit(x_type, K, N):
+    """Rows of odd length and float32 ones, on both sides of the limits of the one-launch form, and at odd addresses (K
+    one shorter): the bits of each row alone."""
+    x = torch.randn((1, 200, K), generator=gen(K)).to(TYPES[x_type][0]).to(DEV)
+    wq, ws = sc.sc_quantize_weight_i8(torch.randn((K, N), generator=gen(N)).to(DEV))
+
+    def run(rows, k=K):
+        part = x[:, rows, :k].contiguous()
+        d = sc.LinearDesc(1, part.shape[1], k, N, x_dtype=TYPES[x_type][1])
+        w = wq if k == K else wq.index_fill(1, torch.tensor([k], device=DEV), 0)
+        aligned = sc.sc_linear_i8(d, part, w, ws)[0]
+        assert torch.equal(sc.sc_linear_i8(d, off_by_one(part), w, ws)[0], aligned)
+        return aligned
+    alone = torch.cat([run(slice(i, i + 1)) for i in range(0, 200, 7)])
+    for n in (16, 32, 48, 64, 96, 200):
+        assert torch.equal(run(slice(0, n))[::7], alone[: (n + 6) // 7]), n
+    assert torch.equal(run(slice(0, 96), K - 1)[:16], run(slice(0, 16), K - 1))

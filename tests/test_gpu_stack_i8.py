@@ -148,3 +148,8 @@ def test_stack_i8_binding_refusals():
                 dict(workspace=torch.empty(16, dtype=torch.uint8, device=DEV))):
         with pytest.raises((TypeError, ValueError)):
             call(**bad)
+
+
+def test_stack_with_an_odd_feed_forward_width():
+    """512 rows of 777 values: beyond the one-launch form of bf16 rows of odd length, within that of 8-bit rows."""
+    test_stack_is_its_operators(2, 256, 4, 777, (256, 201), 0, (0.003, 0.004), (64, 64), True, 1.0)
