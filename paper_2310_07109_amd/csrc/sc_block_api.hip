@@ -11,6 +11,8 @@ namespace {
 
 bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
+constexpr int kQuantMaxK = 1 << 29;  // 32-bit byte offsets inside a row
+
 bool float_type(int t) { return t == SC_F32 || t == SC_BF16; }
 
 // A padded batch of rows.
@@ -124,10 +126,10 @@ bool any_overlap(const Span& out, const Span (&others)[N]) {
 
 sc_status quantize_rows_impl(int32_t B, int32_t n, int32_t K, const int32_t* valid_len, int32_t dtype, const void* x,
                              int8_t* xq, float* scale, void* stream) {
-  if (K < 1 || K > INT32_MAX - sc::kI8Pitch || !float_type(dtype) || !x || !xq || !scale) return SC_EINVAL;
+  if (K < 1 || !float_type(dtype) || !x || !xq || !scale) return SC_EINVAL;
   const sc_status st = check_rows(B, n);
   if (st != SC_OK) return st;
-  if (K >= 1 << 29) return SC_EUNSUPPORTED;  // 32-bit byte offsets inside a row
+  if (K >= kQuantMaxK) return SC_EUNSUPPORTED;
   const size_t rows = (size_t)B * n, xb = rows * K * elem_size(dtype), qb = rows * sc::i8_pitch(K), sb = rows * 4;
   if (!aligned(xq, 16)) return SC_EINVAL;
   if (overlaps(xq, qb, x, xb) || overlaps(scale, sb, x, xb) || overlaps(xq, qb, scale, sb)) return SC_EINVAL;
@@ -288,8 +290,9 @@ sc_status sc_quantize_rows_i8(int32_t B, int32_t n, int32_t K, const int32_t* va
 
 sc_status sc_quantize_weight_i8(int32_t K, int32_t N, int32_t dtype, const void* w, int8_t* wq, float* scale,
                                 void* stream) {
-  if (K < 1 || N < 1 || K > INT32_MAX - sc::kI8Pitch || !float_type(dtype) || !w || !wq || !scale) return SC_EINVAL;
+  if (K < 1 || N < 1 || !float_type(dtype) || !w || !wq || !scale) return SC_EINVAL;
   if (!aligned(wq, 16)) return SC_EINVAL;
+  if (K >= kQuantMaxK) return SC_EUNSUPPORTED;
   const long long pitch = sc::i8_pitch(K);
   if (N * pitch >= (1LL << 32)) return SC_EUNSUPPORTED;
   const size_t wb = (size_t)K * N * elem_size(dtype), qb = (size_t)N * pitch, sb = 4 * (size_t)N;

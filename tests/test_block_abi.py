@@ -243,3 +243,15 @@ def test_rows_quantised_in_the_products_launch(x_dtype, n, K, N, one_launch):
     """Where every workgroup quantises its rows for itself no rows are kept in a workspace: as long as that is faster for
     rows of the type and length."""
     assert (sc.sc_linear_i8_workspace_size(sc.LinearDesc(1, n, K, N, x_dtype=x_dtype)) == 0) == one_launch
+
+
+@pytest.mark.parametrize("K", [1 << 29, (1 << 31) - 129, (1 << 31) - 128, (1 << 31) - 1])
+def test_quantisation_refuses_long_rows_alike(K):
+    """K >= 2^29 is unsupported, of rows and of weights, up to the largest int32; invalid arguments come first."""
+    L = sc.load()
+    far = [i << 44 for i in range(1, 5)]  # disjoint whatever K
+    for dt in (sc.SC_F32, sc.SC_BF16):
+        assert L.sc_quantize_rows_i8(1, 1, K, None, dt, far[0], far[1], far[2], None) == B.SC_EUNSUPPORTED
+        assert L.sc_quantize_weight_i8(K, 1, dt, far[0], far[1], far[2], None) == B.SC_EUNSUPPORTED
+    assert L.sc_quantize_rows_i8(1, 1, K, None, 7, far[0], far[1], far[2], None) == B.SC_EINVAL
+    assert L.sc_quantize_weight_i8(K, 1, sc.SC_F32, None, far[1], far[2], None) == B.SC_EINVAL
