@@ -172,9 +172,11 @@ def _on_stream(fn):
     """Runs a wrapper with `stream` (when given) as torch's current stream, so that the outputs and workspaces
     it allocates belong to the stream its kernels are enqueued on: the caching allocator then never hands that
     memory to work on another stream while the kernels still use it."""
+    at = fn.__code__.co_varnames.index("stream")
+
     @functools.wraps(fn)
     def run(*args, **kwargs):
-        stream = kwargs.get("stream")
+        stream = args[at] if len(args) > at else kwargs.get("stream")
         if stream is None:
             return fn(*args, **kwargs)
         import torch

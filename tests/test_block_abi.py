@@ -255,3 +255,23 @@ def test_quantisation_refuses_long_rows_alike(K):
         assert L.sc_quantize_weight_i8(K, 1, dt, far[0], far[1], far[2], None) == B.SC_EUNSUPPORTED
     assert L.sc_quantize_rows_i8(1, 1, K, None, 7, far[0], far[1], far[2], None) == B.SC_EINVAL
     assert L.sc_quantize_weight_i8(K, 1, sc.SC_F32, None, far[1], far[2], None) == B.SC_EINVAL
+
+
+def test_stream_given_by_position(monkeypatch):
+    """A wrapper allocates its outputs and workspaces on the stream that it is given, however it is given."""
+    import contextlib
+    current = [None]
+
+    @contextlib.contextmanager
+    def on(stream):
+        before, current[0] = current[0], stream
+        yield
+        current[0] = before
+    monkeypatch.setattr(torch.cuda, "stream", on)
+
+    @B._on_stream
+    def wrapper(x, out=None, stream=None):
+        return x, out, stream, current[0]
+    assert wrapper(1, 2, "s") == (1, 2, "s", "s") == wrapper(1, 2, stream="s")
+    assert wrapper(1, stream=None) == (1, None, None, None) == wrapper(1, None, None)
+    assert current[0] is None
