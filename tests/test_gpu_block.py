@@ -929,3 +929,26 @@ def test_linear_rows_around_the_one_launch_limit(x_type, K, N):
     for n in (16, 32, 48, 64, 96, 200):
         assert torch.equal(run(slice(0, n))[::7], alone[: (n + 6) // 7]), n
     assert torch.equal(run(slice(0, 96), K - 1)[:16], run(slice(0, 16), K - 1))
+
+
+# More rows than the workgroups that a row takes whole (2048 forward, 512 backward): every width and element access of
+# that form, sequences without rows, and more sequences than workgroups under a gate of their own.
+NORM_ROUNDS = [
+    (3, 901, 1111, (901, 0, 640), "f32", "layer", "channel", True, True, True, 1.5),
+    (700, 4, 1030, (4, 0, 3, 1), "bf16", "layer", "sequence", True, True, True, 1.0),
+    (5, 500, 771, (500, 0, 499, 17, 500), "bf16", "rms", "token", True, True, False, 0.81),
+    (2, 1300, 1501, (1300, 1100), "bf16", "layer", "sequence", True, True, True, 1.0),
+    (1, 2300, 2501, None, "bf16", "layer", "none", False, True, True, 1.0),
+    (2, 1250, 2500, (1250, 1009), "bf16", "rms", "channel", True, False, True, 1.0),
+    (600, 4, 4096, (3, 4, 0), "f32", "layer", "sequence", False, True, True, 1.5),
+]
+
+
+@pytest.mark.parametrize("case", NORM_ROUNDS, ids=lambda c: "-".join(str(v) for v in c[:3]) + f"-{c[4]}-{c[6]}")
+def test_norm_rounds_of_rows(case):
+    test_norm(case)
+
+
+@pytest.mark.parametrize("case", NORM_ROUNDS, ids=lambda c: "-".join(str(v) for v in c[:3]) + f"-{c[4]}-{c[6]}")
+def test_norm_backward_rounds_of_rows(case):
+    test_norm_backward(case)
