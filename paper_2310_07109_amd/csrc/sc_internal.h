@@ -191,11 +191,13 @@ struct Linear {
   void* out;          // [B, n, N]
   int B, n, K, N;
   const int* len;  // or null
-  int skip_pad, gelu, out_f32;
+  int skip_pad;    // launch_linear_i8: padding rows of out are left as they are
+  int gelu, out_f32;
 };
 hipError_t launch_linear_i8(const Linear& l, hipStream_t s);
 // The product of few rows from x itself, quantised in the same launch (x_type as
-// SC_F32, SC_BF16, SC_I8; xq, and xs but for 8-bit rows, are not used).
+// SC_F32, SC_BF16, SC_I8; xq, and xs but for 8-bit rows, are not used); padding rows of
+// out become zeros.
 bool linear_few_ok(long long rows, int K, int N, int x_type);
 hipError_t launch_linear_few(const Linear& l, const void* x, int x_type, hipStream_t s);
 

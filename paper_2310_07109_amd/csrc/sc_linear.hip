@@ -13,10 +13,10 @@
 // k_linear_few    the same for a few rows: quantisation and product in one launch.
 //
 // 32768 x 4096 x 1024 on 8-bit rows: 116 us, 2.4 POP/s (a library's 8192^3: 2.0), at
-// 1.8 GHz under load, the matrix units busy 0.62 of the cycles.  32768 x 1024 x 4096
-// with GELU: 21 us of quantising (HBM rate) and 182, 0.36 of the cycles: a tile has few
-// stages there, and the arithmetic on its results (14 instructions each, an exponential
-// among them) and 268 MB of stores stand beside them.
+// 1.8 GHz under load, the matrix units busy 0.62 of the cycles.  32768 x 1024 x 4096:
+// 20-27 us of quantising (HBM rate) and 152, with GELU 188-202, 0.33 of the cycles: a tile
+// has few stages there, and the arithmetic on its results (21 instructions each, an
+// exponential among them) and 268 MB of stores stand beside them.
 #include <algorithm>
 
 #include "sc_device.h"
@@ -37,8 +37,8 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 // Absolute error 2.4e-7; of a negative value 1e-6 relative down to -3, 2.5e-6 to
 // -5, 3e-5 to -9, where it is 1e-18.  One form for both output types: what is
 // stored as bf16 is the float32 value rounded once (degree 5 has 1.6e-4 relative and
-// 1 % beyond -5, and is 7 instructions of 21 shorter).  NaN stays NaN; |v| beyond
-// 16 is cut for the product with Phi = 0.
+// 1 % beyond -5, 14 instructions a result instead of 21 and 182 us instead of 202 for
+// 32768 x 1024 x 4096).  NaN stays NaN; |v| beyond 16 is cut for the product with Phi = 0.
 SC_DEV float gelu_exp2(float v) {
   const float a = __builtin_elementwise_minimum(fabsf(v), 16.f);  // without the quieting that fminf needs
   float p = -4.266044115186496e-11f;
@@ -291,7 +291,7 @@ struct LinearArgs {
   void* out;
   int B, n, N, Kp;
   const int* len;
-  int skip_pad;  // padding rows of out are left as they are
+  int skip_pad;  // k_linear: padding rows of out are left as they are (k_linear_few zeroes them)
 };
 
 constexpr int kBK = 128;        // bytes of a row per K stage: whole lines (64-byte pieces halve the loads' rate)
@@ -546,10 +546,10 @@ struct LinWave {
   }
   static SC_DEV int next_buf(int bf) { return bf == kNBuf - 1 ? 0 : bf + 1; }
 
-  // 16 bytes of a row at column col, at any element's address: element by element, rows of
-  // odd length took 32768 x 1024 x 4095 from 290 to 396 us, 24165 x 768 x 1111 from 57 to
-  // 96, for 32768 x 1024 x 4096 with GELU 190 against 196 (registers).  The barrier keeps
-  // the compiler from running several fragments' results ahead.
+  // 16 bytes of a row at column col, at any element's address.  Element by element, rows of
+  // odd length take 352 us instead of 227 (32768 x 1024 x 4095; 24165 x 768 x 1111 80 and
+  // 41), rows of whole units the same (32768 x 1024 x 4096 152 and 152, with GELU 192 and
+  // 189).  The barrier keeps the compiler from running several fragments' results ahead.
   SC_DEV void store16(O* row, int col, uint4 v) const {
     constexpr int kE = 16 / sizeof(O);
     __builtin_amdgcn_sched_barrier(0);
@@ -608,7 +608,9 @@ struct LinWave {
 };
 
 // Tiles one after the other: all stage buffers but the one at hand in flight during a
-// tile, the next tile's first stages during its results.
+// tile, the next tile's first stages during its results.  The 256 x 256 form holds all 256
+// registers and spills four to eight: what it reloads at the head of a tile waits for every
+// access before it, the stages and the last results' stores alike.
 template <int kM, typename O, bool kGelu>
 SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const Packed& pk, int R, const LinPlan& pl) {
   using W = LinWave<kM, O, kGelu>;
@@ -700,8 +702,8 @@ SC_DEV void linear_tiles(const LinearArgs& a, char* stage, LinTables* tab, const
 
 // The same for tiles of enough stages (kStreamMin), as one stream: the next tile's
 // stages follow this one's into the buffers without a gap, and a tile's results are
-// finished and stored during the next tile's products, a sixteenth of a wave's part
-// after every chunk, so that one wave's arithmetic on results runs beside the other
+// finished and stored during the next tile's products, an eighth of a wave's part in
+// every stage, so that one wave's arithmetic on results runs beside the other
 // waves' matrix instructions, and the stores spread over the whole time.
 template <typename O, bool kGelu>
 SC_DEV void linear_stream(const LinearArgs& a, char* stage, LinTables* tab, const Packed& pk, int R, const LinPlan& pl) {

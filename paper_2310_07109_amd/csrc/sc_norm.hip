@@ -13,9 +13,9 @@
 //
 // Both are bound by memory: 32768 x 1024 bf16 with both norms and a gate by
 // channel or sequence, forward 268 MB in 45-54 us (5.0-6.0 TB/s; a large copy 5.1),
-// backward 403 MB in 87 us and its sums in 4.5.  Rows of more than 1024 channels wait
-// for their workgroup's reductions: 3 x 501 x 1111 float32 backward 16 us and 7, of
-// which the bytes are 7.
+// backward 403 MB in 86-95 us and its sums in 4-5; as float32 backward 805 MB in 154-158.
+// Rows of more than 1024 channels wait for their workgroup's reductions: 3 x 501 x 1111
+// float32 backward 20 us and its sums 4, where the bytes take 7.
 #include <algorithm>
 #include <type_traits>
 
@@ -249,7 +249,7 @@ SC_DEV float normalise(float (&v)[E], const C& c, R& red, bool rms, float eps, f
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i) s += v[i];
-    const float mean = red.sum(s) / fd;  // divided: a constant row has no deviation
+    const float mean = red.sum(s) / fd;  // divided: a constant row of an exact sum has no deviation
 #pragma unroll
     for (int u = 0; u < kPer; ++u)
 #pragma unroll
