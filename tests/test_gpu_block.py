@@ -952,3 +952,36 @@ def test_norm_rounds_of_rows(case):
 @pytest.mark.parametrize("case", NORM_ROUNDS, ids=lambda c: "-".join(str(v) for v in c[:3]) + f"-{c[4]}-{c[6]}")
 def test_norm_backward_rounds_of_rows(case):
     test_norm_backward(case)
+
+
+def test_linear_inputs_past_31_bits():
+    """8-bit rows and weights of more than 2^31 bytes: the last ones are those of a call of their own."""
+    n, K, N = 20000000, 128, 40
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    xq = torch.randint(-127, 128, (1, n, K), dtype=torch.int8, device=DEV, generator=g)
+    xs = torch.rand((1, n), device=DEV, generator=g)
+    wq = torch.randint(-127, 128, (N, K), dtype=torch.int8, device=DEV, generator=g)
+    one = torch.ones(N, device=DEV)
+
+    def rows(lo, hi):
+        d = sc.LinearDesc(1, hi - lo, K, N, x_dtype=sc.SC_I8)
+        return sc.sc_linear_i8(d, xq[:, lo:hi], wq, one, x_scale=xs[:, lo:hi])[0]
+    whole = rows(0, n)
+    for lo in (0, 2 ** 24 - 150, n - 300):
+        assert torch.equal(whole[lo:lo + 300], rows(lo, lo + 300)), lo
+    del whole, xq, xs
+    K, N = 131072, 20000
+    wq = torch.randint(-127, 128, (N, K), dtype=torch.int8, device=DEV, generator=g)
+    xq = torch.randint(-127, 128, (1, 3, K), dtype=torch.int8, device=DEV, generator=g)
+    ws = torch.rand(N, device=DEV, generator=g)
+
+    def cols(lo, hi):
+        d = sc.LinearDesc(1, 3, K, hi - lo, x_dtype=sc.SC_I8, out_dtype=sc.SC_F32)
+        return sc.sc_linear_i8(d, xq, wq[lo:hi], ws[lo:hi], x_scale=torch.ones((1, 3), device=DEV))[0]
+    whole = cols(0, N)
+    for lo in (0, 2 ** 14 - 50, N - 100):
+        part = cols(lo, lo + 100)
+        assert torch.equal(whole[:, lo:lo + 100], part), lo
+        acc = (xq[0].double() @ wq[lo:lo + 100].double().t()).float()
+        assert torch.equal(part, acc * ws[lo:lo + 100]), lo
