@@ -15,7 +15,9 @@ SC_NOALLOC_SCRATCH_BYTES = 16 << 20
 # bits of sc_validate_desc's result
 SC_VALID_LEN, SC_VALID_POS_RANGE, SC_VALID_POS_ORDER, SC_VALID_POS_UNUSED_FIRST = 1, 2, 4, 8
 SC_F32, SC_BF16, SC_I8 = 0, 1, 2
-SC_ACT_NONE, SC_ACT_GELU = 0, 1
+SC_ACT_NONE, SC_ACT_GELU, SC_ACT_SILU = 0, 1, 2
+SC_ROTARY_HALF, SC_ROTARY_INTERLEAVED = 0, 1
+SC_ROTARY_PLAIN, SC_ROTARY_LINEAR, SC_ROTARY_BASE, SC_ROTARY_BANDS = 0, 1, 2, 3
 SC_NORM_LAYER, SC_NORM_RMS = 0, 1
 SC_GATE_NONE, SC_GATE_CHANNEL, SC_GATE_SEQUENCE, SC_GATE_TOKEN = 0, 1, 2, 3
 SC_SCORE_FROM_PARTIALS, SC_SCORE_FROM_BAND_PROBS = 0, 1
@@ -59,6 +61,25 @@ class _LayerI8(ctypes.Structure):
         [(name, ctypes.c_void_p) for name in ("gate1", "ln1_w", "ln1_b", "gate2", "ln2_w", "ln2_b")]
 
 
+class _RotaryDesc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("B", "n", "Hq", "Hk", "d")] + \
+        [("valid_len", ctypes.c_void_p)] + \
+        [(name, ctypes.c_int32) for name in ("rot_dim", "layout", "norm", "kind")] + \
+        [("eps", ctypes.c_float), ("amplitude", ctypes.c_float), ("dtype", ctypes.c_int32)] + \
+        [(name, ctypes.c_int64) for name in ("q_stride", "k_stride", "v_stride")]
+
+
+class _FfnDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("n", ctypes.c_int32), ("D", ctypes.c_int32), ("F", ctypes.c_int32),
+                ("valid_len", ctypes.c_void_p), ("act", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class _DropoutDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("n", ctypes.c_int32), ("D", ctypes.c_int32), ("valid_len", ctypes.c_void_p),
+                ("p", ctypes.c_double), ("res_scale", ctypes.c_float), ("site", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -89,6 +110,8 @@ def _open(path):
     L = ctypes.CDLL(path)
     vp, sz, i32, f32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.c_float
     dp, lp, np_ = ctypes.POINTER(_Desc), ctypes.POINTER(_LinearDesc), ctypes.POINTER(_NormDesc)
+    f64 = ctypes.c_double
+    rp, fp, op = ctypes.POINTER(_RotaryDesc), ctypes.POINTER(_FfnDesc), ctypes.POINTER(_DropoutDesc)
     sig = {
         "sc_status_str": (ctypes.c_char_p, [i32]),
         "sc_score_partials_size": (sz, [dp]),
@@ -119,6 +142,16 @@ def _open(path):
         "sc_block_norm": (i32, [np_] + 12 * [vp]),
         "sc_block_norm_backward_workspace_size": (sz, [np_]),
         "sc_block_norm_backward": (i32, [np_] + 17 * [vp] + [sz, vp]),
+        "sc_rotary_frequencies": (i32, [i32, f64, i32, f64, f64, f64, f64, vp, vp]),
+        "sc_rotary": (i32, [rp] + 11 * [vp]),
+        "sc_rotary_backward_workspace_size": (sz, [rp]),
+        "sc_rotary_backward": (i32, [rp] + 15 * [vp] + [sz, vp]),
+        "sc_gated_ffn_workspace_size": (sz, [fp, i32]),
+        "sc_gated_ffn_saved_size": (sz, [fp]),
+        "sc_gated_ffn": (i32, [fp] + 7 * [vp] + [sz, vp]),
+        "sc_gated_ffn_backward_workspace_size": (sz, [fp]),
+        "sc_gated_ffn_backward": (i32, [fp] + 11 * [vp] + [sz, vp]),
+        "sc_dropout": (i32, [op] + 5 * [vp]),
         "sc_profile_window_kernel": (i32, [i32]),
         "sc_profile_window_kernel_read": (i32, [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double),
                                                  ctypes.c_int64, ctypes.POINTER(ctypes.c_int64)]),

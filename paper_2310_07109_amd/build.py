@@ -14,13 +14,13 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libsc.so")
 # the same library with SC_DEBUG: device-side argument checks and a synchronisation per call (include/sc.h)
 DEBUG_OUT = os.path.join(HERE, "libsc_debug.so")
-DEBUG_SOURCES = ["sc_api.hip", "sc_block_api.hip"]  # the sources that SC_DEBUG changes
+DEBUG_SOURCES = ["sc_api.hip", "sc_block_api.hip", "sc_layer_api.hip"]  # the sources that SC_DEBUG changes
 # the VALU issue-rate probe behind the roofline figures (bench.py --probe-valu), a library of its own
 PROBE_OUT = os.path.join(HERE, "libsc_probe.so")
 PROBE_SOURCES = ["probe_valu.hip", "probe_lds.hip"]
 BUILD_DIR = os.path.join(HERE, "_build")
-SOURCES = ["sc_attention.hip", "sc_prune.hip", "sc_stack.hip", "sc_backward.hip", "sc_linear.hip", "sc_norm.hip", "sc_api.hip",
-           "sc_block_api.hip"]
+SOURCES = ["sc_attention.hip", "sc_prune.hip", "sc_stack.hip", "sc_backward.hip", "sc_linear.hip", "sc_norm.hip", "sc_rotary.hip",
+           "sc_ffn.hip", "sc_ffn_backward.hip", "sc_dropout.hip", "sc_api.hip", "sc_block_api.hip", "sc_layer_api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = [

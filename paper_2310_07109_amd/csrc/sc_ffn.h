@@ -1,0 +1,550 @@
+// The tiled matrix products of the gated feed-forward block, forward and backward.
+//
+// Six products, one form.  The contraction of an operand lies along its rows in memory
+// (x . Wd^T) or across them (x . W, x^T . g): both are staged as they lie, in whole lines,
+// by direct loads, and the second kind is transposed on the way from LDS to the fragments
+// (ds_read_b64_tr_b16), so no operand is ever laid out anew.
+//
+//   kGate  g = x Wg, u = x Wu     h = act(g) u; g and u kept for the backward
+//   kDown  y = h Wd
+//   kDh    dh = dy Wd^T           dg = dh u act'(g), du = dh act(g)
+//   kDx    dx = dg Wg^T + du Wu^T, one sum over 2 F
+//   kDwd   dWd = h^T dy           over the rows, in slabs
+//   kDwgu  dWg = x^T dg, dWu = x^T du
+//
+// A tile is BM x BN of a workgroup of eight waves; a stage is 64 of the contraction.
+// Sums are float32 in ascending order of the contraction, whatever the tile.
+#pragma once
+#include "sc_act.h"
+#include "sc_device.h"
+#include "sc_internal.h"
+#include "sc_pack.h"
+
+namespace sc {
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+struct u32x3 {  // 12 bytes at any dword (a vector type of three takes 16)
+  unsigned w[3];
+};
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+typedef __attribute__((ext_vector_type(2), aligned(2))) unsigned u32x2_any;
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+
+constexpr int kGate = 0, kDown = 1, kDh = 2, kDx = 3, kDwd = 4, kDwgu = 5;
+constexpr int kFfnWgs = 256;   // one workgroup per CU, each taking tiles in turn
+constexpr int kGroupTiles = 8;  // row tiles that share weights in an XCD's L2
+
+template <int kM>
+struct FfnTile;
+template <>
+struct FfnTile<0> { static constexpr int kBM = 256, kBN = 256, kWgM = 2, kWgN = 4, kNBuf = 2; };
+template <>
+struct FfnTile<1> { static constexpr int kBM = 128, kBN = 128, kWgM = 2, kWgN = 4, kNBuf = 4; };
+template <>
+struct FfnTile<2> { static constexpr int kBM = 64, kBN = 64, kWgM = 4, kWgN = 2, kNBuf = 4; };
+
+// One operand: rows of ld bytes.  Those whose row count is the batch's come packed (the
+// valid rows, one after the other) or, when no row is padding, from where they are.
+struct FfnOperand {
+  const char* p[2];
+  const char* packed;  // instead of p[0] when rows are padding, or null
+  unsigned ld;
+  int rows;            // 0: the valid rows
+};
+
+struct FfnArgs {
+  FfnOperand a, b;
+  const int* map;    // packed row -> row of the batch (null: the same)
+  const int* count;  // the number of valid rows (null: T)
+  int T;
+  int M, N, K;       // output rows (kDwd, kDwgu), columns, contraction (not kDwd, kDwgu)
+  int map_a;         // a's rows are the batch's: read through map
+  void* out[2];      // bf16: h | y | dg, du | dx | dwd | dwg, dwu
+  int ld;            // elements of its rows
+  char* frags;       // kGate: g and u as fragments, or null; kDh: to read
+  int frag_cols;     // fragments of a row of fragments
+  float* part;       // kDwd, kDwgu: sums of the slabs (one slab: null)
+  int slabs;
+};
+
+// -------------------------------------------------------------- loads ----
+// One direct load of 16 bytes a lane through a buffer descriptor: zeros beyond its end.
+SC_DEV void lds_dma16_buf(u32x4 rsrc, unsigned voff, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+               :
+               : "v"(voff), "s"(rsrc), "s"(lds)
+               : "memory", "m0");
+}
+constexpr unsigned kBeyond = 0xfffff000u;  // an offset beyond every descriptor's end
+
+// A descriptor of `bytes` from p + skip on (skip <= bytes), in scalar registers.
+SC_DEV u32x4 descriptor(const char* p, unsigned bytes, unsigned skip) {
+  const unsigned long long at = uniform64((unsigned long long)(size_t)p + skip);
+  return u32x4{(unsigned)at, (unsigned)(at >> 32), (unsigned)__builtin_amdgcn_readfirstlane((int)(bytes - skip)),
+               0x00027000u};
+}
+
+// Contraction along the rows: 128 bytes a row and stage, 16-byte units swizzled by bits
+// 1-3 of the row; lane l reads unit l / 16 of row l % 16.
+SC_DEV int row_off(int row, int unit) { return row * 128 + 16 * (unit ^ ((row >> 1) & 7)); }
+
+// Contraction across the rows: 64 rows of kUnits 16-byte units.  A transposing read
+// touches, in 32 lanes, rows 0-3 and 8-11 and two units of each; the order of the units
+// spreads these over all banks.
+template <int kUnits>
+SC_DEV int col_swz(int k) {
+  if constexpr (kUnits >= 16) return 2 * (k & 3) | (k & 8);
+  else if constexpr (kUnits == 8) return (k & 2) | ((k & 8) >> 1);
+  else return (k & 8) >> 2;
+}
+
+// An operand's part of a stage: kSpan rows of 64 (kAcross: 64 rows of kSpan), a wave's
+// share of the loads and its fragments.  kSubs: the operand is that many matrices side by
+// side, kSpan / kSubs columns of each.
+template <bool kAcross, int kSpan, int kWave, int kSubs>
+struct FfnPart {
+  static constexpr int kLoads = kSpan / 64, kBytes = kSpan * 128;
+  static constexpr int kCols = kSpan / kSubs, kUnits = kCols / 8, kPitch = 2 * kCols;
+  static constexpr int kFrags = kWave / 16, kSubFrags = kFrags / kSubs;
+  static constexpr int kSubLoads = kSpan / 8 / kSubs;  // of the eight waves, a matrix
+  unsigned voff[kLoads];
+  unsigned fa;   // address of the first fragment in the part
+
+  // Which load (of a matrix) a wave's t-th is, and of which matrix.
+  static SC_DEV int load_sub(int w, int t) { return kSubs == 1 ? 0 : (8 * t + w) / kSubLoads; }
+  static SC_DEV int load_at(int w, int t) { return kAcross ? (8 * t + w) % kSubLoads : kLoads * w + t; }
+
+  SC_DEV void init(int lane, int wave_at) {  // wave_at: the wave's first row or column (of a matrix)
+    const int g = lane >> 4;
+    if constexpr (!kAcross) {
+      fa = row_off(wave_at + (lane & 15), g);
+    } else {
+      const int r = (lane >> 2) & 3, k = 8 * g + r, u = wave_at / 8 + ((lane & 3) >> 1);
+      fa = k * kPitch + 16 * (u ^ col_swz<kUnits>(k)) + 8 * (lane & 1);
+    }
+  }
+  // Offsets of a tile whose first row or column is `first`; row(i): bytes to its i-th row.
+  template <typename Row>
+  SC_DEV void offsets(int lane, int w, int first, unsigned ld, Row row) {
+#pragma unroll
+    for (int t = 0; t < kLoads; ++t) {
+      if constexpr (!kAcross) {
+        const int r = 8 * load_at(w, t) + (lane >> 3);
+        voff[t] = row(first + r) + 16u * ((lane & 7) ^ ((r >> 1) & 7));
+      } else {
+        const int k = load_at(w, t) * (64 / kUnits) + lane / kUnits;
+        voff[t] = (unsigned)k * ld + 2u * first + 16u * ((lane % kUnits) ^ col_swz<kUnits>(k));
+      }
+    }
+  }
+  // kAlong with a contraction that ends inside the stage: units from `limit` on are zeros.
+  SC_DEV void issue(const u32x4 (&rsrc)[kSubs], unsigned lds, int lane, int w, int limit) const {
+#pragma unroll
+    for (int t = 0; t < kLoads; ++t) {
+      unsigned v = voff[t];
+      if constexpr (!kAcross) {
+        const int r = 8 * load_at(w, t) + (lane >> 3), unit = (lane & 7) ^ ((r >> 1) & 7);
+        if (limit < 8) v = unit < limit ? v : kBeyond;
+      }
+      const int sub = load_sub(w, t);
+      u32x4 d = rsrc[0];
+      if constexpr (kSubs == 2) d = sub ? rsrc[1] : rsrc[0];
+      lds_dma16_buf(d, v, lds + (unsigned)(sub * 128 * kCols + load_at(w, t) * 1024));
+    }
+  }
+  // Fragment i of chunk c (32 of the stage's 64) of the part at LDS address `lds`.
+  SC_DEV bf16x8 frag(unsigned lds, int i, int c) const {
+    if constexpr (!kAcross) {
+      return lds_read16(((fa ^ (64u * c)) + lds) + i * 2048);
+    } else {
+      const int sub = i / kSubFrags, j = i % kSubFrags;
+      const unsigned at = lds + (fa ^ (32u * j)) + sub * 128 * kCols + c * 32 * kPitch;
+      const i16x4 lo = lds_read_tr16(at), hi = lds_read_tr16(at + 4 * kPitch);
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+};
+
+// ------------------------------------------------------------ results ----
+// 24 of a float32's bits: four of them in three words, and back.
+SC_DEV u32x3 pack24(const f32x4& v) {
+  const u32x4 u = __builtin_bit_cast(u32x4, v);
+  return u32x3{{__builtin_amdgcn_perm(u[1], u[0], 0x05030201u), __builtin_amdgcn_perm(u[2], u[1], 0x06050302u),
+                __builtin_amdgcn_perm(u[3], u[2], 0x07060503u)}};
+}
+SC_DEV f32x4 unpack24(const u32x3& v) {
+  const u32x4 u = {v.w[0] << 8, __builtin_amdgcn_perm(v.w[1], v.w[0], 0x0504030cu),
+                   __builtin_amdgcn_perm(v.w[2], v.w[1], 0x0403020cu), v.w[2] & 0xffffff00u};
+  return __builtin_bit_cast(f32x4, u);
+}
+// Fragment (ri, ci) of g (which = 0) or u (1): a lane's four results as pack24 gives them.
+SC_DEV char* frag_at(char* frags, int cols, int ri, int ci, int which, int lane) {
+  return frags + ((((long long)ri * cols + ci) * 2 + which) * 64 + lane) * 12;
+}
+
+// Up to kCount bf16 values of a row from column col on, those below N, at any address.
+template <int kCount>
+SC_DEV void store_row(__bf16* row, int col, int N, const unsigned (&v)[kCount / 2]) {
+  if (col + kCount <= N) {
+    if constexpr (kCount == 8) *reinterpret_cast<u32x4_any*>(row + col) = u32x4_any{v[0], v[1], v[2], v[3]};
+    else *reinterpret_cast<u32x2_any*>(row + col) = u32x2_any{v[0], v[1]};
+  } else {
+#pragma unroll
+    for (int q = 0; q < kCount - 1; ++q)
+      if (col + q < N) row[col + q] = __builtin_bit_cast(__bf16, (unsigned short)(v[q / 2] >> (16 * (q & 1))));
+  }
+}
+// Two fragments of 16 columns from column c on: a lane holds columns 4 g to 4 g + 3 of
+// each; exchanged between neighbouring groups, 8 of one.
+SC_DEV void store_pair(__bf16* row, int c, int N, int g, const f32x4& a, const f32x4& b, bool on) {
+  const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16(a[0], a[1]), pack_bf16(b[0], b[1]), false, false);
+  const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16(a[2], a[3]), pack_bf16(b[2], b[3]), false, false);
+  const unsigned v[4] = {(unsigned)lo[0], (unsigned)hi[0], (unsigned)lo[1], (unsigned)hi[1]};
+  if (on) store_row<8>(row, c + 16 * (g & 1) + 8 * (g >> 1), N, v);
+}
+SC_DEV void store_one(__bf16* row, int c, int N, int g, const f32x4& a, bool on) {
+  const unsigned v[2] = {pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
+  if (on) store_row<4>(row, c + 4 * g, N, v);
+}
+
+// --------------------------------------------------------------- tile ----
+template <int kKind, int kM, int kAct>
+struct FfnProduct {
+  using S = FfnTile<kM>;
+  static constexpr int BM = S::kBM, BN = S::kBN, kNBuf = S::kNBuf;
+  static constexpr int WM = BM / S::kWgM, WN = BN / S::kWgN, FI = WM / 16, FJ = WN / 16;
+  static constexpr bool kOverRows = kKind == kDwd || kKind == kDwgu;  // contraction over the batch's rows
+  static constexpr bool kAcrossA = kOverRows, kAcrossB = kOverRows || kKind == kGate || kKind == kDown;
+  static constexpr int kSubs = kKind == kGate ? 2 : 1;
+  static constexpr int kH = FI >= 2 ? 2 : 1, FH = FI / kH;  // a wave's rows go in halves
+  using A = FfnPart<kAcrossA, BM, WM, 1>;
+  using B = FfnPart<kAcrossB, BN, WN, kSubs>;
+  static constexpr int kStage = A::kBytes + B::kBytes, kDma = A::kLoads + B::kLoads;
+
+  const FfnArgs& p;
+  const int R, lane, w, g, lr, wm, wn;
+  const unsigned lds0;
+  A a;
+  B b;
+  f32x4 acc[FI][FJ];
+  bf16x8 xf[2][FH], wf[2][FJ];
+  // the tile
+  int m0, n0, sel, slab, k0, ns, seg;  // sel: of two outputs; k0: first stage; ns: stages, of which a segment has seg
+  const char *pa[2], *pb[2];
+  unsigned bytes_a, bytes_b;
+
+  SC_DEV FfnProduct(const FfnArgs& args, char* stage, int rows)
+      : p(args), R(rows), lane(threadIdx.x & 63), w(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), g(lane >> 4),
+        lr(lane & 15), wm(w / S::kWgN * WM), wn(w % S::kWgN * (WN / kSubs)), lds0(lds_addr(stage)) {
+    a.init(lane, wm);
+    b.init(lane, wn);
+    const bool whole = R == p.T;
+    pa[0] = !whole && p.a.packed ? p.a.packed : p.a.p[0];
+    pb[0] = !whole && p.b.packed ? p.b.packed : p.b.p[0];
+    pa[1] = p.a.p[1];
+    pb[1] = p.b.p[1];
+    bytes_a = (unsigned)(p.a.rows ? p.a.rows : R) * p.a.ld;
+    bytes_b = (unsigned)(p.b.rows ? p.b.rows : R) * p.b.ld;
+  }
+  SC_DEV int rows() const { return kOverRows ? p.M : R; }
+  SC_DEV int tiles_n() const {
+    constexpr int bn = BN / kSubs;
+    return (p.N + bn - 1) / bn * (both() ? 2 : 1);
+  }
+  SC_DEV bool both() const { return kKind == kDwgu && p.out[0] && p.out[1]; }
+  SC_DEV long long items() const {
+    return (long long)((rows() + BM - 1) / BM) * tiles_n() * (kOverRows ? p.slabs : 1);
+  }
+  // Tiles in groups of kGroupTiles row tiles by all column tiles.
+  SC_DEV void place(long long item) {
+    const int T = (rows() + BM - 1) / BM, Nt = tiles_n();
+    slab = kOverRows ? __builtin_amdgcn_readfirstlane((int)(item / ((long long)T * Nt))) : 0;
+    const int it = __builtin_amdgcn_readfirstlane((int)(item - (long long)slab * T * Nt));
+    const int per = kGroupTiles * Nt, gi = it / per, rem = it - gi * per, gs = min(kGroupTiles, T - gi * kGroupTiles);
+    m0 = (gi * kGroupTiles + rem % gs) * BM;
+    int nt = rem / gs;
+    sel = 0;
+    if constexpr (kKind == kDwgu) {
+      sel = both() ? nt >= Nt / 2 : p.out[0] == nullptr;
+      if (both() && sel) nt -= Nt / 2;
+    }
+    n0 = nt * (BN / kSubs);
+    if constexpr (kOverRows) {
+      const int all = (R + 63) / 64;
+      k0 = (int)((long long)all * slab / p.slabs);
+      ns = (int)((long long)all * (slab + 1) / p.slabs) - k0;
+      seg = ns;
+    } else {
+      k0 = 0;
+      seg = (p.K + 63) / 64;
+      ns = kKind == kDx ? 2 * seg : seg;
+    }
+    m0 = __builtin_amdgcn_readfirstlane(m0);
+    n0 = __builtin_amdgcn_readfirstlane(n0);
+    const int M = rows(), N = p.N;
+    a.offsets(lane, w, m0, p.a.ld, [&](int r) {
+      int row = min(r, M - 1);
+      if (p.map_a) row = p.map[row];
+      return (unsigned)row * p.a.ld;
+    });
+    b.offsets(lane, w, n0, p.b.ld, [&](int r) { return (unsigned)min(r, N - 1) * p.b.ld; });
+  }
+  SC_DEV void issue(int s, int bf) const {
+    const unsigned at = lds0 + (unsigned)bf * kStage;
+    const int second = kKind == kDx && s >= seg, ks = k0 + (second ? s - seg : s);
+    const int limit = kOverRows || ks < seg - 1 ? 8 : (p.K - 64 * ks + 7) / 8;  // units of the stage (operands along the rows)
+    const unsigned skip_a = kAcrossA ? (unsigned)ks * 64 * p.a.ld : (unsigned)ks * 128;
+    const unsigned skip_b = kAcrossB ? (unsigned)ks * 64 * p.b.ld : (unsigned)ks * 128;
+    const u32x4 ra[1] = {descriptor(pa[second], bytes_a, skip_a)};
+    a.issue(ra, at, lane, w, limit);
+    if constexpr (kSubs == 2) {
+      const u32x4 rb[2] = {descriptor(pb[0], bytes_b, skip_b), descriptor(pb[1], bytes_b, skip_b)};
+      b.issue(rb, at + A::kBytes, lane, w, limit);
+    } else {
+      const u32x4 rb[1] = {descriptor(pb[kKind == kDwgu ? sel : second], bytes_b, skip_b)};
+      b.issue(rb, at + A::kBytes, lane, w, limit);
+    }
+  }
+  SC_DEV void cols(int q, int bf, int c) {
+    const unsigned at = lds0 + (unsigned)bf * kStage + A::kBytes;
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) wf[q][j] = b.frag(at, j, c);
+  }
+  SC_DEV void rows(int q, int bf, int c, int h) {
+    const unsigned at = lds0 + (unsigned)bf * kStage;
+#pragma unroll
+    for (int i = 0; i < FH; ++i) xf[q][i] = a.frag(at, h * FH + i, c);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  SC_DEV void mul(int h, int qx, int qw) {
+#pragma unroll
+    for (int i = 0; i < FH; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j)
+        acc[h * FH + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[qw][j], xf[qx][i], acc[h * FH + i][j], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  static SC_DEV int next_buf(int bf) { return bf == kNBuf - 1 ? 0 : bf + 1; }
+
+  // The tile's sums.  Every half's fragments are in flight during the products of the one
+  // before, across stages too; one barrier a stage, before its last products: the next
+  // stage has landed, and every wave holds its last fragments of this one, whose buffer is
+  // refilled.
+  SC_DEV void sums() {
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (kOverRows && ns == 0) return;
+    wait_vm<0>();
+    __syncthreads();
+    int bf = 0;
+    cols(0, 0, 0);
+    rows(0, 0, 0, 0);
+    for (int s = 0; s < ns; ++s) {
+      const int bn = next_buf(bf);
+#pragma unroll
+      for (int q = 0; q < 2 * kH; ++q) {
+        const int nq = q + 1;
+        if (nq < 2 * kH) {
+          if (nq == kH) cols(1, bf, 1);
+          rows(nq & 1, bf, nq / kH, nq % kH);
+        } else if (s + 1 < ns) {
+          wait_stages<kNBuf - 1, kDma>(min(ns - 2 - s, kNBuf - 2));
+          __syncthreads();
+          if (s + kNBuf < ns) issue(s + kNBuf, bf);
+          cols(0, bn, 0);
+          rows(0, bn, 0, 0);
+        }
+        mul(q % kH, q & 1, q / kH);
+      }
+      bf = bn;
+    }
+  }
+  SC_DEV void start() {
+#pragma unroll
+    for (int s = 0; s < kNBuf; ++s)
+      if (s < ns) issue(s, s);
+  }
+
+  // Element e of a lane: row 16 i + lr, column 16 j + 4 g + e.
+  SC_DEV void emit_h(int i) const {
+    constexpr int J = FJ / 2;
+    const int r = m0 + wm + 16 * i + lr, c = n0 + wn;
+    const bool on = r < R;
+    __bf16* row = static_cast<__bf16*>(p.out[0]) + (long long)r * p.ld;
+    f32x4 h[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const f32x4 gt = acc[i][j], up = acc[i][J + j];
+      if (p.frags && m0 + wm + 16 * i < R && c + 16 * j < 16 * p.frag_cols) {
+        const int ri = (m0 + wm) / 16 + i, ci = c / 16 + j;
+        *reinterpret_cast<u32x3*>(frag_at(p.frags, p.frag_cols, ri, ci, 0, lane)) = pack24(gt);
+        *reinterpret_cast<u32x3*>(frag_at(p.frags, p.frag_cols, ri, ci, 1, lane)) = pack24(up);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[j][e] = act<kAct>(gt[e]) * up[e];
+    }
+    if constexpr (J == 1) {
+      store_one(row, c, p.N, g, h[0], on);
+    } else {
+#pragma unroll
+      for (int j = 0; j < J; j += 2) store_pair(row, c + 16 * j, p.N, g, h[j], h[j + 1], on);
+    }
+  }
+  SC_DEV void emit_dh(int i) const {
+    const int r = m0 + wm + 16 * i + lr, c = n0 + wn;
+    const bool on = r < R;
+    __bf16* dg = static_cast<__bf16*>(p.out[0]) + (long long)r * p.ld;
+    __bf16* du = static_cast<__bf16*>(p.out[1]) + (long long)r * p.ld;
+#pragma unroll
+    for (int j = 0; j < FJ; j += 2) {
+      f32x4 vg[2], vu[2];
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        u32x3 sg = {{0, 0, 0}}, su = {{0, 0, 0}};
+        if (m0 + wm + 16 * i < R && c + 16 * (j + f) < 16 * p.frag_cols) {
+          const int ri = (m0 + wm) / 16 + i, ci = c / 16 + j + f;
+          sg = *reinterpret_cast<const u32x3*>(frag_at(p.frags, p.frag_cols, ri, ci, 0, lane));
+          su = *reinterpret_cast<const u32x3*>(frag_at(p.frags, p.frag_cols, ri, ci, 1, lane));
+        }
+        const f32x4 gt = unpack24(sg), up = unpack24(su);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float slope;
+          const float v = act_slope<kAct>(gt[e], slope), dh = acc[i][j + f][e];
+          vg[f][e] = dh * up[e] * slope;
+          vu[f][e] = dh * v;
+        }
+      }
+      store_pair(dg, c + 16 * j, p.N, g, vg[0], vg[1], on);
+      store_pair(du, c + 16 * j, p.N, g, vu[0], vu[1], on);
+    }
+  }
+  SC_DEV void emit_rows(int i) const {  // kDown, kDx, kDwd, kDwgu
+    const int r = m0 + wm + 16 * i + lr, c = n0 + wn;
+    const bool on = r < rows();
+    if constexpr (kOverRows) {
+      if (p.part) {
+        float* part = p.part + ((long long)sel * p.slabs + slab) * p.M * p.N + (long long)r * p.N;
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) {
+          const int col = c + 16 * j + 4 * g;
+          if (!on) continue;
+          if (col + 4 <= p.N) {
+            *reinterpret_cast<f32x4_any*>(part + col) = acc[i][j];
+          } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+              if (col + e < p.N) part[col + e] = acc[i][j][e];
+          }
+        }
+        return;
+      }
+    }
+    long long at = r;
+    if (!kOverRows && p.map && on) at = p.map[r];
+    __bf16* row = static_cast<__bf16*>(p.out[sel]) + at * p.ld;
+#pragma unroll
+    for (int j = 0; j < FJ; j += 2) store_pair(row, c + 16 * j, p.N, g, acc[i][j], acc[i][j + 1], on);
+  }
+  SC_DEV void results() const {
+#pragma unroll
+    for (int i = 0; i < FI; ++i) {
+      if constexpr (kKind == kGate) emit_h(i);
+      else if constexpr (kKind == kDh) emit_dh(i);
+      else emit_rows(i);
+    }
+  }
+};
+
+template <int kKind, int kM, int kAct>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_ffn(FfnArgs a) {
+  using P = FfnProduct<kKind, kM, kAct>;
+  __shared__ __attribute__((aligned(1024))) char stage[P::kNBuf * P::kStage];
+  const int R = a.count ? __builtin_amdgcn_readfirstlane(a.count[0]) : a.T;
+  P p(a, stage, R);
+  // The tiles go to the XCDs in contiguous ranges (workgroup i runs on XCD i % 8): what an
+  // XCD runs at a time shares rows and weights in its L2.
+  const long long items = p.items();
+  const int xcd = blockIdx.x & 7, step = gridDim.x >> 3;
+  const long long last = items * (xcd + 1) / 8;
+  for (long long it = items * xcd / 8 + (blockIdx.x >> 3); it < last; it += step) {
+    p.place(it);
+    __syncthreads();  // the last tile's stages are read
+    p.start();
+    p.sums();
+    p.results();
+  }
+}
+
+template <int kKind, int kM, int kAct>
+hipError_t run_ffn(const FfnArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((k_ffn<kKind, kM, kAct>), dim3(kFfnWgs), dim3(512), 0, s, a);
+  return hipGetLastError();
+}
+// The tile by the number of tiles that the largest one leaves.
+template <int kKind, int kAct>
+hipError_t run_ffn(const FfnArgs& a, long long rows, long long cols, hipStream_t s) {
+  const long long slabs = a.slabs > 1 ? a.slabs : 1;
+  auto tiles = [&](int m) { return (rows + m - 1) / m * ((cols + m - 1) / m) * slabs; };
+  if (tiles(256) >= kFfnWgs) return run_ffn<kKind, 0, kAct>(a, s);
+  if (tiles(128) >= kFfnWgs / 2) return run_ffn<kKind, 1, kAct>(a, s);
+  return run_ffn<kKind, 2, kAct>(a, s);
+}
+
+// -------------------------------------------------------------- sizes ----
+inline int up8(int v) { return (v + 7) / 8 * 8; }
+// Widths that direct loads of 16 bytes cannot take: those tensors are copied to rows
+// rounded up to 8, zeros behind.
+inline bool ffn_odd(const Ffn& a) { return a.D % 8 != 0 || a.F % 8 != 0; }
+
+struct FfnSaved {
+  char* h;      // [valid rows, Fp] bf16
+  char* frags;  // g and u
+  size_t bytes;
+};
+inline FfnSaved ffn_saved(const Ffn& a, void* base) {
+  const size_t T = (size_t)a.B * a.n, Fp = up8(a.F);
+  FfnSaved s;
+  s.h = static_cast<char*>(base);
+  const size_t h = (T * Fp * 2 + 255) / 256 * 256;
+  s.frags = s.h + h;
+  s.bytes = h + (T + 15) / 16 * ((Fp + 15) / 16) * 2 * 768;
+  return s;
+}
+
+struct FfnCarve {
+  char* base;
+  size_t off = 0;
+  char* take(size_t bytes) {
+    char* p = base ? base + off : nullptr;
+    off += (bytes + 255) / 256 * 256;
+    return p;
+  }
+};
+
+// What stands before the products: the numbering of the valid rows, zeros into the
+// padding rows of an output, and the copies.
+struct FfnCopy {
+  const char* src;
+  char* dst;
+  int rows, cols, pitch;  // elements; rows 0: the batch's valid rows
+};
+struct FfnRows {
+  const int* len;
+  int B, n;
+  int* map;    // null without lengths
+  int* count;
+  char* zero;  // rows of zero_bytes whose padding ones are zeroed, or null
+  long long zero_bytes;
+  int always;  // the batch's rows are copied even if none is padding
+  int copies;
+  FfnCopy copy[5];
+};
+}  // namespace
+
+hipError_t launch_ffn_rows(const void* rows, hipStream_t s);  // an FfnRows
+
+}  // namespace sc

@@ -1,0 +1,201 @@
+// The gated feed-forward block, backward (the products are in sc_ffn.h).
+#include <algorithm>
+
+#include "sc_ffn.h"
+
+namespace sc {
+namespace {
+
+struct BackwardWs {
+  int *count, *map;
+  char *x, *dy, *w[3], *dg, *du;
+  float *part_d, *part_gu;
+};
+
+// Slabs of the rows that a weight gradient's sum is cut into: as many as give every
+// workgroup a tile, of 512 rows at least.
+int slabs_of(const Ffn& a, int mats) {
+  const long long T = (long long)a.B * a.n;
+  auto tiles = [&](long long m) { return (a.D + m - 1) / m * ((a.F + m - 1) / m) * mats; };
+  const long long t = tiles(256);
+  return (int)std::max<long long>(1, std::min<long long>(kFfnWgs / std::max<long long>(t, 1), T / 512));
+}
+
+size_t carve(const Ffn& a, void* base, BackwardWs* out) {
+  const size_t T = (size_t)a.B * a.n, Dp = up8(a.D), Fp = up8(a.F), DF = (size_t)a.D * a.F;
+  FfnCarve c{static_cast<char*>(base)};
+  BackwardWs s = {};
+  if (a.len) {
+    s.count = reinterpret_cast<int*>(c.take(4));
+    s.map = reinterpret_cast<int*>(c.take(4 * T));
+  }
+  if (a.len || ffn_odd(a)) {
+    s.x = c.take(T * Dp * 2);
+    s.dy = c.take(T * Dp * 2);
+  }
+  if (ffn_odd(a)) {
+    s.w[0] = c.take(a.D * Fp * 2);
+    s.w[1] = c.take(a.D * Fp * 2);
+    s.w[2] = c.take(a.F * Dp * 2);
+  }
+  s.dg = c.take(T * Fp * 2);
+  s.du = c.take(T * Fp * 2);
+  const int sd = slabs_of(a, 1), sg = slabs_of(a, 2);
+  if (sd > 1) s.part_d = reinterpret_cast<float*>(c.take(4 * DF * sd));
+  if (sg > 1) s.part_gu = reinterpret_cast<float*>(c.take(4 * DF * 2 * sg));
+  if (out) *out = s;
+  return c.off;
+}
+
+// The slabs' sums, in order, rounded once: up to three gradients of `count` elements.
+struct SlabSums {
+  const float* part[3];
+  __bf16* out[3];
+  int slabs[3];
+  long long count;
+};
+__global__ __launch_bounds__(256) void k_ffn_slabs(SlabSums a) {
+  const int m = blockIdx.y;
+  const float* p = a.part[m];
+  __bf16* o = a.out[m];
+  if (!o) return;
+  const long long step = (long long)gridDim.x * 1024;
+  for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4; i < a.count; i += step) {
+    if (i + 4 <= a.count) {
+      f32x4 s = *reinterpret_cast<const f32x4_any*>(p + i);
+      for (int k = 1; k < a.slabs[m]; ++k) s += *reinterpret_cast<const f32x4_any*>(p + k * a.count + i);
+      *reinterpret_cast<u32x2_any*>(o + i) = u32x2_any{pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3])};
+    } else {
+      for (long long q = i; q < a.count; ++q) {
+        float s = p[q];
+        for (int k = 1; k < a.slabs[m]; ++k) s += p[k * a.count + q];
+        o[q] = (__bf16)s;
+      }
+    }
+  }
+}
+
+}  // namespace
+
+size_t ffn_backward_workspace_bytes(const Ffn& a) { return carve(a, nullptr, nullptr); }
+
+hipError_t launch_ffn_backward(const Ffn& a, hipStream_t s) {
+  const long long T = (long long)a.B * a.n, DF = (long long)a.D * a.F;
+  const int Dp = up8(a.D), Fp = up8(a.F);
+  const bool odd = ffn_odd(a);
+  BackwardWs ws;
+  carve(a, a.ws, &ws);
+  const char *x = static_cast<const char*>(a.x), *dy = static_cast<const char*>(a.dy),
+             *wg = static_cast<const char*>(a.wg), *wu = static_cast<const char*>(a.wu),
+             *wd = static_cast<const char*>(a.wd);
+  hipError_t e;
+  if (a.len || odd) {
+    FfnRows r = {};
+    r.len = a.len;
+    r.B = a.B;
+    r.n = a.n;
+    r.map = ws.map;
+    r.count = ws.count;
+    r.zero = static_cast<char*>(a.dx);
+    r.zero_bytes = 2LL * a.D;
+    r.always = odd;
+    r.copies = 2;
+    r.copy[0] = {x, ws.x, 0, a.D, Dp};
+    r.copy[1] = {dy, ws.dy, 0, a.D, Dp};
+    if (odd) {
+      r.copies = 5;
+      r.copy[2] = {wg, ws.w[0], a.D, a.F, Fp};
+      r.copy[3] = {wu, ws.w[1], a.D, a.F, Fp};
+      r.copy[4] = {wd, ws.w[2], a.F, a.D, Dp};
+      x = ws.x;
+      dy = ws.dy;
+      wg = ws.w[0];
+      wu = ws.w[1];
+      wd = ws.w[2];
+    }
+    e = launch_ffn_rows(&r, s);
+    if (e != hipSuccess) return e;
+  }
+  const FfnSaved sv = ffn_saved(a, const_cast<void*>(a.saved));
+  const FfnOperand opx = {{x, nullptr}, ws.x, 2u * Dp, 0}, opdy = {{dy, nullptr}, ws.dy, 2u * Dp, 0};
+  FfnArgs base = {};
+  base.T = (int)T;
+  base.count = ws.count;
+  if (a.dx || a.dwg || a.dwu) {
+    FfnArgs h = base;
+    h.a = opdy;
+    h.b = {{wd, nullptr}, nullptr, 2u * Dp, a.F};
+    h.N = Fp;
+    h.K = Dp;
+    h.out[0] = ws.dg;
+    h.out[1] = ws.du;
+    h.ld = Fp;
+    h.frags = sv.frags;
+    h.frag_cols = (Fp + 15) / 16;
+    e = a.act == kActGelu   ? run_ffn<kDh, kActGelu>(h, T, Fp, s)
+        : a.act == kActSilu ? run_ffn<kDh, kActSilu>(h, T, Fp, s)
+                            : run_ffn<kDh, kActNone>(h, T, Fp, s);
+    if (e != hipSuccess) return e;
+  }
+  if (a.dx) {
+    FfnArgs d = base;
+    d.map = ws.map;
+    d.a = {{ws.dg, ws.du}, nullptr, 2u * Fp, 0};
+    d.b = {{wg, wu}, nullptr, 2u * Fp, a.D};
+    d.N = a.D;
+    d.K = Fp;
+    d.out[0] = a.dx;
+    d.ld = a.D;
+    e = run_ffn<kDx, kActNone>(d, T, a.D, s);
+    if (e != hipSuccess) return e;
+  }
+  SlabSums sums = {};
+  sums.count = DF;
+  if (a.dwd) {
+    FfnArgs d = base;
+    d.a = {{sv.h, nullptr}, nullptr, 2u * Fp, 0};
+    d.b = opdy;
+    d.M = a.F;
+    d.N = a.D;
+    d.out[0] = a.dwd;
+    d.ld = a.D;
+    d.slabs = slabs_of(a, 1);
+    d.part = ws.part_d;
+    e = run_ffn<kDwd, kActNone>(d, a.F, a.D, s);
+    if (e != hipSuccess) return e;
+    if (d.slabs > 1) {
+      sums.part[0] = ws.part_d;
+      sums.out[0] = static_cast<__bf16*>(a.dwd);
+      sums.slabs[0] = d.slabs;
+    }
+  }
+  if (a.dwg || a.dwu) {
+    FfnArgs d = base;
+    d.a = opx;
+    d.b = {{ws.dg, ws.du}, nullptr, 2u * Fp, 0};
+    d.M = a.D;
+    d.N = a.F;
+    d.out[0] = a.dwg;
+    d.out[1] = a.dwu;
+    d.ld = a.F;
+    d.slabs = slabs_of(a, 2);
+    d.part = ws.part_gu;
+    e = run_ffn<kDwgu, kActNone>(d, a.D, 2LL * a.F, s);
+    if (e != hipSuccess) return e;
+    if (d.slabs > 1) {
+      for (int i = 0; i < 2; ++i) {
+        sums.part[1 + i] = ws.part_gu + i * d.slabs * DF;
+        sums.out[1 + i] = static_cast<__bf16*>(i ? a.dwu : a.dwg);
+        sums.slabs[1 + i] = d.slabs;
+      }
+    }
+  }
+  if (sums.out[0] || sums.out[1] || sums.out[2]) {
+    hipLaunchKernelGGL(k_ffn_slabs, dim3((unsigned)std::min<long long>((DF + 1023) / 1024, 1024), 3), dim3(256), 0, s,
+                       sums);
+    return hipGetLastError();
+  }
+  return hipSuccess;
+}
+
+}  // namespace sc

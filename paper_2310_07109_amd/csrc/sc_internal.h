@@ -224,6 +224,55 @@ hipError_t launch_block_norm(const Norm& a, hipStream_t s);
 size_t block_norm_backward_floats(const Norm& a);
 hipError_t launch_block_norm_backward(const Norm& a, hipStream_t s);
 
+// Rotary positions (sc_rotary.hip).
+constexpr int kRotaryMaxD = 256;
+struct RotaryTurns {
+  unsigned long long t[kRotaryMaxD / 2];  // turns per position, in 2^-64
+};
+struct Rotary {
+  const void *q, *k, *v;     // strided inputs (backward: q and k, with norm)
+  const void *gq, *gk, *gv;  // backward: dense gradients of the outputs
+  void *oq, *ok, *ov;        // dense outputs (backward: strided gradients); null: that part is not computed
+  long long q_stride, k_stride, v_stride;
+  const float *q_w, *k_w;
+  float *dq_w, *dk_w, *ws;   // backward
+  const int *len, *pos;      // or null
+  int B, n, Hq, Hk, d, R, interleaved, norm, rms, f32;
+  float eps, amplitude;
+  RotaryTurns turns;
+};
+hipError_t launch_rotary(const Rotary& r, hipStream_t s);
+hipError_t launch_rotary_backward(const Rotary& r, hipStream_t s);
+size_t rotary_backward_floats(long long rows, int d);
+
+// Dropout (sc_dropout.hip).
+struct Dropout {
+  const void *x, *residual;  // residual: or null
+  void* out;
+  const int64_t* seed;
+  const int* len;  // or null
+  int B, n, D, site, f32;
+  unsigned threshold;
+  float scale, res_scale;
+};
+hipError_t launch_dropout(const Dropout& a, hipStream_t s);
+
+// The gated feed-forward block (sc_ffn.hip), forward and backward.
+struct Ffn {
+  const void *x, *wg, *wu, *wd, *dy;
+  void* y;
+  void* saved;                     // forward: or null
+  void *dx, *dwg, *dwu, *dwd;      // backward: or null
+  void* ws;
+  const int* len;                  // or null
+  int B, n, D, F, act;             // act: 0 none, 1 GELU, 2 SiLU
+};
+size_t ffn_saved_bytes(const Ffn& a);
+size_t ffn_workspace_bytes(const Ffn& a, bool save);
+size_t ffn_backward_workspace_bytes(const Ffn& a);
+hipError_t launch_ffn(const Ffn& a, hipStream_t s);
+hipError_t launch_ffn_backward(const Ffn& a, hipStream_t s);
+
 hipError_t launch_copy_i32(const int* src, int* dst, long long count, hipStream_t s);
 hipError_t launch_iota_orig(const int* valid_len, int* orig, int B, int n, hipStream_t s);
 

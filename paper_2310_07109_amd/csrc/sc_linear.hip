@@ -19,6 +19,7 @@
 // exponential among them) and 268 MB of stores stand beside them.
 #include <algorithm>
 
+#include "sc_act.h"
 #include "sc_device.h"
 #include "sc_internal.h"
 #include "sc_pack.h"
@@ -30,33 +31,6 @@ namespace {
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 
 // -------------------------------------------------------- activations ----
-// gelu(v) = max(v, 0) - |v| Phi(-|v|), with Phi(-a) = exp2(P(a)): log2 Phi(-a)
-// is close to a parabola, so a polynomial (fitted here on [0, 9], minimax in the
-// relative error of Phi) replaces the rational form and its reciprocal, and a
-// negative leading coefficient lets it run on to 0 beyond the fitted range.
-// Absolute error 2.4e-7; of a negative value 1e-6 relative down to -3, 2.5e-6 to
-// -5, 3e-5 to -9, where it is 1e-18.  One form for both output types: what is
-// stored as bf16 is the float32 value rounded once (degree 5 has 1.6e-4 relative and
-// 1 % beyond -5, 14 instructions a result instead of 21 and 182 us instead of 202 for
-// 32768 x 1024 x 4096).  NaN stays NaN; |v| beyond 16 is cut for the product with Phi = 0.
-SC_DEV float gelu_exp2(float v) {
-  const float a = __builtin_elementwise_minimum(fabsf(v), 16.f);  // without the quieting that fminf needs
-  float p = -4.266044115186496e-11f;
-  p = fmaf(p, a, 2.5370372469524227e-09f);
-  p = fmaf(p, a, -6.685024089847502e-08f);
-  p = fmaf(p, a, 1.0232761269435287e-06f);
-  p = fmaf(p, a, -9.952474101737607e-06f);
-  p = fmaf(p, a, 6.172758003231138e-05f);
-  p = fmaf(p, a, -0.00020646034681703895f);
-  p = fmaf(p, a, -0.00019499764312058687f);
-  p = fmaf(p, a, 0.007243024185299873f);
-  p = fmaf(p, a, -0.05268990248441696f);
-  p = fmaf(p, a, -0.45911744236946106f);
-  p = fmaf(p, a, -1.1511205434799194f);
-  p = fmaf(p, a, -0.9999995827674866f);
-  return fmaf(-a, fast_exp2(p), vmax(v, 0.f));
-}
-
 template <bool kGelu>
 SC_DEV float finish(int acc, float sx, float sw, float bias) {
   const float v = fmaf((float)acc * sx, sw, bias);

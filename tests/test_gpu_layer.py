@@ -1,0 +1,473 @@
+"""The layer operators (include/sc_layer.h) against plain float64 forms.
+
+Tolerances count roundings (u = 2^-24 of float32, half a step of the storage type at the end):
+  rotary    a cosine or sine is off by 2^-27 of a turn (4.7e-8), the series' 4e-9 and its roundings (3 u): 2.4e-7 = 4 u;
+            a rotated pair by amplitude * (|a| + |b|) * (4 u + 2 u), and by what its inputs are off.  A normalised
+            value: sums of d values in chains of at most 20 additions, the deviation from the mean, the factor and the
+            product: 50 u (1 + |hat| + max|x| / sigma).  Weight gradients: sums over rows in chains of at most 256.
+  ffn       on small integers every product and sum is exact and the results are equal to those of a form that rounds
+            where the header says.  On random values a result has two roundings to bf16 behind it (h, dg or du, and its
+            own), each of 2^-8 of the value at most and, spread evenly over a step, 2^-8 / sqrt(3) of it in the mean
+            square: sqrt(2 / 3) 2^-8 = 0.0032 of the result's 2-norm, 0.0035 with what float32 sums, activations
+            (3e-5 at most) and the 24 bits of what is saved (2^-16) add.  A value by itself: 2^-8 of the sum of the
+            products' magnitudes, twice, more than float32 sums of up to 4096 products add.
+  dropout   masks are equal; x * scale, the FMA with the residual and the store round once each.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2310_07109_amd as sc
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = {"f32": (torch.float32, sc.SC_F32, 2.0 ** -24), "bf16": (torch.bfloat16, sc.SC_BF16, 2.0 ** -8)}
+
+
+def gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def lens_of(spec, B, n):
+    if spec is None:
+        return None, torch.full((B,), n)
+    L = torch.tensor([spec[b % len(spec)] for b in range(B)], dtype=torch.int32)
+    return L.to(DEV), L.clamp(0, n).long()
+
+
+def valid_mask(L, n):
+    return torch.arange(n)[None, :] < L[:, None]
+
+
+def assert_close(got, want, tol, what):
+    got = got.double().cpu()
+    assert got.shape == want.shape, what
+    bad = ~((got - want).abs() <= tol)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} off, worst " \
+        f"{float(((got - want).abs() / tol.clamp(min=1e-300))[bad].max()):.3g} times the tolerance"
+
+
+# ---------------------------------------------------------------- rotary ----
+def rotate64(x, angle, amplitude, R, layout):
+    """x [B, n, H, d] rotated by angle [B, n, R / 2], in float64; and |a| + |b| of every rotated dimension."""
+    c, s = angle.cos()[:, :, None], angle.sin()[:, :, None]
+    i = torch.arange(R // 2)
+    ia, ib = (i, i + R // 2) if layout == sc.SC_ROTARY_HALF else (2 * i, 2 * i + 1)
+    out, mag = x.clone(), torch.zeros_like(x)
+    a, b = x[..., ia], x[..., ib]
+    out[..., ia], out[..., ib] = amplitude * (a * c - b * s), amplitude * (a * s + b * c)
+    mag[..., ia] = mag[..., ib] = abs(amplitude) * (a.abs() + b.abs())
+    return out, mag
+
+
+def head_norm64(x, kind, eps):
+    """(hat, 1 / sigma, error of hat)"""
+    v = x - x.mean(-1, keepdim=True) if kind == sc.SC_NORM_LAYER else x
+    inv = (v.pow(2).mean(-1, keepdim=True) + eps).rsqrt()
+    hat = v * inv
+    return hat, inv, 50 * U * (1 + hat.abs() + x.abs().amax(-1, keepdim=True) * inv)
+
+
+def rotary_forward64(x, w, angle, amplitude, R, layout, norm, kind, eps):
+    err = torch.zeros_like(x)
+    if norm:
+        hat, _, e = head_norm64(x, kind, eps)
+        w = torch.ones(x.shape[-1], dtype=torch.float64) if w is None else w.double()
+        x, err = hat * w, (e + 2 * U * hat.abs()) * w.abs()
+    out, mag = rotate64(x, angle, amplitude, R, layout)
+    _, emag = rotate64(err, angle, amplitude, R, layout)
+    return out, torch.where(mag > 0, emag + 6 * U * mag, err)
+
+
+def rotary_case(B, n, Hq, Hk, d, R, dtype, norm, layout, kind=sc.SC_NORM_RMS, lens=None, fused=True, weights=True,
+                pos=None, amplitude=1.0, seed=0, backward=False):
+    g = gen(seed)
+    dt, code, half = TYPES[dtype]
+    W = (Hq + 2 * Hk) * d
+    pad = 16 if fused else 0
+    rows = (torch.randn((B, n, W + pad), generator=g) * torch.exp(0.5 * torch.randn(W + pad, generator=g))).to(dt)
+    L_dev, L = lens_of(lens, B, n)
+    m = valid_mask(L, n)
+    rows[~m] = float("nan")
+    freq, _ = sc.sc_rotary_frequencies(R) if R else (None, 1.0)
+    if pos is None:
+        p = torch.arange(n).expand(B, n)
+    else:
+        p = torch.randint(-pos, pos, (B, n), generator=g)
+    angle = p.double()[..., None] * (freq if R else torch.zeros(0, dtype=torch.float64))
+    cut = (0, Hq * d, (Hq + Hk) * d, W)
+    dev = rows.to(DEV)
+    parts = [dev[..., cut[i]:cut[i + 1]].unflatten(-1, (-1, d)) for i in range(3)]
+    host = [rows[..., cut[i]:cut[i + 1]].unflatten(-1, (-1, d)).double() for i in range(3)]
+    host = [torch.where(m[..., None, None], t, 0.0) for t in host]
+    if not fused:
+        parts = [t.contiguous() for t in parts]
+    qw, kw = ((1 + 0.2 * torch.randn(d, generator=g)) if norm and weights else None for _ in range(2))
+    D = sc.RotaryDesc(B, n, Hq, Hk, d=d, rot_dim=R, valid_len=L_dev, layout=layout, norm=norm, kind=kind, eps=1e-5,
+                      amplitude=amplitude, dtype=code)
+    args = dict(q_w=None if qw is None else qw.to(DEV), k_w=None if kw is None else kw.to(DEV),
+                positions=None if pos is None else p.to(torch.int32).to(DEV))
+    if not backward:
+        outs = sc.sc_rotary(D, freq, *parts, **args)
+        for i, (nm, w) in enumerate((("q", qw), ("k", kw))):
+            want, tol = rotary_forward64(host[i], w, angle, amplitude, R, layout, norm, kind, 1e-5)
+            mm = m[..., None, None]
+            assert_close(outs[i], torch.where(mm, want, 0.0), torch.where(mm, tol + half * want.abs(), 0.0), nm)
+        assert torch.equal(outs[2].double().cpu(), host[2])
+        return
+    go = [torch.randn((B, n, h, d), generator=g).to(dt) for h in (Hq, Hk, Hk)]
+    for t in go:
+        t[~m] = float("nan")
+    grads = torch.full_like(dev, 7.0)
+    gp = [grads[..., cut[i]:cut[i + 1]].unflatten(-1, (-1, d)) for i in range(3)]
+    if not fused:
+        gp = [torch.empty_like(t) for t in parts]
+    dw = dict(dq_w=torch.empty(d, device=DEV), dk_w=torch.empty(d, device=DEV)) if norm else {}
+    out = sc.sc_rotary_backward(D, freq, *[t.to(DEV) for t in go], q=parts[0], k=parts[1],
+                                grads=dict(dq=gp[0], dk=gp[1], dv=gp[2], **dw), **args)
+    if fused:
+        assert bool((grads[..., W:] == 7).all())  # only its own parts are written
+    mm = m[..., None, None]
+    for i, (nm, w) in enumerate((("dq", qw), ("dk", kw))):
+        gr = torch.where(mm, go[i].double(), 0.0)
+        du, mag = rotate64(gr, -angle, amplitude, R, layout)
+        e = 6 * U * mag
+        if norm:
+            hat, inv, eh = head_norm64(host[i], kind, 1e-5)
+            ww = torch.ones(d, dtype=torch.float64) if w is None else w.double()
+            dwant, dmag = (du * hat).sum((0, 1, 2)), (du.abs() * hat.abs()).sum((0, 1, 2))
+            dtol = (e * hat.abs() + du.abs() * torch.where(mm, eh, 0.0)).sum((0, 1, 2)) + 256 * U * dmag
+            assert_close(out["dq_w" if i == 0 else "dk_w"], dwant, dtol, nm + "_w")
+            gw, e = du * ww, (e + U * du.abs()) * ww.abs()
+            gh = (gw * hat).mean(-1, keepdim=True)
+            gs = gw.mean(-1, keepdim=True) if kind == sc.SC_NORM_LAYER else torch.zeros_like(gh)
+            want = inv * (gw - hat * gh - gs)
+            ah, ag = (gw * hat).abs().mean(-1, keepdim=True), gw.abs().mean(-1, keepdim=True)
+            egh = (e * hat.abs() + gw.abs() * eh).mean(-1, keepdim=True) + 25 * U * ah
+            tol = inv * (e + eh * gh.abs() + hat.abs() * egh + e.mean(-1, keepdim=True) + 25 * U * ag +
+                         4 * U * (gw.abs() + hat.abs() * ah + ag)) + 30 * U * want.abs()
+        else:
+            want, tol = du, torch.where(mag > 0, e, 0.0)
+        assert_close(out[nm], torch.where(mm, want, 0.0), torch.where(mm, tol + half * want.abs(), 0.0), nm)
+    assert torch.equal(out["dv"].double().cpu(), torch.where(mm, go[2].double(), 0.0))
+
+
+HALF, INTER = sc.SC_ROTARY_HALF, sc.SC_ROTARY_INTERLEAVED
+ROTARY = [  # B, n, Hq, Hk, d, R, dtype, norm, layout, kind
+    (1, 1, 8, 8, 64, 64, "bf16", True, HALF, sc.SC_NORM_RMS), (1, 1, 1, 1, 2, 2, "f32", True, INTER, sc.SC_NORM_RMS),
+    (2, 33, 12, 4, 64, 64, "bf16", False, HALF, 0), (3, 17, 5, 5, 80, 40, "f32", True, INTER, sc.SC_NORM_LAYER),
+    (2, 40, 3, 1, 128, 64, "bf16", True, HALF, sc.SC_NORM_LAYER), (1, 9, 2, 2, 256, 256, "bf16", True, HALF, 1),
+    (2, 31, 4, 2, 96, 32, "f32", True, HALF, 1), (2, 31, 4, 2, 66, 6, "bf16", True, HALF, 0),
+    (2, 31, 3, 3, 72, 72, "bf16", True, INTER, 1), (1, 50, 3, 3, 64, 0, "bf16", True, HALF, 1),
+    (1, 50, 3, 3, 18, 10, "f32", False, INTER, 0), (7, 700, 2, 1, 64, 48, "f32", True, HALF, 0),
+]
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("B,n,Hq,Hk,d,R,dtype,norm,layout,kind", ROTARY)
+def test_rotary(B, n, Hq, Hk, d, R, dtype, norm, layout, kind, backward):
+    for i, (lens, fused, weights, pos, amp) in enumerate((
+            (None, True, True, None, 1.0), ((n, 0, (n + 1) // 2), False, True, 2 ** 31 - 1, 0.75),
+            ((1, n), True, False, 5000, 1.0))):
+        rotary_case(B, n, Hq, Hk, d, R, dtype, norm, layout, kind, lens=lens, fused=fused, weights=weights, pos=pos,
+                    amplitude=amp, seed=i, backward=backward)
+
+
+def test_rotary_large_grid_and_offsets():
+    """More tokens than workgroups, and fused rows whose byte offsets pass 32 bits."""
+    rotary_case(9, 2048, 2, 1, 64, 64, "bf16", True, HALF, lens=(2048, 5, 0, 1999), backward=False)
+    rotary_case(9, 2048, 2, 1, 64, 64, "bf16", True, HALF, lens=(2048, 5, 0, 1999), backward=True)
+    B, n, step = 1, 1 << 15, 1 << 17  # 8 GiB between the first token and the last
+    rows = torch.empty(B * n * step, dtype=torch.bfloat16, device=DEV)
+    q = rows.as_strided((B, n, 2, 64), (n * step, step, 64, 1))
+    q.copy_(torch.randn((B, n, 2, 64), generator=gen(1)).to(torch.bfloat16))
+    freq, _ = sc.sc_rotary_frequencies(64)
+    D = sc.RotaryDesc(B, n, 2, 1)
+    out = sc.sc_rotary(D, freq, q)[0]
+    assert torch.equal(out, sc.sc_rotary(D, freq, q.contiguous())[0])
+    g = torch.randn((B, n, 2, 64), generator=gen(2)).to(torch.bfloat16).to(DEV)
+    sc.sc_rotary_backward(D, freq, g, grads=dict(dq=q))
+    assert torch.equal(q.contiguous(), sc.sc_rotary_backward(D, freq, g)["dq"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rotary_inverse_in_place_and_parts(dtype):
+    """Backward without norms turns back what forward turned; in place; q alone, k alone, v alone."""
+    dt, code, half = TYPES[dtype]
+    B, n, H = 2, 37, 3
+    q = torch.randn((B, n, H, 64), generator=gen(3)).to(dt).to(DEV)
+    freq, _ = sc.sc_rotary_frequencies(64, scaling=sc.SC_ROTARY_BANDS, factor=4.0, length=512)
+    d = sc.RotaryDesc(B, n, H, H, dtype=code)
+    out, k_out, v_out = sc.sc_rotary(d, freq, q)
+    assert k_out is None and v_out is None
+    assert torch.equal(sc.sc_rotary(d, freq, None, k=q)[1], out)
+    assert torch.equal(sc.sc_rotary(d, freq, None, None, q)[2], q)
+    back = sc.sc_rotary_backward(d, freq, out)["dq"]
+    pair = q.double().abs() + q.double().abs().roll(32, -1)
+    assert_close(back, q.double().cpu(), (3 * (12 * U + 2 * half) * pair).cpu(), "turned back")
+    buf = q.clone()
+    assert sc.sc_rotary(d, freq, buf, q_out=buf)[0].data_ptr() == buf.data_ptr() and torch.equal(buf, out)
+    sc.sc_rotary_backward(d, freq, buf, grads=dict(dq=buf))
+    assert torch.equal(buf, back)
+
+
+def test_rotary_gradients_by_differences():
+    """Central differences of the float32 forward along random directions, within their own error."""
+    B, n, H, d = 2, 5, 2, 16
+    g = gen(9)
+    x = torch.randn((B, n, H, d), generator=g)
+    w = 1 + 0.2 * torch.randn(d, generator=g)
+    freq, _ = sc.sc_rotary_frequencies(d)
+    for kind in (sc.SC_NORM_LAYER, sc.SC_NORM_RMS):
+        D = sc.RotaryDesc(B, n, H, H, d=d, norm=True, kind=kind, eps=1e-5, dtype=sc.SC_F32)
+        go = torch.randn((B, n, H, d), generator=g)
+        out = sc.sc_rotary_backward(D, freq, go.to(DEV), q=x.to(DEV), q_w=w.to(DEV))
+
+        def loss(x, w):
+            return float((sc.sc_rotary(D, freq, x.to(DEV), q_w=w.to(DEV))[0].double().cpu() * go.double()).sum())
+        h = 2.0 ** -7
+        for _ in range(4):
+            vx, vw = torch.randn(x.shape, generator=g), torch.randn(d, generator=g)
+            num = (loss(x + h * vx, w + h * vw) - loss(x - h * vx, w - h * vw)) / (2 * h)
+            ana = float((out["dq"].double().cpu() * vx).sum() + (out["dq_w"].double().cpu() * vw).sum())
+            # third derivatives of a normalised head grow with the step's size against its deviation (about 1 here)
+            scale = float((go.abs() * (1 + vx.abs()).pow(3)).sum())
+            assert abs(num - ana) <= h * h * scale + 64 * U * scale / h, (num, ana)
+
+
+# ------------------------------------------------------------------- ffn ----
+def bf(t):
+    return t.to(torch.bfloat16).double()
+
+
+def ffn_ints(B, n, D, F, lens, seed):
+    """Inputs of small integers, few of them not 0, so that every sum is an integer far below 2^24."""
+    g = gen(seed)
+    L_dev, L = lens_of(lens, B, n)
+    m = valid_mask(L, n)
+
+    def sparse(*shape, keep):
+        return (torch.randint(-2, 3, shape, generator=g) * (torch.rand(shape, generator=g) < keep)).to(torch.bfloat16)
+    x, dy = sparse(B, n, D, keep=0.5), sparse(B, n, D, keep=0.5)
+    wg, wu, wd = sparse(D, F, keep=min(1.0, 8 / D)), sparse(D, F, keep=min(1.0, 8 / D)), sparse(F, D, keep=min(1.0, 8 / F))
+    x[~m], dy[~m] = float("nan"), float("nan")
+    return L_dev, m, x, wg, wu, wd, dy
+
+
+def ffn_ints_check(B, n, D, F, lens, seed=0):
+    L_dev, m, x, wg, wu, wd, dy = ffn_ints(B, n, D, F, lens, seed)
+    d = sc.FfnDesc(B, n, D, F, valid_len=L_dev, act=sc.SC_ACT_NONE)
+    dev = [t.to(DEV) for t in (x, wg, wu, wd)]
+    y, saved = sc.sc_gated_ffn(d, *dev, saved=True)
+    y2, none = sc.sc_gated_ffn(d, *dev)
+    assert none is None and torch.equal(y, y2)
+    out = sc.sc_gated_ffn_backward(d, *dev, saved, dy.to(DEV))
+    xs, ds = x[m].double().to(DEV), dy[m].double().to(DEV)
+    wg, wu, wd = (t.double().to(DEV) for t in (wg, wu, wd))
+    g, u = xs @ wg, xs @ wu
+    h = bf(g * u)
+    dh = ds @ wd.t()
+    dg, du = bf(dh * u), bf(dh * g)
+
+    def rows(v):
+        t = torch.zeros((B, n, D), dtype=torch.float64, device=DEV)
+        t[m.to(DEV)] = bf(v)
+        return t
+    want = dict(y=rows(h @ wd), dx=rows(dg @ wg.t() + du @ wu.t()), dwg=bf(xs.t() @ dg), dwu=bf(xs.t() @ du),
+                dwd=bf(h.t() @ ds))
+    assert max(float(v.abs().max()) for v in (h.t() @ ds, xs.t() @ dg, xs.t() @ du)) < 2 ** 24
+    for nm, v in want.items():
+        got = (y if nm == "y" else out[nm]).double()
+        assert torch.equal(got, v), f"{nm}: {int((got != v).sum())} of {v.numel()} differ"
+
+
+@pytest.mark.parametrize("B,n,D,F,lens", [
+    (1, 1, 64, 64, None), (1, 1, 8, 8, None), (1, 1, 1, 1, None), (1, 1, 768, 2048, (1,)), (1, 5, 33, 47, None),
+    (2, 3, 100, 70, (3, 0)), (2, 9, 64, 136, (0, 0)), (16, 8, 768, 2304, (8, 4, 5, 1)), (1, 40, 96, 1000, None),
+    (3, 501, 500, 1111, (300, 501, 0)), (1, 300, 264, 520, None), (5, 129, 72, 328, (129, 128, 1, 64, 65)),
+    (1, 2000, 1024, 512, None), (4, 1100, 512, 1536, (1100, 7, 900)), (2, 2048, 1000, 1032, (2048, 1991))])
+def test_ffn_exact_on_integers(B, n, D, F, lens):
+    ffn_ints_check(B, n, D, F, lens)
+
+
+def test_ffn_many_tiles():
+    """Several tiles a workgroup in every product, padding between them."""
+    ffn_ints_check(16, 1024, 1024, 2816, (1024, 1000, 513, 0))
+
+
+def act64(act, g):
+    """act(g) and its slope."""
+    if act == sc.SC_ACT_SILU:
+        p = torch.sigmoid(g)
+        return g * p, p * (1 + g * (1 - p))
+    if act == sc.SC_ACT_GELU:
+        p = 0.5 * torch.special.erfc(-g / math.sqrt(2))
+        return g * p, p + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+    return g, torch.ones_like(g)
+
+
+@pytest.mark.parametrize("act", [sc.SC_ACT_NONE, sc.SC_ACT_GELU, sc.SC_ACT_SILU])
+@pytest.mark.parametrize("B,n,D,F,lens", [(1, 1, 512, 768, None), (3, 11, 200, 333, (11, 0, 4)),
+                                          (2, 700, 264, 512, (700, 333)), (1, 3000, 512, 1024, None)])
+def test_ffn_values_and_gradients(B, n, D, F, lens, act):
+    g_ = gen(D + act)
+    L_dev, L = lens_of(lens, B, n)
+    m = valid_mask(L, n)
+    x = torch.randn((B, n, D), generator=g_).to(torch.bfloat16)
+    wg, wu = ((torch.randn((D, F), generator=g_) * 2 / math.sqrt(D)).to(torch.bfloat16) for _ in range(2))
+    wd = (torch.randn((F, D), generator=g_) / math.sqrt(F)).to(torch.bfloat16)
+    dy = torch.randn((B, n, D), generator=g_).to(torch.bfloat16)
+    d = sc.FfnDesc(B, n, D, F, valid_len=L_dev, act=act)
+    dev = [t.to(DEV) for t in (x, wg, wu, wd)]
+    y, saved = sc.sc_gated_ffn(d, *dev, saved=True)
+    out = sc.sc_gated_ffn_backward(d, *dev, saved, dy.to(DEV))
+    xs, ds = x[m].double(), dy[m].double()
+    wg, wu, wd = (t.double() for t in (wg, wu, wd))
+    g, u = xs @ wg, xs @ wu
+    a, slope = act64(act, g)
+    h, dh = a * u, ds @ wd.t()
+    dg, du = dh * u * slope, dh * a
+    A = torch.abs
+    want = dict(y=(h @ wd, A(h) @ A(wd)), dx=(dg @ wg.t() + du @ wu.t(), A(dg) @ A(wg).t() + A(du) @ A(wu).t()),
+                dwg=(xs.t() @ dg, A(xs).t() @ A(dg)), dwu=(xs.t() @ du, A(xs).t() @ A(du)),
+                dwd=(h.t() @ ds, A(h).t() @ A(ds)))
+    for nm, (v, mag) in want.items():
+        got = (y if nm == "y" else out[nm]).double().cpu()
+        if nm in ("y", "dx"):
+            assert not got[~m].any(), nm
+            got = got[m]
+        assert float((got - v).norm()) <= 0.0035 * float(v.norm()), nm
+        assert_close(got, v, 2 * 2.0 ** -8 * mag, nm)
+
+
+def test_ffn_gradients_by_differences():
+    """The loss along a direction, in float64 on the rounded inputs, against the gradients' product with it."""
+    B, n, D, F = 2, 30, 40, 56
+    g = gen(4)
+    x = torch.randn((B, n, D), generator=g).to(torch.bfloat16)
+    w = [(torch.randn(s, generator=g) / math.sqrt(s[0])).to(torch.bfloat16) for s in ((D, F), (D, F), (F, D))]
+    dy = torch.randn((B, n, D), generator=g).to(torch.bfloat16)
+    for act in (sc.SC_ACT_GELU, sc.SC_ACT_SILU):
+        d = sc.FfnDesc(B, n, D, F, act=act)
+        dev = [t.to(DEV) for t in (x, *w)]
+        _, saved = sc.sc_gated_ffn(d, *dev, saved=True)
+        out = sc.sc_gated_ffn_backward(d, *dev, saved, dy.to(DEV))
+
+        def loss(p):
+            return float(((act64(act, p[0] @ p[1])[0] * (p[0] @ p[2])) @ p[3] * dy.double()).sum())
+        leaves = [t.double() for t in (x, *w)]
+        for i, nm in enumerate(("dx", "dwg", "dwu", "dwd")):
+            v = torch.randn(leaves[i].shape, generator=g, dtype=torch.float64)
+            h = 1e-4
+            num = (loss([t + h * v if j == i else t for j, t in enumerate(leaves)]) -
+                   loss([t - h * v if j == i else t for j, t in enumerate(leaves)])) / (2 * h)
+            ana = float((out[nm].double().cpu() * v).sum())
+            # errors of 0.0035 of the gradient's norm in a direction that does not know them: 5 of their deviations
+            assert abs(num - ana) <= 5 * 0.0035 * float(out[nm].double().norm()), (nm, num, ana)
+
+
+def test_ffn_infinities_and_nans_stay_in_their_rows():
+    B, n, D, F = 1, 140, 64, 72
+    g = gen(6)
+    x = torch.randn((B, n, D), generator=g).to(torch.bfloat16)
+    w = [(torch.randn(s, generator=g) / math.sqrt(s[0])).to(torch.bfloat16).to(DEV) for s in ((D, F), (D, F), (F, D))]
+    d = sc.FfnDesc(B, n, D, F)
+    clean = sc.sc_gated_ffn(d, x.to(DEV), *w)[0]
+    x[0, 7, 3], x[0, 130, 0] = float("nan"), float("inf")
+    y = sc.sc_gated_ffn(d, x.to(DEV), *w)[0]
+    assert y[0, 7].isnan().all() and not y[0, 130].isfinite().any()
+    keep = [i for i in range(n) if i not in (7, 130)]
+    assert torch.equal(y[0, keep], clean[0, keep])
+
+
+@pytest.mark.parametrize("names", [("dx",), ("dwg",), ("dwu",), ("dwd",), ("dx", "dwd"), ("dwg", "dwu")])
+@pytest.mark.parametrize("B,n,D,F", [(2, 20, 24, 40), (1, 1500, 264, 136)])
+def test_ffn_backward_parts(B, n, D, F, names):
+    """Only the gradients asked for, the same as all of them; backward twice from what was saved once."""
+    L_dev, m, x, wg, wu, wd, dy = ffn_ints(B, n, D, F, (n, n - 3), 1)
+    x, dy = (torch.nan_to_num(t) for t in (x, dy))
+    d = sc.FfnDesc(B, n, D, F, valid_len=L_dev)
+    dev = [t.to(DEV) for t in (x, wg, wu, wd)]
+    _, saved = sc.sc_gated_ffn(d, *dev, saved=True)
+    keep = saved.clone()
+    full = sc.sc_gated_ffn_backward(d, *dev, saved, dy.to(DEV))
+    part = sc.sc_gated_ffn_backward(d, *dev, saved, dy.to(DEV), grads={k: torch.full_like(full[k], 9) for k in names})
+    for k, v in part.items():
+        assert (v is None) == (k not in names)
+        assert v is None or torch.equal(v, full[k])
+    assert torch.equal(saved, keep)
+
+
+# --------------------------------------------------------------- dropout ----
+def philox(counter, key):
+    """Philox4x32-10 of uint32 arrays."""
+    c = [np.asarray(v, dtype=np.uint64) for v in counter]
+    k = [int(v) for v in key]
+    lo = np.uint64(0xFFFFFFFF)
+    for _ in range(10):
+        p, q = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        c = [(q >> np.uint64(32)) ^ c[1] ^ np.uint64(k[0]), q & lo, (p >> np.uint64(32)) ^ c[3] ^ np.uint64(k[1]), p & lo]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    return c
+
+
+def keep_mask(B, n, D, p, seed, site):
+    G = (D + 7) // 8
+    z = np.zeros((B, n, G), dtype=np.uint64)
+    seed %= 1 << 64
+    w = philox((z + np.arange(G, dtype=np.uint64), z + np.arange(n, dtype=np.uint64)[:, None],
+                z + np.arange(B, dtype=np.uint64)[:, None, None], z + np.uint64(site % (1 << 32))),
+               (seed & 0xFFFFFFFF, seed >> 32))
+    r = np.stack([h for v in w for h in (v & np.uint64(0xFFFF), v >> np.uint64(16))], -1).reshape(B, n, -1)[..., :D]
+    return torch.from_numpy(r.astype(np.int64) >= round(p * 65536))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,n,D,lens,p,site", [
+    (1, 1, 1, None, 0.5, 0), (1, 1, 512, None, 0.1, 3), (2, 3, 7, (0, 2), 0.3, -1), (3, 17, 33, (17, 0, 5), 0.999, 99),
+    (2, 5, 1111, None, 0.0, 1), (5, 300, 768, (300, 11, 299), 0.25, 2), (1, 20000, 96, (19999,), 0.1, 2 ** 31 - 1),
+    (9000, 2, 9, (2, 1), 0.5, 4)])
+def test_dropout(B, n, D, lens, p, site, dtype):
+    dt, code, half = TYPES[dtype]
+    g = gen(D)
+    L_dev, L = lens_of(lens, B, n)
+    m = valid_mask(L, n)[..., None]
+    x, res = torch.randn((B, n, D), generator=g).to(dt), torch.randn((B, n, D), generator=g).to(dt)
+    x, res = torch.where(m, x, torch.nan).to(dt), torch.where(m, res, torch.nan).to(dt)
+    for seed in (-3, 0x123456789ABCDEF):
+        s = torch.tensor([seed], device=DEV)
+        keep = keep_mask(B, n, D, p, seed, site)
+        d = sc.DropoutDesc(B, n, D, p, valid_len=L_dev, site=site, res_scale=0.81, dtype=code)
+        t = round(p * 65536)
+        dropped = torch.where(keep & m, x.double() * (65536 / (65536 - t)), 0.0)
+        out = sc.sc_dropout(d, x.to(DEV), s)
+        assert_close(out, dropped, (2 * U + half) * dropped.abs(), "no residual")
+        want = torch.where(m, 0.81 * res.double() + dropped, 0.0)
+        got = sc.sc_dropout(d, x.to(DEV), s, residual=res.to(DEV))
+        # 0.81 itself is rounded to float32
+        tol = torch.where(m, 2 * U * (dropped.abs() + res.double().abs()) + (U + half) * want.abs(), 0.0)
+        assert_close(got, want, tol, "residual")
+        for into in ("x", "residual"):
+            a, b = x.to(DEV), res.to(DEV)
+            sc.sc_dropout(d, a, s, residual=b, out=a if into == "x" else b)
+            assert torch.equal(a if into == "x" else b, got)
+
+
+def test_dropout_mask_is_a_function_of_the_token():
+    """Neither n, D, dtype nor the lengths change a token's mask; seeds and sites do; a dropped infinity is 0."""
+    s = torch.tensor([77], device=DEV)
+    big = sc.sc_dropout(sc.DropoutDesc(3, 50, 640, 0.5), torch.ones((3, 50, 640), dtype=torch.bfloat16, device=DEV), s)
+    small = sc.sc_dropout(sc.DropoutDesc(2, 9, 100, 0.5, dtype=sc.SC_F32), torch.ones((2, 9, 100), device=DEV), s)
+    assert torch.equal(small, big[:2, :9, :100].float())
+    assert abs(float((big != 0).float().mean()) - 0.5) < 6 * 0.5 / math.sqrt(big.numel())
+    x = torch.full((2, 9, 100), float("inf"), device=DEV)
+    out = sc.sc_dropout(sc.DropoutDesc(2, 9, 100, 0.5, dtype=sc.SC_F32), x, s)
+    assert torch.equal(out == 0, small == 0) and torch.equal(out.isinf(), small != 0)
+    other = sc.sc_dropout(sc.DropoutDesc(2, 9, 100, 0.5, dtype=sc.SC_F32, site=1), torch.ones_like(x), s)
+    again = sc.sc_dropout(sc.DropoutDesc(2, 9, 100, 0.5, dtype=sc.SC_F32), torch.ones_like(x), s + 1)
+    assert not torch.equal(other, small) and not torch.equal(again, small)
