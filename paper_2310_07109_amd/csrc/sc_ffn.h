@@ -24,14 +24,12 @@ namespace sc {
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
-struct u32x3 {  // 12 bytes at any dword (a vector type of three takes 16)
-  unsigned w[3];
-};
+typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;
 typedef __attribute__((ext_vector_type(2), aligned(2))) unsigned u32x2_any;
 typedef f32x4 __attribute__((aligned(4))) f32x4_any;
 
-constexpr int kGate = 0, kDown = 1, kDh = 2, kDx = 3, kDwd = 4, kDwgu = 5;
+constexpr int kGate = 0, kDown = 1, kDh = 2, kDx = 3, kDwd = 4, kDwgu = 5, kGateKeep = 6;  // 6: kGate that keeps g and u
 constexpr int kFfnWgs = 256;   // one workgroup per CU, each taking tiles in turn
 constexpr int kGroupTiles = 8;  // row tiles that share weights in an XCD's L2
 
@@ -62,8 +60,8 @@ struct FfnArgs {
   int map_a;         // a's rows are the batch's: read through map
   void* out[2];      // bf16: h | y | dg, du | dx | dwd | dwg, dwu
   int ld;            // elements of its rows
-  char* frags;       // kGate: g and u as fragments, or null; kDh: to read
-  int frag_cols;     // fragments of a row of fragments
+  char* blocks;      // kGate: g and u for the backward, or null; kDh: to read
+  int across;        // blocks of a row of blocks
   float* part;       // kDwd, kDwgu: sums of the slabs (one slab: null)
   int slabs;
 };
@@ -73,7 +71,7 @@ struct FfnArgs {
 SC_DEV void lds_dma16_buf(u32x4 rsrc, unsigned voff, unsigned lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
                :
-               : "v"(voff), "s"(rsrc), "s"(lds)
+               : "v"(voff), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane((int)lds))
                : "memory", "m0");
 }
 constexpr unsigned kBeyond = 0xfffff000u;  // an offset beyond every descriptor's end
@@ -139,18 +137,22 @@ struct FfnPart {
     }
   }
   // kAlong with a contraction that ends inside the stage: units from `limit` on are zeros.
-  SC_DEV void issue(const u32x4 (&rsrc)[kSubs], unsigned lds, int lane, int w, int limit) const {
+  SC_DEV void issue(const u32x4 (&rsrc)[kSubs], unsigned lds, int w, int limit) const {
+    if (!kAcross && limit < 8) {
+      const int lane = opaque_lane();
+#pragma unroll
+      for (int t = 0; t < kLoads; ++t) {
+        const int r = 8 * load_at(w, t) + (lane >> 3), unit = (lane & 7) ^ ((r >> 1) & 7);
+        lds_dma16_buf(rsrc[0], unit < limit ? voff[t] : kBeyond, lds + (unsigned)load_at(w, t) * 1024);
+      }
+      return;
+    }
 #pragma unroll
     for (int t = 0; t < kLoads; ++t) {
-      unsigned v = voff[t];
-      if constexpr (!kAcross) {
-        const int r = 8 * load_at(w, t) + (lane >> 3), unit = (lane & 7) ^ ((r >> 1) & 7);
-        if (limit < 8) v = unit < limit ? v : kBeyond;
-      }
       const int sub = load_sub(w, t);
       u32x4 d = rsrc[0];
       if constexpr (kSubs == 2) d = sub ? rsrc[1] : rsrc[0];
-      lds_dma16_buf(d, v, lds + (unsigned)(sub * 128 * kCols + load_at(w, t) * 1024));
+      lds_dma16_buf(d, voff[t], lds + (unsigned)(sub * 128 * kCols + load_at(w, t) * 1024));
     }
   }
   // Fragment i of chunk c (32 of the stage's 64) of the part at LDS address `lds`.
@@ -167,20 +169,39 @@ struct FfnPart {
 };
 
 // ------------------------------------------------------------ results ----
-// 24 of a float32's bits: four of them in three words, and back.
-SC_DEV u32x3 pack24(const f32x4& v) {
+// 24 of a float32's bits, four values in three words, and back.
+SC_DEV void pack24(const f32x4& v, unsigned* w) {
   const u32x4 u = __builtin_bit_cast(u32x4, v);
-  return u32x3{{__builtin_amdgcn_perm(u[1], u[0], 0x05030201u), __builtin_amdgcn_perm(u[2], u[1], 0x06050302u),
-                __builtin_amdgcn_perm(u[3], u[2], 0x07060503u)}};
+  w[0] = __builtin_amdgcn_perm(u[1], u[0], 0x05030201u);
+  w[1] = __builtin_amdgcn_perm(u[2], u[1], 0x06050302u);
+  w[2] = __builtin_amdgcn_perm(u[3], u[2], 0x07060503u);
 }
-SC_DEV f32x4 unpack24(const u32x3& v) {
-  const u32x4 u = {v.w[0] << 8, __builtin_amdgcn_perm(v.w[1], v.w[0], 0x0504030cu),
-                   __builtin_amdgcn_perm(v.w[2], v.w[1], 0x0403020cu), v.w[2] & 0xffffff00u};
+SC_DEV f32x4 unpack24(const unsigned* w) {
+  const u32x4 u = {w[0] << 8, __builtin_amdgcn_perm(w[1], w[0], 0x0504030cu),
+                   __builtin_amdgcn_perm(w[2], w[1], 0x0403020cu), w[2] & 0xffffff00u};
   return __builtin_bit_cast(f32x4, u);
 }
-// Fragment (ri, ci) of g (which = 0) or u (1): a lane's four results as pack24 gives them.
-SC_DEV char* frag_at(char* frags, int cols, int ri, int ci, int which, int lane) {
-  return frags + ((((long long)ri * cols + ci) * 2 + which) * 64 + lane) * 12;
+// What the backward needs of g and u: blocks of 16 rows by 32 columns, of a block a lane's
+// twelve words (g and u of its columns 4 g on, g and u of columns 16 + 4 g on) in three
+// planes of 16 bytes a lane, so that whole lines move.
+constexpr int kBlockBytes = 3 * 1024;
+SC_DEV char* block_at(char* blocks, int across, int ri, int cb, int lane) {
+  return blocks + ((long long)ri * across + cb) * kBlockBytes + 16 * lane;
+}
+SC_DEV void store_block(char* at, const unsigned (&w)[12]) {
+#pragma unroll
+  for (int p = 0; p < 3; ++p)
+    *reinterpret_cast<u32x4*>(at + 1024 * p) = u32x4{w[4 * p], w[4 * p + 1], w[4 * p + 2], w[4 * p + 3]};
+}
+// Six words of one half of a block.
+SC_DEV void store_half_block(char* at, int half, const unsigned (&w)[6]) {
+  if (half == 0) {
+    *reinterpret_cast<u32x4*>(at) = u32x4{w[0], w[1], w[2], w[3]};
+    *reinterpret_cast<u32x2*>(at + 1024) = u32x2{w[4], w[5]};
+  } else {
+    *reinterpret_cast<u32x2*>(at + 1024 + 8) = u32x2{w[0], w[1]};
+    *reinterpret_cast<u32x4*>(at + 2048) = u32x4{w[2], w[3], w[4], w[5]};
+  }
 }
 
 // Up to kCount bf16 values of a row from column col on, those below N, at any address.
@@ -214,9 +235,10 @@ struct FfnProduct {
   using S = FfnTile<kM>;
   static constexpr int BM = S::kBM, BN = S::kBN, kNBuf = S::kNBuf;
   static constexpr int WM = BM / S::kWgM, WN = BN / S::kWgN, FI = WM / 16, FJ = WN / 16;
+  static constexpr bool kIsGate = kKind == kGate || kKind == kGateKeep;
   static constexpr bool kOverRows = kKind == kDwd || kKind == kDwgu;  // contraction over the batch's rows
-  static constexpr bool kAcrossA = kOverRows, kAcrossB = kOverRows || kKind == kGate || kKind == kDown;
-  static constexpr int kSubs = kKind == kGate ? 2 : 1;
+  static constexpr bool kAcrossA = kOverRows, kAcrossB = kOverRows || kIsGate || kKind == kDown;
+  static constexpr int kSubs = kIsGate ? 2 : 1;
   static constexpr int kH = FI >= 2 ? 2 : 1, FH = FI / kH;  // a wave's rows go in halves
   using A = FfnPart<kAcrossA, BM, WM, 1>;
   using B = FfnPart<kAcrossB, BN, WN, kSubs>;
@@ -230,7 +252,10 @@ struct FfnProduct {
   f32x4 acc[FI][FJ];
   bf16x8 xf[2][FH], wf[2][FJ];
   // the tile
-  int m0, n0, sel, slab, k0, ns, seg;  // sel: of two outputs; k0: first stage; ns: stages, of which a segment has seg
+  struct Tile {
+    int m0, n0, sel, slab;  // sel: of two outputs
+  };
+  int m0, n0, sel, slab, k0, ns, seg;  // k0: first stage; ns: stages, of which a segment has seg
   const char *pa[2], *pb[2];
   unsigned bytes_a, bytes_b;
 
@@ -282,7 +307,7 @@ struct FfnProduct {
     }
     m0 = __builtin_amdgcn_readfirstlane(m0);
     n0 = __builtin_amdgcn_readfirstlane(n0);
-    const int M = rows(), N = p.N;
+    const int M = rows(), N = p.N, lane = opaque_lane();
     a.offsets(lane, w, m0, p.a.ld, [&](int r) {
       int row = min(r, M - 1);
       if (p.map_a) row = p.map[row];
@@ -296,14 +321,14 @@ struct FfnProduct {
     const int limit = kOverRows || ks < seg - 1 ? 8 : (p.K - 64 * ks + 7) / 8;  // units of the stage (operands along the rows)
     const unsigned skip_a = kAcrossA ? (unsigned)ks * 64 * p.a.ld : (unsigned)ks * 128;
     const unsigned skip_b = kAcrossB ? (unsigned)ks * 64 * p.b.ld : (unsigned)ks * 128;
-    const u32x4 ra[1] = {descriptor(pa[second], bytes_a, skip_a)};
-    a.issue(ra, at, lane, w, limit);
+    const u32x4 ra[1] = {descriptor(second ? pa[1] : pa[0], bytes_a, skip_a)};
+    a.issue(ra, at, w, limit);
     if constexpr (kSubs == 2) {
       const u32x4 rb[2] = {descriptor(pb[0], bytes_b, skip_b), descriptor(pb[1], bytes_b, skip_b)};
-      b.issue(rb, at + A::kBytes, lane, w, limit);
+      b.issue(rb, at + A::kBytes, w, limit);
     } else {
-      const u32x4 rb[1] = {descriptor(pb[kKind == kDwgu ? sel : second], bytes_b, skip_b)};
-      b.issue(rb, at + A::kBytes, lane, w, limit);
+      const u32x4 rb[1] = {descriptor((kKind == kDwgu ? sel : second) ? pb[1] : pb[0], bytes_b, skip_b)};
+      b.issue(rb, at + A::kBytes, w, limit);
     }
   }
   SC_DEV void cols(int q, int bf, int c) {
@@ -327,40 +352,64 @@ struct FfnProduct {
   }
   static SC_DEV int next_buf(int bf) { return bf == kNBuf - 1 ? 0 : bf + 1; }
 
+  // Stores that every wave issues for a tile without an edge.  While the last tile's are
+  // under way, newer than the stages that start() loaded, a stage is waited for past them.
+  // A count above what was issued would let a stage be read before it has landed; below, it
+  // only waits longer.
+  static constexpr int kStores = kKind == kGateKeep ? FI * (FJ == 2 ? 3 : 4)
+                                 : kKind == kGate   ? FI
+                                 : kKind == kDh     ? FI * FJ
+                                                    : FI * FJ / 2;
+  SC_DEV bool whole(const Tile& t) const { return t.m0 + BM <= rows() && t.n0 + BN / kSubs <= p.N; }
+  template <int kFrom>
+  SC_DEV void wait_first(bool stored, int later) const {
+    constexpr int kMost = 63 - (kNBuf - 1) * kDma;  // the counter ends at 63
+    if (stored)
+      wait_stages<kNBuf - kFrom, kDma, kStores < kMost ? kStores : kMost>(later);
+    else
+      wait_stages<kNBuf - kFrom, kDma>(later);
+  }
   // The tile's sums.  Every half's fragments are in flight during the products of the one
   // before, across stages too; one barrier a stage, before its last products: the next
   // stage has landed, and every wave holds its last fragments of this one, whose buffer is
   // refilled.
-  SC_DEV void sums() {
+  SC_DEV void sums(bool stored) {
 #pragma unroll
     for (int i = 0; i < FI; ++i)
 #pragma unroll
       for (int j = 0; j < FJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (kOverRows && ns == 0) return;
-    wait_vm<0>();
+    wait_first<0>(stored, min(ns, kNBuf) - 1);
     __syncthreads();
     int bf = 0;
     cols(0, 0, 0);
     rows(0, 0, 0, 0);
-    for (int s = 0; s < ns; ++s) {
+    for (int s = 0; s + 1 < ns; ++s) {
       const int bn = next_buf(bf);
 #pragma unroll
-      for (int q = 0; q < 2 * kH; ++q) {
-        const int nq = q + 1;
-        if (nq < 2 * kH) {
-          if (nq == kH) cols(1, bf, 1);
-          rows(nq & 1, bf, nq / kH, nq % kH);
-        } else if (s + 1 < ns) {
-          wait_stages<kNBuf - 1, kDma>(min(ns - 2 - s, kNBuf - 2));
-          __syncthreads();
-          if (s + kNBuf < ns) issue(s + kNBuf, bf);
-          cols(0, bn, 0);
-          rows(0, bn, 0, 0);
-        }
-        mul(q % kH, q & 1, q / kH);
-      }
+      for (int q = 0; q + 1 < 2 * kH; ++q) half(q, bf);
+      if (s + 1 < kNBuf)
+        wait_first<1>(stored, min(ns - 2 - s, kNBuf - 2));
+      else
+        wait_stages<kNBuf - 1, kDma>(min(ns - 2 - s, kNBuf - 2));
+      __syncthreads();
+      if (s + kNBuf < ns) issue(s + kNBuf, bf);
+      cols(0, bn, 0);
+      rows(0, bn, 0, 0);
+      mul((2 * kH - 1) % kH, 1, 1);
       bf = bn;
     }
+    // the last stage by itself: joined with the others, its products would wait for
+    // fragments that the loop has just asked for
+#pragma unroll
+    for (int q = 0; q + 1 < 2 * kH; ++q) half(q, bf);
+    mul((2 * kH - 1) % kH, 1, 1);
+  }
+  // Half q of a stage (of 2 kH, the last one apart), and the fragments of the next one.
+  SC_DEV void half(int q, int bf) {
+    if (q + 1 == kH) cols(1, bf, 1);
+    rows((q + 1) & 1, bf, (q + 1) / kH, (q + 1) % kH);
+    mul(q % kH, q & 1, q / kH);
   }
   SC_DEV void start() {
 #pragma unroll
@@ -368,66 +417,80 @@ struct FfnProduct {
       if (s < ns) issue(s, s);
   }
 
+  SC_DEV Tile tile() const { return {m0, n0, sel, slab}; }
   // Element e of a lane: row 16 i + lr, column 16 j + 4 g + e.
-  SC_DEV void emit_h(int i) const {
+  SC_DEV void emit_h(const Tile& t, int i, int lane) const {
     constexpr int J = FJ / 2;
-    const int r = m0 + wm + 16 * i + lr, c = n0 + wn;
-    const bool on = r < R;
+    const int g = lane >> 4, lr = lane & 15;
+    const int r0 = t.m0 + wm + 16 * i, r = r0 + lr, c = t.n0 + wn;
+    const bool on = r < R, keep = kKind == kGateKeep && r0 < R && c < 32 * p.across;
     __bf16* row = static_cast<__bf16*>(p.out[0]) + (long long)r * p.ld;
     f32x4 h[J];
+    unsigned w[6 * J];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const f32x4 gt = acc[i][j], up = acc[i][J + j];
-      if (p.frags && m0 + wm + 16 * i < R && c + 16 * j < 16 * p.frag_cols) {
-        const int ri = (m0 + wm) / 16 + i, ci = c / 16 + j;
-        *reinterpret_cast<u32x3*>(frag_at(p.frags, p.frag_cols, ri, ci, 0, lane)) = pack24(gt);
-        *reinterpret_cast<u32x3*>(frag_at(p.frags, p.frag_cols, ri, ci, 1, lane)) = pack24(up);
+      if constexpr (kKind == kGateKeep) {
+        pack24(gt, w + 6 * j);
+        pack24(up, w + 6 * j + 3);
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) h[j][e] = act<kAct>(gt[e]) * up[e];
     }
+    char* at = block_at(p.blocks, p.across, r0 / 16, c / 32, lane);
     if constexpr (J == 1) {
+      if (keep) store_half_block(at, c / 16 & 1, w);
       store_one(row, c, p.N, g, h[0], on);
     } else {
-#pragma unroll
-      for (int j = 0; j < J; j += 2) store_pair(row, c + 16 * j, p.N, g, h[j], h[j + 1], on);
+      static_assert(J == 2, "a block a wave and 16 rows");
+      if (keep) store_block(at, w);
+      store_pair(row, c, p.N, g, h[0], h[1], on);
     }
   }
-  SC_DEV void emit_dh(int i) const {
-    const int r = m0 + wm + 16 * i + lr, c = n0 + wn;
+  // The words of block j (of the wave's FJ / 2) of rows i.
+  SC_DEV void load_block(const Tile& t, int i, int j, int lane, unsigned (&w)[12]) const {
+    const int r0 = t.m0 + wm + 16 * i, c = t.n0 + wn + 32 * j;
+    if (r0 < R && c < 32 * p.across) {
+      const char* at = block_at(p.blocks, p.across, r0 / 16, c / 32, lane);
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(at + 1024 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[4 * q + e] = v[e];
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 12; ++q) w[q] = 0;
+    }
+  }
+  SC_DEV void emit_dh(const Tile& t, int i, int j, int lane, const unsigned (&w)[12]) const {
+    const int g = lane >> 4, lr = lane & 15;
+    const int r = t.m0 + wm + 16 * i + lr, c = t.n0 + wn + 32 * j;
     const bool on = r < R;
     __bf16* dg = static_cast<__bf16*>(p.out[0]) + (long long)r * p.ld;
     __bf16* du = static_cast<__bf16*>(p.out[1]) + (long long)r * p.ld;
+    f32x4 vg[2], vu[2];
 #pragma unroll
-    for (int j = 0; j < FJ; j += 2) {
-      f32x4 vg[2], vu[2];
+    for (int f = 0; f < 2; ++f) {
+      const f32x4 gt = unpack24(w + 6 * f), up = unpack24(w + 6 * f + 3);
 #pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        u32x3 sg = {{0, 0, 0}}, su = {{0, 0, 0}};
-        if (m0 + wm + 16 * i < R && c + 16 * (j + f) < 16 * p.frag_cols) {
-          const int ri = (m0 + wm) / 16 + i, ci = c / 16 + j + f;
-          sg = *reinterpret_cast<const u32x3*>(frag_at(p.frags, p.frag_cols, ri, ci, 0, lane));
-          su = *reinterpret_cast<const u32x3*>(frag_at(p.frags, p.frag_cols, ri, ci, 1, lane));
-        }
-        const f32x4 gt = unpack24(sg), up = unpack24(su);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float slope;
-          const float v = act_slope<kAct>(gt[e], slope), dh = acc[i][j + f][e];
-          vg[f][e] = dh * up[e] * slope;
-          vu[f][e] = dh * v;
-        }
+      for (int e = 0; e < 4; ++e) {
+        float slope;
+        const float v = act_slope<kAct>(gt[e], slope), dh = acc[i][2 * j + f][e];
+        vg[f][e] = dh * up[e] * slope;
+        vu[f][e] = dh * v;
       }
-      store_pair(dg, c + 16 * j, p.N, g, vg[0], vg[1], on);
-      store_pair(du, c + 16 * j, p.N, g, vu[0], vu[1], on);
     }
+    store_pair(dg, c, p.N, g, vg[0], vg[1], on);
+    store_pair(du, c, p.N, g, vu[0], vu[1], on);
   }
-  SC_DEV void emit_rows(int i) const {  // kDown, kDx, kDwd, kDwgu
-    const int r = m0 + wm + 16 * i + lr, c = n0 + wn;
+  SC_DEV void emit_rows(const Tile& t, int i, int lane) const {  // kDown, kDx, kDwd, kDwgu
+    const int g = lane >> 4, lr = lane & 15;
+    const int r = t.m0 + wm + 16 * i + lr, c = t.n0 + wn;
     const bool on = r < rows();
     if constexpr (kOverRows) {
       if (p.part) {
-        float* part = p.part + ((long long)sel * p.slabs + slab) * p.M * p.N + (long long)r * p.N;
+        float* part = p.part + ((long long)t.sel * p.slabs + t.slab) * p.M * p.N + (long long)r * p.N;
 #pragma unroll
         for (int j = 0; j < FJ; ++j) {
           const int col = c + 16 * j + 4 * g;
@@ -445,16 +508,31 @@ struct FfnProduct {
     }
     long long at = r;
     if (!kOverRows && p.map && on) at = p.map[r];
-    __bf16* row = static_cast<__bf16*>(p.out[sel]) + at * p.ld;
+    __bf16* row = static_cast<__bf16*>(t.sel ? p.out[1] : p.out[0]) + at * p.ld;
 #pragma unroll
     for (int j = 0; j < FJ; j += 2) store_pair(row, c + 16 * j, p.N, g, acc[i][j], acc[i][j + 1], on);
   }
-  SC_DEV void results() const {
+  SC_DEV void results(const Tile& t) const {
+    const int lane = opaque_lane();
+    if constexpr (kKind == kDh) {
+      // the blocks of kAhead units (16 rows by 32 columns) ahead are in flight
+      constexpr int kUnits = FI * FJ / 2, kAhead = kUnits < 3 ? kUnits : 3;
+      unsigned w[kAhead][12];
 #pragma unroll
-    for (int i = 0; i < FI; ++i) {
-      if constexpr (kKind == kGate) emit_h(i);
-      else if constexpr (kKind == kDh) emit_dh(i);
-      else emit_rows(i);
+      for (int u = 0; u < kAhead; ++u) load_block(t, u / (FJ / 2), u % (FJ / 2), lane, w[u]);
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) {
+        __builtin_amdgcn_sched_barrier(0);
+        emit_dh(t, u / (FJ / 2), u % (FJ / 2), lane, w[u % kAhead]);
+        if (u + kAhead < kUnits) load_block(t, (u + kAhead) / (FJ / 2), (u + kAhead) % (FJ / 2), lane, w[u % kAhead]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < FI; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kIsGate) emit_h(t, i, lane);
+        else emit_rows(t, i, lane);
+      }
     }
   }
 };
@@ -470,12 +548,24 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   const long long items = p.items();
   const int xcd = blockIdx.x & 7, step = gridDim.x >> 3;
   const long long last = items * (xcd + 1) / 8;
-  for (long long it = items * xcd / 8 + (blockIdx.x >> 3); it < last; it += step) {
-    p.place(it);
-    __syncthreads();  // the last tile's stages are read
-    p.start();
-    p.sums();
-    p.results();
+  long long it = items * xcd / 8 + (blockIdx.x >> 3);
+  if (it >= last) return;
+  p.place(it);
+  p.start();
+  bool stored = false;
+  while (true) {
+    p.sums(stored);
+    const typename P::Tile t = p.tile();
+    const bool more = it + step < last;
+    if (more) {  // the next tile's first stages are loaded during this one's results
+      it += step;
+      p.place(it);
+      __syncthreads();  // every wave has read the last stage
+      p.start();
+    }
+    p.results(t);
+    if (!more) return;
+    stored = p.whole(t);
   }
 }
 
@@ -484,13 +574,36 @@ hipError_t run_ffn(const FfnArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((k_ffn<kKind, kM, kAct>), dim3(kFfnWgs), dim3(512), 0, s, a);
   return hipGetLastError();
 }
-// The tile by the number of tiles that the largest one leaves.
+// What a product costs with tiles of kind m, in ns: rounds of workgroups times the stages of
+// a tile and what stands beside them.
+inline long long ffn_cost(int m, long long rows, long long cols, long long stages, int slabs) {
+  const long long bm = m == 0 ? 256 : m == 1 ? 128 : 64;
+  const long long stage = m == 0 ? 1750 : m == 1 ? 560 : 210, fixed = m == 0 ? 12000 : m == 1 ? 6000 : 3500;
+  const long long tiles = (rows + bm - 1) / bm * ((cols + bm - 1) / bm) * slabs;
+  return (tiles + kFfnWgs - 1) / kFfnWgs * ((stages + slabs - 1) / slabs * stage + fixed);
+}
+struct FfnPlan {
+  int tile, slabs;
+};
+// most_slabs > 1: the contraction may be cut; each slab's sums are written and read again.
+inline FfnPlan ffn_plan(long long rows, long long cols, long long stages, int most_slabs) {
+  FfnPlan best = {0, 1};
+  long long least = 1LL << 62;
+  for (int m = 0; m < 3; ++m)
+    for (int s = 1; s <= most_slabs && (s == 1 || s * 4 <= stages); ++s) {
+      const long long extra = s == 1 ? 0 : 4000 + rows * cols * s * 8 / 5000;  // a launch, and 5 TB/s
+      const long long t = ffn_cost(m, rows, cols, stages, s) + extra;
+      if (t < least) {
+        least = t;
+        best = {m, s};
+      }
+    }
+  return best;
+}
 template <int kKind, int kAct>
-hipError_t run_ffn(const FfnArgs& a, long long rows, long long cols, hipStream_t s) {
-  const long long slabs = a.slabs > 1 ? a.slabs : 1;
-  auto tiles = [&](int m) { return (rows + m - 1) / m * ((cols + m - 1) / m) * slabs; };
-  if (tiles(256) >= kFfnWgs) return run_ffn<kKind, 0, kAct>(a, s);
-  if (tiles(128) >= kFfnWgs / 2) return run_ffn<kKind, 1, kAct>(a, s);
+hipError_t run_ffn(const FfnArgs& a, int tile, hipStream_t s) {
+  if (tile == 0) return run_ffn<kKind, 0, kAct>(a, s);
+  if (tile == 1) return run_ffn<kKind, 1, kAct>(a, s);
   return run_ffn<kKind, 2, kAct>(a, s);
 }
 
@@ -502,7 +615,7 @@ inline bool ffn_odd(const Ffn& a) { return a.D % 8 != 0 || a.F % 8 != 0; }
 
 struct FfnSaved {
   char* h;      // [valid rows, Fp] bf16
-  char* frags;  // g and u
+  char* blocks;  // g and u
   size_t bytes;
 };
 inline FfnSaved ffn_saved(const Ffn& a, void* base) {
@@ -510,8 +623,8 @@ inline FfnSaved ffn_saved(const Ffn& a, void* base) {
   FfnSaved s;
   s.h = static_cast<char*>(base);
   const size_t h = (T * Fp * 2 + 255) / 256 * 256;
-  s.frags = s.h + h;
-  s.bytes = h + (T + 15) / 16 * ((Fp + 15) / 16) * 2 * 768;
+  s.blocks = s.h + h;
+  s.bytes = h + (T + 15) / 16 * ((Fp + 31) / 32) * kBlockBytes;
   return s;
 }
 

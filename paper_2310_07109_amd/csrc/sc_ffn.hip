@@ -89,8 +89,8 @@ size_t carve(const Ffn& a, void* base, bool save, ForwardWs* out) {
 }
 
 template <int kAct>
-hipError_t gate(const FfnArgs& g, long long rows, long long cols, hipStream_t s) {
-  return run_ffn<kGate, kAct>(g, rows, cols, s);
+hipError_t gate(const FfnArgs& g, int tile, hipStream_t s) {
+  return g.blocks ? run_ffn<kGateKeep, kAct>(g, tile, s) : run_ffn<kGate, kAct>(g, tile, s);
 }
 
 }  // namespace
@@ -147,8 +147,8 @@ hipError_t launch_ffn(const Ffn& a, hipStream_t s) {
   if (a.saved) {
     const FfnSaved sv = ffn_saved(a, a.saved);
     h = sv.h;
-    g.frags = sv.frags;
-    g.frag_cols = (Fp + 15) / 16;
+    g.blocks = sv.blocks;
+    g.across = (Fp + 31) / 32;
   }
   g.a = {{x, nullptr}, nullptr, 2u * Dp, g.map_a ? (int)T : 0};
   g.b = {{wg, wu}, nullptr, 2u * Fp, a.D};
@@ -156,9 +156,10 @@ hipError_t launch_ffn(const Ffn& a, hipStream_t s) {
   g.K = Dp;
   g.out[0] = h;
   g.ld = Fp;
-  const hipError_t e = a.act == kActGelu   ? gate<kActGelu>(g, T, 2LL * Fp, s)
-                       : a.act == kActSilu ? gate<kActSilu>(g, T, 2LL * Fp, s)
-                                           : gate<kActNone>(g, T, 2LL * Fp, s);
+  const int tile = ffn_plan(T, 2LL * Fp, (Dp + 63) / 64, 1).tile;
+  const hipError_t e = a.act == kActGelu   ? gate<kActGelu>(g, tile, s)
+                       : a.act == kActSilu ? gate<kActSilu>(g, tile, s)
+                                           : gate<kActNone>(g, tile, s);
   if (e != hipSuccess) return e;
   FfnArgs d = {};
   d.T = (int)T;
@@ -170,7 +171,7 @@ hipError_t launch_ffn(const Ffn& a, hipStream_t s) {
   d.K = Fp;
   d.out[0] = a.y;
   d.ld = a.D;
-  return run_ffn<kDown, kActNone>(d, T, a.D, s);
+  return run_ffn<kDown, kActNone>(d, ffn_plan(T, a.D, (Fp + 63) / 64, 1).tile, s);
 }
 
 }  // namespace sc

@@ -12,13 +12,11 @@ struct BackwardWs {
   float *part_d, *part_gu;
 };
 
-// Slabs of the rows that a weight gradient's sum is cut into: as many as give every
-// workgroup a tile, of 512 rows at least.
-int slabs_of(const Ffn& a, int mats) {
+// The weight gradients' sums over rows, cut into slabs so that every workgroup has a tile.
+constexpr int kMostSlabs = 16;
+FfnPlan weight_plan(const Ffn& a, int mats) {
   const long long T = (long long)a.B * a.n;
-  auto tiles = [&](long long m) { return (a.D + m - 1) / m * ((a.F + m - 1) / m) * mats; };
-  const long long t = tiles(256);
-  return (int)std::max<long long>(1, std::min<long long>(kFfnWgs / std::max<long long>(t, 1), T / 512));
+  return ffn_plan(a.D, (long long)mats * a.F, (T + 63) / 64, kMostSlabs);
 }
 
 size_t carve(const Ffn& a, void* base, BackwardWs* out) {
@@ -40,7 +38,7 @@ size_t carve(const Ffn& a, void* base, BackwardWs* out) {
   }
   s.dg = c.take(T * Fp * 2);
   s.du = c.take(T * Fp * 2);
-  const int sd = slabs_of(a, 1), sg = slabs_of(a, 2);
+  const int sd = weight_plan(a, 1).slabs, sg = weight_plan(a, 2).slabs;
   if (sd > 1) s.part_d = reinterpret_cast<float*>(c.take(4 * DF * sd));
   if (sg > 1) s.part_gu = reinterpret_cast<float*>(c.take(4 * DF * 2 * sg));
   if (out) *out = s;
@@ -130,11 +128,12 @@ hipError_t launch_ffn_backward(const Ffn& a, hipStream_t s) {
     h.out[0] = ws.dg;
     h.out[1] = ws.du;
     h.ld = Fp;
-    h.frags = sv.frags;
-    h.frag_cols = (Fp + 15) / 16;
-    e = a.act == kActGelu   ? run_ffn<kDh, kActGelu>(h, T, Fp, s)
-        : a.act == kActSilu ? run_ffn<kDh, kActSilu>(h, T, Fp, s)
-                            : run_ffn<kDh, kActNone>(h, T, Fp, s);
+    h.blocks = sv.blocks;
+    h.across = (Fp + 31) / 32;
+    const int tile = ffn_plan(T, Fp, (Dp + 63) / 64, 1).tile;
+    e = a.act == kActGelu   ? run_ffn<kDh, kActGelu>(h, tile, s)
+        : a.act == kActSilu ? run_ffn<kDh, kActSilu>(h, tile, s)
+                            : run_ffn<kDh, kActNone>(h, tile, s);
     if (e != hipSuccess) return e;
   }
   if (a.dx) {
@@ -146,7 +145,7 @@ hipError_t launch_ffn_backward(const Ffn& a, hipStream_t s) {
     d.K = Fp;
     d.out[0] = a.dx;
     d.ld = a.D;
-    e = run_ffn<kDx, kActNone>(d, T, a.D, s);
+    e = run_ffn<kDx, kActNone>(d, ffn_plan(T, a.D, 2 * ((Fp + 63) / 64), 1).tile, s);
     if (e != hipSuccess) return e;
   }
   SlabSums sums = {};
@@ -159,9 +158,10 @@ hipError_t launch_ffn_backward(const Ffn& a, hipStream_t s) {
     d.N = a.D;
     d.out[0] = a.dwd;
     d.ld = a.D;
-    d.slabs = slabs_of(a, 1);
+    const FfnPlan plan = weight_plan(a, 1);
+    d.slabs = plan.slabs;
     d.part = ws.part_d;
-    e = run_ffn<kDwd, kActNone>(d, a.F, a.D, s);
+    e = run_ffn<kDwd, kActNone>(d, plan.tile, s);
     if (e != hipSuccess) return e;
     if (d.slabs > 1) {
       sums.part[0] = ws.part_d;
@@ -178,9 +178,10 @@ hipError_t launch_ffn_backward(const Ffn& a, hipStream_t s) {
     d.out[0] = a.dwg;
     d.out[1] = a.dwu;
     d.ld = a.F;
-    d.slabs = slabs_of(a, 2);
+    const FfnPlan plan = weight_plan(a, 2);
+    d.slabs = plan.slabs;
     d.part = ws.part_gu;
-    e = run_ffn<kDwgu, kActNone>(d, a.D, 2LL * a.F, s);
+    e = run_ffn<kDwgu, kActNone>(d, plan.tile, s);
     if (e != hipSuccess) return e;
     if (d.slabs > 1) {
       for (int i = 0; i < 2; ++i) {
