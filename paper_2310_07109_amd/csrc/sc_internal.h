@@ -243,7 +243,7 @@ struct Rotary {
 };
 hipError_t launch_rotary(const Rotary& r, hipStream_t s);
 hipError_t launch_rotary_backward(const Rotary& r, hipStream_t s);
-size_t rotary_backward_floats(long long rows, int d);
+size_t rotary_backward_floats(long long rows, int d, int heads);  // heads: the larger of Hq and Hk
 
 // Dropout (sc_dropout.hip).
 struct Dropout {

@@ -401,7 +401,7 @@ sc_status sc_rotary(const sc_rotary_desc* d, const double* freq, const void* q, 
 
 size_t sc_rotary_backward_workspace_size(const sc_rotary_desc* d) {
   if (check_rotary(d) != SC_OK || !d->norm) return 0;
-  return sc::rotary_backward_floats((long long)d->B * d->n, d->d) * sizeof(float);
+  return sc::rotary_backward_floats((long long)d->B * d->n, d->d, d->Hq > d->Hk ? d->Hq : d->Hk) * sizeof(float);
 }
 
 sc_status sc_rotary_backward(const sc_rotary_desc* d, const double* freq, const void* dq_out, const void* dk_out,

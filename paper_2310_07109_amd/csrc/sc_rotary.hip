@@ -12,7 +12,9 @@
 // The angles of a token serve all its heads: a workgroup makes the cosines and sines
 // of its tokens once, in LDS.  An angle is a turn in 64-bit fixed point: position times
 // frequency modulo 2^64 is exact in integers whatever the position, and what is left is
-// at most an eighth of a turn for a polynomial.
+// at most an eighth of a turn for a polynomial.  Queries, keys and values have workgroups
+// of their own, so that a lane's weights, and the sums of their gradients, stay in
+// registers over all the heads that it sees.
 #include <algorithm>
 
 #include "sc_device.h"
@@ -26,17 +28,20 @@ typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 constexpr int kThreads = 256;
 constexpr int kMaxTokens = 16;  // of a workgroup at a time
 
+struct RotaryPart {
+  const char *x, *g;      // input and, backward, the gradient of the output
+  char* o;                // output
+  long long xs, gs, os;   // bytes between tokens
+  const float* w;         // or null
+  float* part;            // backward: [workgroups, d] sums of the weight's gradient, or null
+  int heads, wgs;
+};
 struct RotaryArgs {
-  const char *x[3], *g[3];  // q, k, v and, backward, the gradients of the outputs
-  char *o[3];               // outputs
-  long long xs[3], gs[3], os[3];  // bytes between tokens
-  const float* w[2];
+  RotaryPart part[3];  // q, k, v
   const int* len;
   const int* pos;
-  float* part;  // backward: [workgroups, 2, d] sums of the weights' gradients, or null
-  int B, n, heads, h1, h2;  // heads: of a token in all; h1, h2: the first key and value head
-  int d, R, lanes;          // lanes of a head
-  int tokens, interleaved, norm, rms;
+  int B, n, d, R, lanes;  // lanes of a head
+  int tokens, norm, rms;
   float eps, amplitude;
   RotaryTurns turns;
 };
@@ -77,12 +82,11 @@ SC_DEV float head_sum(float v, int lanes) {
 template <typename T, bool kVec>
 struct Pairs {
   float a[8], b[8];
-  SC_DEV static float one(const T* p) { return (float)*p; }
-  SC_DEV static void vec(const T* p, float* v) {  // eight elements at 16 bytes
+  SC_DEV static void vec(const T* p, float (&v)[8]) {  // eight elements at 16 bytes
     if constexpr (sizeof(T) == 4) {
       const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = lo[i], v[4 + i] = hi[i];
+      for (int i = 0; i < 8; ++i) v[i] = i < 4 ? lo[i & 3] : hi[i & 3];
     } else {
       const u32x4 u = *reinterpret_cast<const u32x4*>(p);
 #pragma unroll
@@ -92,7 +96,7 @@ struct Pairs {
       }
     }
   }
-  SC_DEV static void put(T* p, const float* v) {
+  SC_DEV static void put(T* p, const float (&v)[8]) {
     if constexpr (sizeof(T) == 4) {
       *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
       *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
@@ -101,41 +105,74 @@ struct Pairs {
           u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
     }
   }
+  SC_DEV void take(const T* p) {  // eight interleaved pairs
+    if constexpr (sizeof(T) == 4) {
+      f32x4 x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = reinterpret_cast<const f32x4*>(p)[j];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        a[i] = x[i / 2][2 * (i & 1)];
+        b[i] = x[i / 2][2 * (i & 1) + 1];
+      }
+    } else {
+      u32x4 x[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) x[j] = reinterpret_cast<const u32x4*>(p)[j];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const unsigned u = x[i / 4][i & 3];
+        a[i] = __builtin_bit_cast(float, u << 16);
+        b[i] = __builtin_bit_cast(float, u & 0xffff0000u);
+      }
+    }
+  }
+  SC_DEV void give(T* p) const {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        reinterpret_cast<f32x4*>(p)[j] = f32x4{a[2 * j], b[2 * j], a[2 * j + 1], b[2 * j + 1]};
+    } else {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        reinterpret_cast<u32x4*>(p)[j] = u32x4{pack_bf16(a[4 * j], b[4 * j]), pack_bf16(a[4 * j + 1], b[4 * j + 1]),
+                                               pack_bf16(a[4 * j + 2], b[4 * j + 2]), pack_bf16(a[4 * j + 3], b[4 * j + 3])};
+    }
+  }
 };
 
 // Where a lane's pairs are: pair i (of the lane) is live below `live`, rotated below
 // `rot`; elements first(i) and second(i).
+template <bool kInter>
 struct Place {
-  int p0, live, rot, R2, d2, R, interleaved;
-  SC_DEV Place(int d, int R_, int inter, int sub)
-      : p0(8 * sub), live(d / 2 - 8 * sub), rot(R_ / 2 - 8 * sub), R2(R_ / 2), d2(d / 2), R(R_), interleaved(inter) {}
+  int p0, live, rot, R2, d2;
+  SC_DEV Place(int d, int R, int sub)
+      : p0(8 * sub), live(d / 2 - 8 * sub), rot(R / 2 - 8 * sub), R2(R / 2), d2(d / 2) {}
   SC_DEV int first(int i) const {
     const int p = p0 + i;
-    return interleaved ? 2 * p : i < rot ? p : p + R2;  // passed pair q = p - R2: element R + q
+    return kInter ? 2 * p : i < rot ? p : p + R2;  // passed pair q = p - R2: element R + q
   }
   SC_DEV int second(int i) const {
     const int p = p0 + i;
-    return interleaved ? 2 * p + 1 : i < rot ? p + R2 : p + d2;  // R + (d - R) / 2 + q
+    return kInter ? 2 * p + 1 : i < rot ? p + R2 : p + d2;  // R + (d - R) / 2 + q
   }
 };
 
-template <typename T, bool kVec>
-SC_DEV void load_pairs(Pairs<T, kVec>& v, const T* x, const Place& pl) {
+template <typename T, bool kVec, bool kInter>
+SC_DEV void load_pairs(Pairs<T, kVec>& v, const T* x, const Place<kInter>& pl) {
   if constexpr (kVec) {
-    if (pl.live > 0) {
-      if (pl.interleaved) {
-        float t[16];
-        Pairs<T, kVec>::vec(x + pl.first(0), t);
-        Pairs<T, kVec>::vec(x + pl.first(0) + 8, t + 8);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v.a[i] = t[2 * i], v.b[i] = t[2 * i + 1];
-      } else {
-        Pairs<T, kVec>::vec(x + pl.first(0), v.a);
-        Pairs<T, kVec>::vec(x + pl.second(0), v.b);
-      }
+    // lanes beyond the head's end read its start, and keep nothing of it
+    const bool live = pl.live > 0;
+    if constexpr (kInter) {
+      v.take(x + (live ? pl.first(0) : 0));
     } else {
+      Pairs<T, kVec>::vec(x + (live ? pl.first(0) : 0), v.a);
+      Pairs<T, kVec>::vec(x + (live ? pl.second(0) : 0), v.b);
+    }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v.a[i] = v.b[i] = 0.f;
+    for (int i = 0; i < 8; ++i) {
+      v.a[i] = live ? v.a[i] : 0.f;
+      v.b[i] = live ? v.b[i] : 0.f;
     }
   } else {
 #pragma unroll
@@ -146,16 +183,12 @@ SC_DEV void load_pairs(Pairs<T, kVec>& v, const T* x, const Place& pl) {
   }
 }
 
-template <typename T, bool kVec>
-SC_DEV void store_pairs(const Pairs<T, kVec>& v, T* x, const Place& pl) {
+template <typename T, bool kVec, bool kInter>
+SC_DEV void store_pairs(const Pairs<T, kVec>& v, T* x, const Place<kInter>& pl) {
   if constexpr (kVec) {
     if (pl.live <= 0) return;
-    if (pl.interleaved) {
-      float t[16];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) t[2 * i] = v.a[i], t[2 * i + 1] = v.b[i];
-      Pairs<T, kVec>::put(x + pl.first(0), t);
-      Pairs<T, kVec>::put(x + pl.first(0) + 8, t + 8);
+    if constexpr (kInter) {
+      v.give(x + pl.first(0));
     } else {
       Pairs<T, kVec>::put(x + pl.first(0), v.a);
       Pairs<T, kVec>::put(x + pl.second(0), v.b);
@@ -170,8 +203,9 @@ SC_DEV void store_pairs(const Pairs<T, kVec>& v, T* x, const Place& pl) {
   }
 }
 
-// kWeight of a lane's pairs (1 beyond the head's end or without weights).
-SC_DEV void load_weight(const float* w, const Place& pl, float (&a)[8], float (&b)[8]) {
+// Weights of a lane's pairs (1 beyond the head's end or without weights).
+template <bool kInter>
+SC_DEV void load_weight(const float* w, const Place<kInter>& pl, float (&a)[8], float (&b)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const bool on = w && i < pl.live;
@@ -182,8 +216,8 @@ SC_DEV void load_weight(const float* w, const Place& pl, float (&a)[8], float (&
 
 // The normalised head in place of x (elements beyond the head's end stay 0); returns
 // 1 / deviation.
-template <typename P>
-SC_DEV float normalise(P& v, const RotaryArgs& a, const Place& pl) {
+template <typename P, bool kInter>
+SC_DEV float normalise(P& v, const RotaryArgs& a, const Place<kInter>& pl) {
   const float scale = 1.f / (float)a.d;
   if (!a.rms) {
     float s = 0.f;
@@ -191,11 +225,10 @@ SC_DEV float normalise(P& v, const RotaryArgs& a, const Place& pl) {
     for (int i = 0; i < 8; ++i) s += v.a[i] + v.b[i];
     const float mean = head_sum(s, a.lanes) * scale;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < pl.live) {
-        v.a[i] -= mean;
-        v.b[i] -= mean;
-      }
+    for (int i = 0; i < 8; ++i) {
+      v.a[i] -= i < pl.live ? mean : 0.f;
+      v.b[i] -= i < pl.live ? mean : 0.f;
+    }
   }
   float q = 0.f;
 #pragma unroll
@@ -209,66 +242,90 @@ SC_DEV float normalise(P& v, const RotaryArgs& a, const Place& pl) {
   return inv;
 }
 
-template <typename T, bool kVec, bool kBack>
+// The rotation of a lane's pairs by the cosines and sines of a token, kept apart in LDS.
+template <typename P, bool kInter>
+SC_DEV void rotate(P& v, const float* cs, const float* sn, const Place<kInter>& pl, bool whole) {
+  if (whole) {  // all eight pairs or none
+    if (pl.rot <= 0) return;
+    float c[8], s[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(cs + pl.p0 + 4 * h);
+      const f32x4 y = *reinterpret_cast<const f32x4*>(sn + pl.p0 + 4 * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[4 * h + e] = x[e], s[4 * h + e] = y[e];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float p = v.a[i], q = v.b[i];
+      v.a[i] = p * c[i] - q * s[i];
+      v.b[i] = p * s[i] + q * c[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float c = cs[pl.p0 + i], s = sn[pl.p0 + i], p = v.a[i], q = v.b[i];
+      v.a[i] = i < pl.rot ? p * c - q * s : p;
+      v.b[i] = i < pl.rot ? p * s + q * c : q;
+    }
+  }
+}
+
+template <typename T, bool kVec, bool kInter, bool kBack>
 __global__ __launch_bounds__(kThreads) void k_rotary(RotaryArgs a) {
-  __shared__ float2 cs[kMaxTokens * 128];
-  __shared__ float red[kBack ? 4 : 1][2][256];
+  __shared__ __attribute__((aligned(16))) float cs[kMaxTokens][kRotaryMaxD / 2], sn[kMaxTokens][kRotaryMaxD / 2];
+  __shared__ int live_of[kMaxTokens];
+  __shared__ float red[kBack ? 4 : 1][256];
   const int tid = threadIdx.x, lane = tid & 63, lanes = a.lanes;
-  const int sub = tid & (lanes - 1), R2 = a.R / 2;
+  const int q0 = a.part[0].wgs, k0 = q0 + a.part[1].wgs;
+  const int which = (int)blockIdx.x < q0 ? 0 : (int)blockIdx.x < k0 ? 1 : 2;
+  const RotaryPart pt = which == 0 ? a.part[0] : which == 1 ? a.part[1] : a.part[2];
+  const int wg = (int)blockIdx.x - (which == 0 ? 0 : which == 1 ? q0 : k0);
+  const bool turned = which < 2, norm = a.norm && turned;
+  const int sub = tid & (lanes - 1), R2 = turned ? a.R / 2 : 0, heads = pt.heads;
+  const bool whole = kVec && a.R % 16 == 0;
   const long long rows = (long long)a.B * a.n;
-  const Place pl(a.d, a.R, a.interleaved, sub);
-  float dwa[2][8], dwb[2][8];
+  const Place<kInter> pl(a.d, a.R, sub);
+  float wa[8], wb[8], dwa[8], dwb[8];
+  if (norm) load_weight(pt.w, pl, wa, wb);
   if constexpr (kBack) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) dwa[p][i] = dwb[p][i] = 0.f;
+    for (int i = 0; i < 8; ++i) dwa[i] = dwb[i] = 0.f;
   }
-  for (long long t0 = (long long)blockIdx.x * a.tokens; t0 < rows; t0 += (long long)gridDim.x * a.tokens) {
+  for (long long t0 = (long long)wg * a.tokens; t0 < rows; t0 += (long long)pt.wgs * a.tokens) {
     const int nt = (int)min((long long)a.tokens, rows - t0);
-    if (R2 > 0) {
-      __syncthreads();  // the last tokens' angles are read
-      for (int i = tid; i < nt * R2; i += kThreads) {
-        const int t = i / R2, f = i - t * R2;
-        const long long row = t0 + t;
-        const long long p = a.pos ? a.pos[row] : (int)((unsigned)row % (unsigned)a.n);
-        const unsigned turn = (unsigned)(((unsigned long long)p * a.turns.t[f]) >> 32);
-        float c, s;
-        cos_sin(turn, c, s);
-        cs[t * R2 + f] = make_float2(c * a.amplitude, (kBack ? -s : s) * a.amplitude);
-      }
-      __syncthreads();
+    __syncthreads();  // the last tokens' angles are read
+    if (tid < nt) {
+      const unsigned row = (unsigned)(t0 + tid), b = row / (unsigned)a.n;
+      live_of[tid] = !a.len || (int)(row - b * a.n) < clampi(a.len[b], 0, a.n);
     }
-    const int items = nt * a.heads, step = kThreads / lanes;
-    const int rounds = (items + step - 1) / step;  // whole rounds: sums over lanes stay in one wave's lanes
-    int item = tid / lanes;
-    for (int r = 0; r < rounds; ++r, item += step) {
-      const bool on = item < items;
-      const int t = on ? item / a.heads : 0, head = on ? item - t * a.heads : a.h2;
+    for (int i = tid; i < nt * R2; i += kThreads) {
+      const int t = i / R2, f = i - t * R2;
       const long long row = t0 + t;
-      const int part = head >= a.h2 ? 2 : head >= a.h1 ? 1 : 0;
-      const long long at = (long long)(head - (part == 2 ? a.h2 : part == 1 ? a.h1 : 0)) * a.d;
-      T* o = reinterpret_cast<T*>((part == 2 ? a.o[2] : part == 1 ? a.o[1] : a.o[0]) +
-                                  row * (part == 2 ? a.os[2] : part == 1 ? a.os[1] : a.os[0])) + at;
-      bool live = on;
-      if (a.len && on) {
-        const unsigned b = (unsigned)row / (unsigned)a.n;
-        live = (int)((unsigned)row - b * a.n) < clampi(a.len[b], 0, a.n);
-      }
+      const long long p = a.pos ? a.pos[row] : (int)((unsigned)row % (unsigned)a.n);
+      const unsigned turn = (unsigned)(((unsigned long long)p * a.turns.t[f]) >> 32);
+      float c, s;
+      cos_sin(turn, c, s);
+      cs[t][f] = c * a.amplitude;
+      sn[t][f] = (kBack ? -s : s) * a.amplitude;
+    }
+    __syncthreads();
+    const int items = nt * heads, step = kThreads / lanes;
+    const int rounds = (items + step - 1) / step;  // whole rounds: sums over lanes stay in one wave's lanes
+    int item = tid / lanes, t = item / heads, head = item - t * heads;
+    const int dt = step / heads, dh = step - dt * heads;
+    for (int r = 0; r < rounds; ++r) {
+      const bool on = item < items;
+      const int tok = on ? t : 0;
+      const long long row = t0 + tok, at = (long long)head * a.d * (int)sizeof(T);
+      const bool live = on && live_of[tok];
       Pairs<T, kVec> v, g;
 #pragma unroll
       for (int i = 0; i < 8; ++i) v.a[i] = v.b[i] = 0.f;
-      if (live && (!kBack || (a.norm && part < 2))) {
-        const T* x = reinterpret_cast<const T*>((part == 2 ? a.x[2] : part == 1 ? a.x[1] : a.x[0]) +
-                                                row * (part == 2 ? a.xs[2] : part == 1 ? a.xs[1] : a.xs[0])) + at;
-        load_pairs(v, x, pl);
-      }
-      float wa[8], wb[8];
-      const bool turned = part < 2;
-      if (a.norm && turned) load_weight(part == 1 ? a.w[1] : a.w[0], pl, wa, wb);
+      if (live && (!kBack || norm)) load_pairs(v, reinterpret_cast<const T*>(pt.x + row * pt.xs + at), pl);
+      T* o = reinterpret_cast<T*>(pt.o + row * pt.os + at);
       if constexpr (!kBack) {
-        if (a.norm && turned) {
-          // in every lane of the head alike
+        if (norm) {
           normalise(v, a, pl);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
@@ -276,45 +333,22 @@ __global__ __launch_bounds__(kThreads) void k_rotary(RotaryArgs a) {
             v.b[i] *= wb[i];
           }
         }
-        if (turned && live) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (i < pl.rot) {
-              const float2 z = cs[t * R2 + pl.p0 + i];
-              const float p = v.a[i], q = v.b[i];
-              v.a[i] = p * z.x - q * z.y;
-              v.b[i] = p * z.y + q * z.x;
-            }
-        }
+        if (turned && live) rotate(v, cs[tok], sn[tok], pl, whole);
         if (on) store_pairs(v, o, pl);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) g.a[i] = g.b[i] = 0.f;
         if (live) {
-          const T* p = reinterpret_cast<const T*>((part == 2 ? a.g[2] : part == 1 ? a.g[1] : a.g[0]) +
-                                                  row * (part == 2 ? a.gs[2] : part == 1 ? a.gs[1] : a.gs[0])) + at;
-          load_pairs(g, p, pl);
-          if (turned) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (i < pl.rot) {
-                const float2 z = cs[t * R2 + pl.p0 + i];
-                const float p = g.a[i], q = g.b[i];
-                g.a[i] = p * z.x - q * z.y;
-                g.b[i] = p * z.y + q * z.x;
-              }
-          }
+          load_pairs(g, reinterpret_cast<const T*>(pt.g + row * pt.gs + at), pl);
+          if (turned) rotate(g, cs[tok], sn[tok], pl, whole);
         }
-        if (a.norm && turned) {
+        if (norm) {
           const float inv = normalise(v, a, pl);
           float gh = 0.f, gs = 0.f;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const float ha = g.a[i] * v.a[i], hb = g.b[i] * v.b[i];
-            dwa[0][i] += part == 0 ? ha : 0.f;
-            dwb[0][i] += part == 0 ? hb : 0.f;
-            dwa[1][i] += part == 1 ? ha : 0.f;
-            dwb[1][i] += part == 1 ? hb : 0.f;
+            dwa[i] = fmaf(g.a[i], v.a[i], dwa[i]);
+            dwb[i] = fmaf(g.b[i], v.b[i], dwb[i]);
             g.a[i] *= wa[i];
             g.b[i] *= wb[i];
             gh = fmaf(g.a[i], v.a[i], fmaf(g.b[i], v.b[i], gh));
@@ -331,128 +365,159 @@ __global__ __launch_bounds__(kThreads) void k_rotary(RotaryArgs a) {
         }
         if (on) store_pairs(g, o, pl);
       }
+      item += step;
+      t += dt;
+      head += dh;
+      if (head >= heads) {
+        head -= heads;
+        ++t;
+      }
     }
   }
   if constexpr (kBack) {
-    if (!a.part) return;
+    if (!pt.part) return;
     // over the lanes of a wave that hold the same pairs, then over the waves
     const int w = tid >> 6;
 #pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float x = dwa[p][i], y = dwb[p][i];
-        for (int m = lanes; m < 64; m *= 2) {
-          x += __shfl_xor(x, m);
-          y += __shfl_xor(y, m);
-        }
-        if (lane < lanes && i < pl.live) {
-          red[w][p][pl.first(i)] = x;
-          red[w][p][pl.second(i)] = y;
-        }
+    for (int i = 0; i < 8; ++i) {
+      float x = dwa[i], y = dwb[i];
+      for (int m = lanes; m < 64; m *= 2) {
+        x += __shfl_xor(x, m);
+        y += __shfl_xor(y, m);
       }
-    __syncthreads();
-    for (int c = tid; c < 2 * a.d; c += kThreads) {
-      const int p = c >= a.d, e = p ? c - a.d : c;
-      a.part[((long long)blockIdx.x * 2 + p) * a.d + e] =
-          (red[0][p][e] + red[1][p][e]) + (red[2][p][e] + red[3][p][e]);
+      if (lane < lanes && i < pl.live) {
+        red[w][pl.first(i)] = x;
+        red[w][pl.second(i)] = y;
+      }
     }
+    __syncthreads();
+    for (int e = tid; e < a.d; e += kThreads)
+      pt.part[(long long)wg * a.d + e] = (red[0][e] + red[1][e]) + (red[2][e] + red[3][e]);
   }
 }
 
-// The workgroups' sums of 16 columns (of 2 d), 16 lanes a column, then a tree.
-__global__ __launch_bounds__(256) void k_rotary_weights(const float* __restrict__ part, float* __restrict__ dq_w,
-                                                        float* __restrict__ dk_w, int wgs, int d) {
+// The workgroups' sums of 16 columns, 16 lanes a column, then a tree.
+struct WeightSums {
+  const float* part[2];
+  float* out[2];
+  int wgs[2];
+};
+__global__ __launch_bounds__(256) void k_rotary_weights(WeightSums a, int d) {
   __shared__ float red[16][17];
-  const int col = threadIdx.x & 15, row = threadIdx.x >> 4, c = blockIdx.x * 16 + col;
+  const int m = blockIdx.y, col = threadIdx.x & 15, row = threadIdx.x >> 4, c = blockIdx.x * 16 + col;
+  if (!a.out[m]) return;
+  const float* p = a.part[m];
   float s = 0.f;
-  if (c < 2 * d)
-    for (int i = row; i < wgs; i += 16) s += part[(long long)i * 2 * d + c];
+  if (c < d) {
+#pragma unroll 8
+    for (int i = row; i < a.wgs[m]; i += 16) s += p[(long long)i * d + c];
+  }
   red[row][col] = s;
   __syncthreads();
   for (int h = 8; h > 0; h >>= 1) {
     if (row < h) red[row][col] += red[row + h][col];
     __syncthreads();
   }
-  if (row == 0 && c < 2 * d) {
-    float* o = c < d ? dq_w : dk_w;
-    if (o) o[c < d ? c : c - d] = red[0][col];
-  }
+  if (row == 0 && c < d) a.out[m][c] = red[0][col];
 }
 
-constexpr int kWeightWgs = 1024;  // workgroups that leave sums
+constexpr int kWeightWgs = 512;  // workgroups of a part that leave sums
 
-int tokens_of(long long rows) { return (int)std::max<long long>(1, std::min<long long>(kMaxTokens, rows / 2048)); }
+int lanes_of(int d) {
+  int lanes = 1;
+  while (lanes * 16 < d) lanes *= 2;
+  return lanes;
+}
+// Tokens of a workgroup at a time: enough for a head to every group of lanes, more where
+// there are many, since their angles are made together.
+int tokens_of(long long rows, int d, int heads) {
+  const long long fill = kThreads / lanes_of(d) / std::max(1, heads);
+  return (int)std::max<long long>(1, std::min<long long>(kMaxTokens, std::max(fill, rows / 1024)));
+}
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+template <typename T, bool kVec, bool kBack>
+void start(const RotaryArgs& a, int grid, int interleaved, hipStream_t s) {
+  if (interleaved)
+    hipLaunchKernelGGL((k_rotary<T, kVec, true, kBack>), dim3(grid), dim3(kThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_rotary<T, kVec, false, kBack>), dim3(grid), dim3(kThreads), 0, s, a);
+}
 
 template <bool kBack>
 hipError_t run(const Rotary& r, hipStream_t s) {
   RotaryArgs a;
-  const long long e = r.f32 ? 4 : 2;
+  const long long e = r.f32 ? 4 : 2, rows = (long long)r.B * r.n;
   const void* xs[3] = {r.q, r.k, r.v};
   const void* gs[3] = {r.gq, r.gk, r.gv};
   void* os[3] = {r.oq, r.ok, r.ov};
-  const int heads[3] = {os[0] ? r.Hq : 0, os[1] ? r.Hk : 0, os[2] ? r.Hk : 0};
   const long long ld[3] = {r.q_stride, r.k_stride, r.v_stride};
+  const float* ws[3] = {r.q_w, r.k_w, nullptr};
+  float* dw[3] = {r.dq_w, r.dk_w, nullptr};
+  a.tokens = tokens_of(rows, r.d, std::max(r.Hq, r.Hk));
+  const long long tiles = (rows + a.tokens - 1) / a.tokens;
   bool vec = true;
+  float* part = r.ws;
+  WeightSums sums = {};
+  int grid = 0;
   for (int i = 0; i < 3; ++i) {
-    const long long dense = (long long)(i == 0 ? r.Hq : r.Hk) * r.d;
-    a.x[i] = static_cast<const char*>(xs[i]);
-    a.g[i] = static_cast<const char*>(gs[i]);
-    a.o[i] = static_cast<char*>(os[i]);
-    a.xs[i] = ld[i] * e;
-    a.gs[i] = dense * e;
-    a.os[i] = (kBack ? ld[i] : dense) * e;
-    if (!os[i]) continue;
-    vec = vec && aligned16(xs[i]) && aligned16(gs[i]) && aligned16(os[i]) && ld[i] * e % 16 == 0 && dense * e % 16 == 0;
+    RotaryPart& p = a.part[i];
+    p.heads = os[i] ? (i == 0 ? r.Hq : r.Hk) : 0;
+    const long long dense = (long long)p.heads * r.d;
+    p.x = static_cast<const char*>(xs[i]);
+    p.g = static_cast<const char*>(gs[i]);
+    p.o = static_cast<char*>(os[i]);
+    p.xs = ld[i] * e;
+    p.gs = dense * e;
+    p.os = (kBack ? ld[i] : dense) * e;
+    p.w = ws[i];
+    p.part = nullptr;
+    p.wgs = os[i] ? (int)std::min<long long>(tiles, kBack && dw[i] ? kWeightWgs : 1 << 16) : 0;
+    grid += p.wgs;
+    if (kBack && dw[i]) {
+      p.part = part;
+      sums.part[i] = part;
+      sums.out[i] = dw[i];
+      sums.wgs[i] = p.wgs;
+      part += (long long)p.wgs * r.d;
+    }
+    if (os[i])
+      vec = vec && aligned16(xs[i]) && aligned16(gs[i]) && aligned16(os[i]) && ld[i] * e % 16 == 0 && dense * e % 16 == 0;
   }
   // sixteen elements of a lane as vectors: of the rotated part or of the rest, not both
   vec = vec && r.d % 16 == 0 && (r.interleaved || r.R % 16 == 0);
-  a.w[0] = r.q_w;
-  a.w[1] = r.k_w;
   a.len = r.len;
   a.pos = r.pos;
-  a.part = kBack && (r.dq_w || r.dk_w) ? r.ws : nullptr;
   a.B = r.B;
   a.n = r.n;
-  a.h1 = heads[0];
-  a.h2 = heads[0] + heads[1];
-  a.heads = a.h2 + heads[2];
   a.d = r.d;
   a.R = r.R;
-  a.lanes = 1;
-  while (a.lanes * 16 < r.d) a.lanes *= 2;
-  const long long rows = (long long)r.B * r.n;
-  a.tokens = tokens_of(rows);
-  a.interleaved = r.interleaved;
+  a.lanes = lanes_of(r.d);
   a.norm = r.norm;
   a.rms = r.rms;
   a.eps = r.eps;
   a.amplitude = r.amplitude;
   a.turns = r.turns;
-  const long long tiles = (rows + a.tokens - 1) / a.tokens;
-  const int wgs = (int)std::min<long long>(tiles, a.part ? kWeightWgs : 1 << 16);
-  const dim3 grid(wgs), block(kThreads);
   if (r.f32) {
     if (vec)
-      hipLaunchKernelGGL((k_rotary<float, true, kBack>), grid, block, 0, s, a);
+      start<float, true, kBack>(a, grid, r.interleaved, s);
     else
-      hipLaunchKernelGGL((k_rotary<float, false, kBack>), grid, block, 0, s, a);
+      start<float, false, kBack>(a, grid, r.interleaved, s);
   } else if (vec) {
-    hipLaunchKernelGGL((k_rotary<__bf16, true, kBack>), grid, block, 0, s, a);
+    start<__bf16, true, kBack>(a, grid, r.interleaved, s);
   } else {
-    hipLaunchKernelGGL((k_rotary<__bf16, false, kBack>), grid, block, 0, s, a);
+    start<__bf16, false, kBack>(a, grid, r.interleaved, s);
   }
-  if (a.part)
-    hipLaunchKernelGGL(k_rotary_weights, dim3((2 * r.d + 15) / 16), dim3(256), 0, s, a.part, r.dq_w, r.dk_w, wgs, r.d);
+  if (sums.out[0] || sums.out[1])
+    hipLaunchKernelGGL(k_rotary_weights, dim3((r.d + 15) / 16, 2), dim3(256), 0, s, sums, r.d);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t rotary_backward_floats(long long rows, int d) {
-  const int t = tokens_of(rows);
+size_t rotary_backward_floats(long long rows, int d, int heads) {
+  const int t = tokens_of(rows, d, heads);
   return (size_t)std::min<long long>((rows + t - 1) / t, kWeightWgs) * 2 * d;
 }
 hipError_t launch_rotary(const Rotary& r, hipStream_t s) { return run<false>(r, s); }
