@@ -126,8 +126,8 @@ typedef struct sc_ffn_desc {
 
 size_t sc_gated_ffn_workspace_size(const sc_ffn_desc *desc, int32_t save);
 
-/* Bytes of what the backward needs of the forward: the products x Wg and x Wu
- * to 24 bits and h, of the valid rows, in a layout private to the library. */
+/* Bytes of what the backward needs of the forward, of the valid rows: h, and
+ * act(g) and u act'(g) cut to 24 bits, in a layout private to the library. */
 size_t sc_gated_ffn_saved_size(const sc_ffn_desc *desc);
 
 /*
@@ -151,7 +151,7 @@ size_t sc_gated_ffn_backward_workspace_size(const sc_ffn_desc *desc);
 
 /*
  * Gradients of sc_gated_ffn from dy = dL/dy, bf16 [B, n, D]:
- *   dh = dy . Wd^T,  dg = bf16(dh u act'(g)),  du = bf16(dh act(g)),
+ *   dh = dy . Wd^T,  dg = bf16(dh (u act'(g))),  du = bf16(dh act(g)),
  *   dx = bf16(dg . Wg^T + du . Wu^T),
  *   dwg = bf16(x^T . dg),  dwu = bf16(x^T . du),  dwd = bf16(h^T . dy),
  * sums in float32 and in a fixed order, over rows too.

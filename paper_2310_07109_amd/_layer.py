@@ -219,7 +219,7 @@ def sc_gated_ffn(desc: FfnDesc, x, wg, wu, wd, y=None, saved=False, workspace=No
     call = _Call(stream, x)
     dt, ins = _ffn_inputs(call, desc, x, wg, wu, wd)
     cd = ctypes.byref(desc.c())
-    y = call.new(dt, x.shape) if y is None else y
+    y = torch.empty_like(x) if y is None else y
     ps = None
     if saved is True:
         saved = call.new(torch.uint8, (L.sc_gated_ffn_saved_size(cd),))
@@ -280,6 +280,6 @@ def sc_dropout(desc: DropoutDesc, x, seed, residual=None, out=None, stream=None)
     call.lengths(desc.valid_len, desc.B)
     px, ps = call.ptr(x, "x", dt, shape), call.ptr(seed, "seed", torch.int64, (1,))
     pr = call.opt(residual, "residual", dt, shape)
-    out = call.new(dt, shape) if out is None else out
+    out = torch.empty_like(x) if out is None else out
     _check(L.sc_dropout(ctypes.byref(desc.c()), px, ps, pr, call.ptr(out, "out", dt, shape), call.stream), "sc_dropout")
     return out

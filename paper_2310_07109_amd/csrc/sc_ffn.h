@@ -5,7 +5,7 @@
 // by direct loads, and the second kind is transposed on the way from LDS to the fragments
 // (ds_read_b64_tr_b16), so no operand is ever laid out anew.
 //
-//   kGate  g = x Wg, u = x Wu     h = act(g) u; g and u kept for the backward
+//   kGate  g = x Wg, u = x Wu     h = act(g) u; kept for the backward: act(g) and u act'(g)
 //   kDown  y = h Wd
 //   kDh    dh = dy Wd^T           dg = dh u act'(g), du = dh act(g)
 //   kDx    dx = dg Wg^T + du Wu^T, one sum over 2 F
@@ -29,7 +29,7 @@ typedef u32x4 __attribute__((aligned(2))) u32x4_any;
 typedef __attribute__((ext_vector_type(2), aligned(2))) unsigned u32x2_any;
 typedef f32x4 __attribute__((aligned(4))) f32x4_any;
 
-constexpr int kGate = 0, kDown = 1, kDh = 2, kDx = 3, kDwd = 4, kDwgu = 5, kGateKeep = 6;  // 6: kGate that keeps g and u
+constexpr int kGate = 0, kDown = 1, kDh = 2, kDx = 3, kDwd = 4, kDwgu = 5, kGateKeep = 6;  // 6: kGate that keeps the factors
 constexpr int kFfnWgs = 256;   // one workgroup per CU, each taking tiles in turn
 constexpr int kGroupTiles = 8;  // row tiles that share weights in an XCD's L2
 
@@ -60,7 +60,7 @@ struct FfnArgs {
   int map_a;         // a's rows are the batch's: read through map
   void* out[2];      // bf16: h | y | dg, du | dx | dwd | dwg, dwu
   int ld;            // elements of its rows
-  char* blocks;      // kGate: g and u for the backward, or null; kDh: to read
+  char* blocks;      // kGate: the factors for the backward, or null; kDh: to read
   int across;        // blocks of a row of blocks
   float* part;       // kDwd, kDwgu: sums of the slabs (one slab: null)
   int slabs;
@@ -181,9 +181,11 @@ SC_DEV f32x4 unpack24(const unsigned* w) {
                    __builtin_amdgcn_perm(w[2], w[1], 0x0403020cu), w[2] & 0xffffff00u};
   return __builtin_bit_cast(f32x4, u);
 }
-// What the backward needs of g and u: blocks of 16 rows by 32 columns, of a block a lane's
-// twelve words (g and u of its columns 4 g on, g and u of columns 16 + 4 g on) in three
-// planes of 16 bytes a lane, so that whole lines move.
+// What the backward needs of g and u, its two factors of dh: u act'(g) and act(g), made
+// where the exponential is at hand (from g and u themselves the backward's results took 34
+// of a tile's 64 us).  Blocks of 16 rows by 32 columns, of a block a lane's twelve words
+// (both factors of its columns 4 g on, both of columns 16 + 4 g on) in three planes of 16
+// bytes a lane, so that whole lines move.
 constexpr int kBlockBytes = 3 * 1024;
 SC_DEV char* block_at(char* blocks, int across, int ri, int cb, int lane) {
   return blocks + ((long long)ri * across + cb) * kBlockBytes + 16 * lane;
@@ -218,11 +220,24 @@ SC_DEV void store_row(__bf16* row, int col, int N, const unsigned (&v)[kCount / 
 }
 // Two fragments of 16 columns from column c on: a lane holds columns 4 g to 4 g + 3 of
 // each; exchanged between neighbouring groups, 8 of one.
+struct Pair {
+  unsigned v[4];
+  SC_DEV void set(const f32x4& a, const f32x4& b) {
+    const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16(a[0], a[1]), pack_bf16(b[0], b[1]), false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16(a[2], a[3]), pack_bf16(b[2], b[3]), false, false);
+    v[0] = (unsigned)lo[0];
+    v[1] = (unsigned)hi[0];
+    v[2] = (unsigned)lo[1];
+    v[3] = (unsigned)hi[1];
+  }
+  SC_DEV void store(__bf16* row, int c, int N, int g) const {
+    store_row<8>(row, c + 16 * (g & 1) + 8 * (g >> 1), N, v);
+  }
+};
 SC_DEV void store_pair(__bf16* row, int c, int N, int g, const f32x4& a, const f32x4& b, bool on) {
-  const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16(a[0], a[1]), pack_bf16(b[0], b[1]), false, false);
-  const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16(a[2], a[3]), pack_bf16(b[2], b[3]), false, false);
-  const unsigned v[4] = {(unsigned)lo[0], (unsigned)hi[0], (unsigned)lo[1], (unsigned)hi[1]};
-  if (on) store_row<8>(row, c + 16 * (g & 1) + 8 * (g >> 1), N, v);
+  Pair p;
+  p.set(a, b);
+  if (on) p.store(row, c, N, g);
 }
 SC_DEV void store_one(__bf16* row, int c, int N, int g, const f32x4& a, bool on) {
   const unsigned v[2] = {pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
@@ -431,11 +446,20 @@ struct FfnProduct {
     for (int j = 0; j < J; ++j) {
       const f32x4 gt = acc[i][j], up = acc[i][J + j];
       if constexpr (kKind == kGateKeep) {
-        pack24(gt, w + 6 * j);
-        pack24(up, w + 6 * j + 3);
-      }
+        f32x4 fg, fu;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) h[j][e] = act<kAct>(gt[e]) * up[e];
+        for (int e = 0; e < 4; ++e) {
+          float slope;
+          fu[e] = act_slope<kAct>(gt[e], slope);
+          fg[e] = up[e] * slope;
+          h[j][e] = fu[e] * up[e];
+        }
+        pack24(fg, w + 6 * j);
+        pack24(fu, w + 6 * j + 3);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[j][e] = act<kAct>(gt[e]) * up[e];
+      }
     }
     char* at = block_at(p.blocks, p.across, r0 / 16, c / 32, lane);
     if constexpr (J == 1) {
@@ -463,26 +487,19 @@ struct FfnProduct {
       for (int q = 0; q < 12; ++q) w[q] = 0;
     }
   }
-  SC_DEV void emit_dh(const Tile& t, int i, int j, int lane, const unsigned (&w)[12]) const {
-    const int g = lane >> 4, lr = lane & 15;
-    const int r = t.m0 + wm + 16 * i + lr, c = t.n0 + wn + 32 * j;
-    const bool on = r < R;
-    __bf16* dg = static_cast<__bf16*>(p.out[0]) + (long long)r * p.ld;
-    __bf16* du = static_cast<__bf16*>(p.out[1]) + (long long)r * p.ld;
+  SC_DEV void make_dh(int i, int j, const unsigned (&w)[12], Pair& dg, Pair& du) const {
     f32x4 vg[2], vu[2];
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
-      const f32x4 gt = unpack24(w + 6 * f), up = unpack24(w + 6 * f + 3);
+      const f32x4 fg = unpack24(w + 6 * f), fu = unpack24(w + 6 * f + 3);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float slope;
-        const float v = act_slope<kAct>(gt[e], slope), dh = acc[i][2 * j + f][e];
-        vg[f][e] = dh * up[e] * slope;
-        vu[f][e] = dh * v;
+        vg[f][e] = acc[i][2 * j + f][e] * fg[e];
+        vu[f][e] = acc[i][2 * j + f][e] * fu[e];
       }
     }
-    store_pair(dg, c, p.N, g, vg[0], vg[1], on);
-    store_pair(du, c, p.N, g, vu[0], vu[1], on);
+    dg.set(vg[0], vg[1]);
+    du.set(vu[0], vu[1]);
   }
   SC_DEV void emit_rows(const Tile& t, int i, int lane) const {  // kDown, kDx, kDwd, kDwgu
     const int g = lane >> 4, lr = lane & 15;
@@ -515,16 +532,29 @@ struct FfnProduct {
   SC_DEV void results(const Tile& t) const {
     const int lane = opaque_lane();
     if constexpr (kKind == kDh) {
-      // the blocks of kAhead units (16 rows by 32 columns) ahead are in flight
-      constexpr int kUnits = FI * FJ / 2, kAhead = kUnits < 3 ? kUnits : 3;
+      // Units of 16 rows by 32 columns, the factors of kAhead of them in flight.  Loads and
+      // stores retire in order, so a load behind a store waits for it: all factors come
+      // first, the results in the place of the sums, then all stores (mixed, 358 us for
+      // 32768 x 2816 x 1024, 225 without the loads and 250 without the stores).
+      constexpr int kJ = FJ / 2, kUnits = FI * kJ, kAhead = kUnits < 4 ? kUnits : 4;
       unsigned w[kAhead][12];
+      Pair dg[kUnits], du[kUnits];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) load_block(t, u / (FJ / 2), u % (FJ / 2), lane, w[u]);
+      for (int u = 0; u < kAhead; ++u) load_block(t, u / kJ, u % kJ, lane, w[u]);
 #pragma unroll
       for (int u = 0; u < kUnits; ++u) {
         __builtin_amdgcn_sched_barrier(0);
-        emit_dh(t, u / (FJ / 2), u % (FJ / 2), lane, w[u % kAhead]);
-        if (u + kAhead < kUnits) load_block(t, (u + kAhead) / (FJ / 2), (u + kAhead) % (FJ / 2), lane, w[u % kAhead]);
+        make_dh(u / kJ, u % kJ, w[u % kAhead], dg[u], du[u]);
+        if (u + kAhead < kUnits) load_block(t, (u + kAhead) / kJ, (u + kAhead) % kJ, lane, w[u % kAhead]);
+      }
+      const int g = lane >> 4, lr = lane & 15;
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) {
+        __builtin_amdgcn_sched_barrier(0);
+        const int r = t.m0 + wm + 16 * (u / kJ) + lr, c = t.n0 + wn + 32 * (u % kJ);
+        if (r >= R) continue;
+        dg[u].store(static_cast<__bf16*>(p.out[0]) + (long long)r * p.ld, c, p.N, g);
+        du[u].store(static_cast<__bf16*>(p.out[1]) + (long long)r * p.ld, c, p.N, g);
       }
     } else {
 #pragma unroll
@@ -615,7 +645,7 @@ inline bool ffn_odd(const Ffn& a) { return a.D % 8 != 0 || a.F % 8 != 0; }
 
 struct FfnSaved {
   char* h;      // [valid rows, Fp] bf16
-  char* blocks;  // g and u
+  char* blocks;  // the factors of dh
   size_t bytes;
 };
 inline FfnSaved ffn_saved(const Ffn& a, void* base) {
@@ -645,6 +675,7 @@ struct FfnCopy {
   char* dst;
   int rows, cols, pitch;  // elements; rows 0: the batch's valid rows
 };
+constexpr int kFfnCopies = 5;
 struct FfnRows {
   const int* len;
   int B, n;
@@ -654,7 +685,7 @@ struct FfnRows {
   long long zero_bytes;
   int always;  // the batch's rows are copied even if none is padding
   int copies;
-  FfnCopy copy[5];
+  FfnCopy copy[kFfnCopies];
 };
 }  // namespace
 

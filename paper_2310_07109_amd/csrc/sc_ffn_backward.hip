@@ -131,9 +131,7 @@ hipError_t launch_ffn_backward(const Ffn& a, hipStream_t s) {
     h.blocks = sv.blocks;
     h.across = (Fp + 31) / 32;
     const int tile = ffn_plan(T, Fp, (Dp + 63) / 64, 1).tile;
-    e = a.act == kActGelu   ? run_ffn<kDh, kActGelu>(h, tile, s)
-        : a.act == kActSilu ? run_ffn<kDh, kActSilu>(h, tile, s)
-                            : run_ffn<kDh, kActNone>(h, tile, s);
+    e = run_ffn<kDh, kActNone>(h, tile, s);
     if (e != hipSuccess) return e;
   }
   if (a.dx) {

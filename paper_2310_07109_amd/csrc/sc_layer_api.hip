@@ -91,8 +91,8 @@ sc_status turns_of(const sc_rotary_desc* d, const double* freq, sc::RotaryTurns*
   const long double turn = 6.283185307179586476925286766559L;
   for (int i = 0; i < d->rot_dim / 2; ++i) {
     if (!std::isfinite(freq[i])) return SC_EINVAL;
-    long double f = std::fmod((long double)freq[i] / turn, 1.0L);
-    if (f < 0) f += 1.0L;
+    long double f = (long double)freq[i] / turn;
+    f -= std::floor(f);
     // in 2^-64, modulo one turn
     const long double v = std::floor(f * 18446744073709551616.0L + 0.5L);
     t->t[i] = v >= 18446744073709551616.0L ? 0 : (unsigned long long)v;
