@@ -76,8 +76,8 @@ typedef struct sc_rotary_desc {
  * for the pairs (a, b) of u, pair i with frequency f_i; dimensions from rot_dim
  * on stay u.  Values are copied.  Float32 from the heads as read, rounded once;
  * angles are right to 2^-27 of a turn at any 32-bit position.
- *   freq     HOST float64 [rot_dim / 2], finite, read in the call (NULL without
- *            rot_dim).
+ *   freq     HOST float64 [rot_dim / 2], |f_i| < 2^20, read in the call (NULL
+ *            without rot_dim).
  *   q, k, v  head h of token (b, j) at (b n + j) stride + h d: dense (stride =
  *            heads * d) or parts of fused rows.  k and v may be NULL.
  *   q_w, k_w float32 [d] or NULL (1), with norm only.

@@ -227,9 +227,18 @@ hipError_t few_gate(const FewArgs& a, hipStream_t s) {
   return run_few<4, true, kAct, 8, 3>(a, s);
 }
 
-// The forward of a few rows, where nothing is kept and nothing has to be copied.
+// The forward of a few rows, where nothing is kept and nothing has to be copied.  us in a
+// graph, these two launches and the three of the tiles: 512 x 1536, 1 row 9.6 and 17.1, 128
+// rows 16.3 and 17.9; 768 x 2304, 1 row 10.7 and 21.2, 128 rows 19.3 and 22.8; 1024 x 4096,
+// 1 row 11.9 and 30.5, 128 rows 27.9 and 33.4.
 constexpr int kFewRows = 128;
-bool few_ok(const Ffn& a) { return !a.saved && !ffn_odd(a) && (long long)a.B * a.n <= kFewRows; }
+// Chunks beyond the contraction are asked for, up to 16 waves' last ones: their offsets
+// stay below 32 bits, and the buffers give zeros for them.
+constexpr long long kFewBeyond = 8192;
+bool few_ok(const Ffn& a) {
+  return !a.saved && !ffn_odd(a) && (long long)a.B * a.n <= kFewRows &&
+         (a.D + kFewBeyond) * 2 * a.F < (1LL << 32) && (a.F + kFewBeyond) * 2 * a.D < (1LL << 32);
+}
 
 hipError_t launch_few(const Ffn& a, char* h, hipStream_t s) {
   FewArgs g = {};

@@ -88,14 +88,18 @@ bool strided_overlap(const sc_rotary_desc* d, const void* p, const RotaryPart& a
 sc_status turns_of(const sc_rotary_desc* d, const double* freq, sc::RotaryTurns* t) {
   std::memset(t, 0, sizeof(*t));
   if (d->rot_dim > 0 && !freq) return SC_EINVAL;
-  const long double turn = 6.283185307179586476925286766559L;
+  // f / (2 pi) as a sum of two doubles, its fraction in 2^-64 (long double arithmetic takes
+  // 4 us of a call for 32 frequencies, this none to speak of).
+  constexpr double inv = 0.15915494309189535, inv_low = -9.839338337591243e-18, one = 18446744073709551616.0;
   for (int i = 0; i < d->rot_dim / 2; ++i) {
-    if (!std::isfinite(freq[i])) return SC_EINVAL;
-    long double f = (long double)freq[i] / turn;
-    f -= std::floor(f);
-    // in 2^-64, modulo one turn
-    const long double v = std::floor(f * 18446744073709551616.0L + 0.5L);
-    t->t[i] = v >= 18446744073709551616.0L ? 0 : (unsigned long long)v;
+    const double f = std::fabs(freq[i]), hi = f * inv;
+    if (!(f < 1048576.0)) return SC_EINVAL;
+    const double low = std::fma(f, inv, -hi) + f * inv_low;
+    double x = (hi - std::floor(hi)) * one;
+    const double whole = std::floor(x);
+    x = (x - whole) + low * one;  // some 2^30 units of 2^-64 at most, signed
+    const unsigned long long turn = (unsigned long long)whole + (unsigned long long)(long long)std::floor(x + 0.5);
+    t->t[i] = freq[i] < 0.0 ? 0 - turn : turn;
   }
   return SC_OK;
 }

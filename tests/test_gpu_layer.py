@@ -471,3 +471,256 @@ def test_dropout_mask_is_a_function_of_the_token():
     other = sc.sc_dropout(sc.DropoutDesc(2, 9, 100, 0.5, dtype=sc.SC_F32, site=1), torch.ones_like(x), s)
     again = sc.sc_dropout(sc.DropoutDesc(2, 9, 100, 0.5, dtype=sc.SC_F32), torch.ones_like(x), s + 1)
     assert not torch.equal(other, small) and not torch.equal(again, small)
+
+
+# ------------------------------------------------------- far from small ----
+def test_rotary_frequencies_of_any_size():
+    """Frequencies beyond a turn, negative and tiny ones, at the far ends of 32-bit positions; the angles from integers."""
+    from fractions import Fraction
+    # 1 / (2 pi) to 100 bits beyond what a double holds
+    inv = Fraction(15915494309189533576888376337251436203445964574046, 10 ** 50)
+    f = torch.tensor([1.0, -1.0, 300.25, -12345.678, 1e-9, -1e-9, 3.0, 0.0], dtype=torch.float64)
+    pos = torch.tensor([[0, 1, -1, 2 ** 31 - 1, -2 ** 31, 1048577, 77]], dtype=torch.int32)
+    n = pos.shape[1]
+    turns = torch.tensor([[float(Fraction(float(v)) * inv * int(p) % 1) for v in f] for p in pos[0]], dtype=torch.float64)
+    x = torch.randn((1, n, 1, 16), generator=gen(8))
+    out = sc.sc_rotary(sc.RotaryDesc(1, n, 1, 1, d=16, dtype=sc.SC_F32), f, x.to(DEV), positions=pos.to(DEV))[0]
+    want, mag = rotate64(x.double(), (turns * 2 * math.pi)[None], 1.0, 16, HALF)
+    assert_close(out, want, 6 * U * mag, "far")
+
+
+def test_dropout_offsets_past_32_bits():
+    """An array of 5.2 GB in place: its last rows, past 2^31 elements and 2^32 bytes."""
+    n, D = 40000, 65544
+    x = torch.full((1, n, D), 1.0, dtype=torch.bfloat16, device=DEV)
+    sc.sc_dropout(sc.DropoutDesc(1, n, D, 0.5), x, torch.tensor([5], device=DEV), out=x)
+    cols = np.arange(D // 8, dtype=np.uint64)
+    for j in (0, 32767, 39999):
+        w = philox((cols, 0 * cols + np.uint64(j), 0 * cols, 0 * cols), (5, 0))
+        r = np.stack([h for v in w for h in (v & np.uint64(0xFFFF), v >> np.uint64(16))], -1).reshape(-1).astype(np.int64)
+        assert torch.equal(x[0, j].cpu().float(), torch.from_numpy(r >= 32768).float() * 2)
+
+
+def test_ffn_offsets_next_to_32_bits():
+    """Rows of h that end 70 KB below 4 GiB, and what is kept beside them past 12 GB."""
+    torch.cuda.empty_cache()
+    ffn_ints_check(1, 32760, 40, 65544, (32760,), seed=3)
+
+
+def test_ffn_poisoned_outputs_and_workspaces():
+    """Nothing that a call writes has to hold anything before, NaNs included, in whole and ragged batches."""
+    for B, n, D, F, lens in ((2, 100, 64, 96, (100, 31)), (3, 77, 50, 33, None), (1, 300, 128, 256, (300,))):
+        L_dev, m, x, wg, wu, wd, dy = ffn_ints(B, n, D, F, lens, 2)
+        d = sc.FfnDesc(B, n, D, F, valid_len=L_dev)
+        dev = [t.to(DEV) for t in (x, wg, wu, wd)]
+        for save in (False, True):
+            y, s = sc.sc_gated_ffn(d, *dev, saved=save)
+            y2 = torch.full_like(y, float("nan"))
+            work = torch.full((sc.sc_gated_ffn_workspace_size(d, save),), 255, dtype=torch.uint8, device=DEV)
+            s2 = torch.full((sc.sc_gated_ffn_saved_size(d),), 255, dtype=torch.uint8, device=DEV) if save else False
+            sc.sc_gated_ffn(d, *dev, y=y2, saved=s2, workspace=work)
+            assert torch.equal(y, y2)
+        out = sc.sc_gated_ffn_backward(d, *dev, s, dy.to(DEV))
+        work = torch.full((sc.sc_gated_ffn_backward_workspace_size(d),), 255, dtype=torch.uint8, device=DEV)
+        got = sc.sc_gated_ffn_backward(d, *dev, s2, dy.to(DEV), workspace=work,
+                                       grads={k: torch.full_like(v, float("nan")) for k, v in out.items()})
+        for k in out:
+            assert torch.equal(out[k], got[k]), k
+
+
+def test_many_sequences():
+    """As many sequences as the packed rows' table holds, most of them empty; without lengths, more."""
+    ffn_ints_check(8192, 2, 16, 24, (0, 2, 0, 1, 0))
+    ffn_ints_check(9000, 1, 16, 24, None)
+    rotary_case(9000, 2, 1, 1, 16, 16, "bf16", True, HALF, lens=(2, 0, 1))
+    rotary_case(9000, 2, 1, 1, 16, 16, "bf16", True, HALF, lens=(2, 0, 1), backward=True)
+
+
+# ----------------------------------------------- graphs, streams, layers ----
+def layer_inputs(B, n, H, F, seed):
+    g = gen(seed)
+    D = 64 * H
+    bf16 = lambda *s: torch.randn(s, generator=g).to(torch.bfloat16)  # noqa: E731
+    w = dict(qkv=(torch.randn((D, 3 * D), generator=g) / math.sqrt(D)).to(torch.bfloat16),
+             o=(torch.randn((D, D), generator=g) / math.sqrt(D)).to(torch.bfloat16),
+             wg=(torch.randn((D, F), generator=g) / math.sqrt(D)).to(torch.bfloat16),
+             wu=(torch.randn((D, F), generator=g) / math.sqrt(D)).to(torch.bfloat16),
+             wd=(torch.randn((F, D), generator=g) / math.sqrt(F)).to(torch.bfloat16),
+             q_w=1 + 0.1 * torch.randn(64, generator=g), k_w=1 + 0.1 * torch.randn(64, generator=g))
+    return bf16(B, n, D), bf16(B, n, D), w
+
+
+class Layer:
+    """A training step of one encoder layer on the framework's operators."""
+
+    def __init__(self, B, n, H, F, valid_len, seed_dev, theta=None):
+        self.B, self.n, self.H, self.D, self.L, self.seed = B, n, H, 64 * H, valid_len, seed_dev
+        self.theta, self.temp = (1.0 / n if theta is None else theta), 0.5 / n
+        self.freq, _ = sc.sc_rotary_frequencies(64)
+        self.rot = sc.RotaryDesc(B, n, H, H, valid_len=valid_len, norm=True, eps=1e-5)
+        self.att = sc.Desc(B, n, H, 32, valid_len)
+        self.nd = sc.NormDesc(B, n, self.D, valid_len=valid_len, kind=sc.SC_NORM_RMS)
+        self.fd = sc.FfnDesc(B, n, self.D, F, valid_len=valid_len)
+        self.drops = [sc.DropoutDesc(B, n, self.D, 0.2, valid_len=valid_len, site=s) for s in range(2)]
+
+    def step(self, x, dout, w):
+        B, n, H, D = self.B, self.n, self.H, self.D
+        heads = lambda t: [t[..., i * D:(i + 1) * D].unflatten(-1, (H, 64)) for i in range(3)]  # noqa: E731
+        y0 = sc.sc_block_norm(self.nd, x, r=False)[1]
+        qkv = (y0.view(B * n, D) @ w["qkv"]).view(B, n, 3 * D)
+        hw = dict(q_w=w["q_w"], k_w=w["k_w"])
+        q, k, v = sc.sc_rotary(self.rot, self.freq, *heads(qkv), **hw)
+        o, lse, sp, _ = sc.sc_window_attention(self.att, q, k, v)
+        mask, y = sc.sc_ltp_soft_mask(self.att, sc.sc_ltp_score(self.att, sp), self.theta, self.temp, o)
+        t1 = (y.view(B * n, D) @ w["o"]).view(B, n, D)
+        r1 = sc.sc_dropout(self.drops[0], t1, self.seed, residual=x)
+        y1 = sc.sc_block_norm(self.nd, r1, r=False)[1]
+        fw = (w["wg"], w["wu"], w["wd"])
+        t2, saved = sc.sc_gated_ffn(self.fd, y1, *fw, saved=True)
+        out = sc.sc_dropout(self.drops[1], t2, self.seed, residual=r1)
+        g = sc.sc_gated_ffn_backward(self.fd, y1, *fw, saved, sc.sc_dropout(self.drops[1], dout, self.seed))
+        dr1 = sc.sc_block_norm_backward(self.nd, r1, dr=dout, dy=g["dx"])["dx"]
+        dt1 = sc.sc_dropout(self.drops[0], dr1, self.seed)
+        dy = (dt1.view(B * n, D) @ w["o"].t()).view(B, n, H, 64)
+        dq, dk, dv, dth = sc.sc_ltp_soft_backward(self.att, q, k, v, o, lse, mask, self.temp, dy)
+        dqkv = torch.zeros_like(qkv)
+        hg = sc.sc_rotary_backward(self.rot, self.freq, dq, dk, dv, *heads(qkv)[:2], **hw, grads=dict(
+            zip(("dq", "dk", "dv", "dq_w", "dk_w"), (*heads(dqkv), torch.empty_like(w["q_w"]), torch.empty_like(w["k_w"])))))
+        dy0 = (dqkv.view(B * n, 3 * D) @ w["qkv"].t()).view(B, n, D)
+        dx = sc.sc_block_norm_backward(self.nd, x, dr=dr1, dy=dy0)["dx"]
+        return dict(out=out, dx=dx, wg=g["dwg"], wu=g["dwu"], wd=g["dwd"], q_w=hg["dq_w"], k_w=hg["dk_w"])
+
+    def reference(self, x, dout, w, lens, seed):
+        """The same step by float64 autograd."""
+        B, n, H, D = self.B, self.n, self.H, self.D
+        leaf = {k: t.double().requires_grad_() for k, t in dict(w, x=x).items()}
+        m = valid_mask(lens, n)[..., None].double()
+        rms = lambda t: t * (t.pow(2).mean(-1, keepdim=True) + 1e-5).rsqrt()  # noqa: E731
+        qkv = rms(leaf["x"]) @ leaf["qkv"]
+        angle = torch.arange(n).double()[None, :, None] * self.freq
+        q, k, v = (qkv[..., i * D:(i + 1) * D].unflatten(-1, (H, 64)) for i in range(3))
+        q, k = (rotate64_graph(rms(t) * leaf[nm], angle) for t, nm in ((q, "q_w"), (k, "k_w")))
+        s = torch.matmul(q.transpose(1, 2), k.permute(0, 2, 3, 1)) * 0.125
+        i = torch.arange(n)
+        on = ((i[:, None] - i[None]).abs() <= 16)[None, None] & (m[:, None, None, :, 0] > 0)
+        p = torch.softmax(s.masked_fill(~on, -1e30), -1) * m[:, None]
+        o = torch.matmul(p, v.transpose(1, 2)).transpose(1, 2)
+        score = p.sum((1, 2)) / (H * lens.double()[:, None])
+        gate = torch.sigmoid((score - self.theta) / self.temp) * m[..., 0]
+        t1 = (o * gate[..., None, None]).flatten(-2) @ leaf["o"]
+        keep = [keep_mask(B, n, D, 0.2, seed, site) * (65536 / (65536 - round(0.2 * 65536))) for site in range(2)]
+        r1 = leaf["x"] + keep[0] * t1
+        y1 = rms(r1)
+        a, _ = act64(sc.SC_ACT_SILU, y1 @ leaf["wg"])
+        out = (r1 + keep[1] * ((a * (y1 @ leaf["wu"])) @ leaf["wd"])) * m
+        out.backward(dout.double())
+        return dict(out=out.detach(), dx=leaf["x"].grad, **{nm: leaf[nm].grad for nm in ("wg", "wu", "wd", "q_w", "k_w")})
+
+
+def rotate64_graph(x, angle):
+    c, s = angle.cos()[:, :, None], angle.sin()[:, :, None]
+    a, b = x[..., :32], x[..., 32:]
+    return torch.cat([a * c - b * s, a * s + b * c], -1)
+
+
+def test_layer_training_step():
+    """The operators together, against float64 autograd: about thirty roundings to bf16 of 2^-8 / sqrt(3) each lie
+    behind a gradient, which norms and softmax pass on at most doubled: 2 sqrt(30) 0.0023 = 0.025 of its 2-norm."""
+    B, n, H, F, seed = 3, 90, 2, 168, 1234567
+    lens = torch.tensor([90, 41, 64])
+    x, dout, w = layer_inputs(B, n, H, F, 5)
+    m = valid_mask(lens, n)
+    dout[~m] = 0
+    layer = Layer(B, n, H, F, lens.to(torch.int32).to(DEV), torch.tensor([seed], device=DEV))
+    got = layer.step(x.to(DEV), dout.to(DEV), {k: t.to(DEV) for k, t in w.items()})
+    want = layer.reference(x, dout, w, lens, seed)
+    for nm, v in want.items():
+        rel = float((got[nm].double().cpu() - v).norm() / v.norm())
+        assert rel <= 0.025, (nm, rel)
+
+
+def test_layer_step_in_a_graph():
+    """A captured training step, replayed with other inputs, lengths and seeds and eager steps between the replays."""
+    B, n, H, F = 2, 150, 2, 200
+    x, dout, w = layer_inputs(B, n, H, F, 6)
+    w = {k: t.to(DEV) for k, t in w.items()}
+    x, dout = x.to(DEV), dout.to(DEV)
+    L, seed = torch.tensor([150, 77], dtype=torch.int32, device=DEV), torch.tensor([1], device=DEV)
+    layer = Layer(B, n, H, F, L, seed)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        layer.step(x, dout, w)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            out = layer.step(x, dout, w)
+    torch.cuda.synchronize()
+    for i, lens in enumerate(([150, 77], [1, 150], [0, 0], [150, 150], [64, 33])):
+        x.copy_(torch.randn(x.shape, generator=gen(i)).to(torch.bfloat16))
+        dout.copy_(torch.randn(x.shape, generator=gen(i + 50)).to(torch.bfloat16))
+        L.copy_(torch.tensor(lens, dtype=torch.int32))
+        seed.fill_(i * 7919 - 3)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        first = {k: v.clone() for k, v in out.items()}
+        eager = layer.step(x, dout, w)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k, v in eager.items():
+            assert torch.equal(first[k], v) and torch.equal(out[k], v), (k, lens)
+
+
+def test_two_streams_at_once():
+    """Calls on two streams with their own outputs and workspaces, and one workspace for two graphs replayed in turn."""
+    B, n, D, F = 2, 300, 128, 256
+    g = gen(11)
+    xs = [torch.randn((B, n, D), generator=g).to(torch.bfloat16).to(DEV) for _ in range(2)]
+    w = [(torch.randn(s, generator=g) / math.sqrt(s[0])).to(torch.bfloat16).to(DEV) for s in ((D, F), (D, F), (F, D))]
+    L = torch.tensor([300, 123], dtype=torch.int32, device=DEV)
+    d = sc.FfnDesc(B, n, D, F, valid_len=L)
+    want = []
+    for x in xs:
+        y, s = sc.sc_gated_ffn(d, x, *w, saved=True)
+        want.append((y, sc.sc_gated_ffn_backward(d, x, *w, s, x)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(5):
+        for i, st in enumerate(streams):
+            y, s = sc.sc_gated_ffn(d, xs[i], *w, saved=True, stream=st)
+            got[i].append((y, s, sc.sc_gated_ffn_backward(d, xs[i], *w, s, xs[i], stream=st)))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for y, _, gr in got[i]:
+            assert torch.equal(y, want[i][0]) and all(torch.equal(gr[k], want[i][1][k]) for k in gr)
+    work = torch.empty(sc.sc_gated_ffn_workspace_size(d), dtype=torch.uint8, device=DEV)
+    ys, graphs = [torch.empty_like(x) for x in xs], []
+    with torch.cuda.stream(streams[0]):
+        for x, y in zip(xs, ys):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=streams[0]):
+                sc.sc_gated_ffn(d, x, *w, y=y, workspace=work)
+        for _ in range(3):
+            for gr in graphs:
+                gr.replay()
+    torch.cuda.synchronize()
+    for y, (ref, _) in zip(ys, want):
+        assert float((y.double() - ref.double()).norm()) <= 0.0035 * float(ref.double().norm())
+
+
+def test_debug_library_refuses_bad_lengths():
+    """The debug build reports lengths out of range; the release build clamps them."""
+    import ctypes
+    import os
+    if not os.path.exists(sc.debug_lib_path()):
+        pytest.skip("libsc_debug.so not built")
+    L = torch.tensor([5, 9], dtype=torch.int32, device=DEV)
+    x = torch.ones((2, 8, 16), dtype=torch.bfloat16, device=DEV)
+    seed, out = torch.tensor([1], device=DEV), torch.empty_like(x)
+    d = sc.DropoutDesc(2, 8, 16, 0.0, valid_len=L)
+    for lib, want in ((sc.load(), 0), (sc.load_debug(), -1)):
+        assert lib.sc_dropout(ctypes.byref(d.c()), x.data_ptr(), seed.data_ptr(), None, out.data_ptr(), None) == want
+    torch.cuda.synchronize()
+    assert torch.equal(out[1], x[1]) and not out[0, 5:].any()

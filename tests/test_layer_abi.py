@@ -94,10 +94,11 @@ def test_rotary_refusals(i):
         return L.sc_rotary(ctypes.byref(c), None if freq is None else freq.data_ptr(), q, k, v, qw, kw_, pos, qo, ko, vo,
                            None)
 
-    inf = torch.full((32,), math.inf, dtype=torch.float64)
+    inf, nan, far = (torch.full((32,), v, dtype=torch.float64) for v in (math.inf, math.nan, -2.0 ** 20))
     for bad in (dict(B=0), dict(n=0), dict(Hq=-1), dict(d=63), dict(d=0), dict(rot_dim=66), dict(rot_dim=-2),
                 dict(rot_dim=3), dict(layout=2), dict(patch=dict(norm=2)), dict(norm=True, kind=2),
                 dict(norm=True, eps=0.0), dict(amplitude=math.inf), dict(dtype=2), dict(freq=None), dict(freq=inf),
+                dict(freq=nan), dict(freq=far),
                 dict(q=None, k=None, v=None, qo=None, ko=None, vo=None), dict(qo=None), dict(q=None), dict(ko=None),
                 dict(qw=A[6]), dict(kw_=A[6]), dict(strides=(255, 128, 128)), dict(strides=(256, 128, 127)), dict(Hq=0),
                 dict(qo=A[1]), dict(qo=A[0] + 128), dict(ko=A[3] + 64), dict(pos=A[3]),
