@@ -30,7 +30,7 @@ typedef __attribute__((ext_vector_type(2), aligned(2))) unsigned u32x2_any;
 typedef f32x4 __attribute__((aligned(4))) f32x4_any;
 
 constexpr int kGate = 0, kDown = 1, kDh = 2, kDx = 3, kDwd = 4, kDwgu = 5, kGateKeep = 6;  // 6: kGate that keeps the factors
-constexpr int kFfnWgs = 256;   // one workgroup per CU, each taking tiles in turn
+constexpr int kFfnWgs = 256;   // CUs; workgroups take tiles in turn
 constexpr int kGroupTiles = 8;  // row tiles that share weights in an XCD's L2
 
 template <int kM>
@@ -601,7 +601,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
 
 template <int kKind, int kM, int kAct>
 hipError_t run_ffn(const FfnArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((k_ffn<kKind, kM, kAct>), dim3(kFfnWgs), dim3(512), 0, s, a);
+  hipLaunchKernelGGL((k_ffn<kKind, kM, kAct>), dim3(kM == 2 ? 2 * kFfnWgs : kFfnWgs), dim3(512), 0, s, a);
   return hipGetLastError();
 }
 // What a product costs with tiles of kind m, in ns: rounds of workgroups times the stages of
@@ -610,7 +610,10 @@ inline long long ffn_cost(int m, long long rows, long long cols, long long stage
   const long long bm = m == 0 ? 256 : m == 1 ? 128 : 64;
   const long long stage = m == 0 ? 1750 : m == 1 ? 560 : 210, fixed = m == 0 ? 12000 : m == 1 ? 6000 : 3500;
   const long long tiles = (rows + bm - 1) / bm * ((cols + bm - 1) / bm) * slabs;
-  return (tiles + kFfnWgs - 1) / kFfnWgs * ((stages + slabs - 1) / slabs * stage + fixed);
+  // 64 x 64 tiles: a CU holds two workgroups, which take half as long again for two tiles
+  const long long rounds = m < 2 ? 2 * ((tiles + kFfnWgs - 1) / kFfnWgs)
+                                 : tiles <= kFfnWgs ? 2 : 3 * ((tiles + 2 * kFfnWgs - 1) / (2 * kFfnWgs));
+  return rounds * ((stages + slabs - 1) / slabs * stage + fixed) / 2;
 }
 struct FfnPlan {
   int tile, slabs;
