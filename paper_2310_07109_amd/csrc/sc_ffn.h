@@ -605,27 +605,32 @@ hipError_t run_ffn(const FfnArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 // What a product costs with tiles of kind m, in ns: rounds of workgroups times the stages of
-// a tile and what stands beside them.
-inline long long ffn_cost(int m, long long rows, long long cols, long long stages, int slabs) {
+// a tile and what stands beside them (kDh reads and writes ten bytes for every result).  A CU
+// holds two workgroups of 64 x 64 tiles, which take about twice as long together.  From
+// launches of every kind, us with tiles of 256, 128 and 64: 2048 rows of 1024 x 2816, gate
+// 35, 39, 56, down 65, 27, 25, dh 40, 30, 32, dx 122, 53, 54; 1504 of 504 x 1112, gate 20,
+// 12, 18, down 31, 14, 8, dh 25, 14, 11, dx 57, 25, 17; 8192 of 1024 x 4096, gate 157, 263,
+// 371, down 106, 102, 146, dh 132, 158, 184, dx 202, 209, 321.
+inline long long ffn_cost(int m, long long rows, long long cols, long long stages, int slabs, bool dh) {
   const long long bm = m == 0 ? 256 : m == 1 ? 128 : 64;
-  const long long stage = m == 0 ? 1750 : m == 1 ? 560 : 210, fixed = m == 0 ? 12000 : m == 1 ? 6000 : 3500;
   const long long tiles = (rows + bm - 1) / bm * ((cols + bm - 1) / bm) * slabs;
-  // 64 x 64 tiles: a CU holds two workgroups, which take half as long again for two tiles
-  const long long rounds = m < 2 ? 2 * ((tiles + kFfnWgs - 1) / kFfnWgs)
-                                 : tiles <= kFfnWgs ? 2 : 3 * ((tiles + 2 * kFfnWgs - 1) / (2 * kFfnWgs));
-  return rounds * ((stages + slabs - 1) / slabs * stage + fixed) / 2;
+  const bool full = tiles >= kFfnWgs;
+  const long long stage = m == 0 ? (full ? 1750 : 1450) : m == 1 ? (full ? 700 : 570) : (full ? 560 : 300);
+  const long long fixed = m == 0 ? (dh ? 38000 : 9000) : m == 1 ? (dh ? 11000 : 4000) : (dh ? 3500 : 2500);
+  const long long at_once = m == 2 && tiles > kFfnWgs ? 2 * kFfnWgs : kFfnWgs;
+  return (tiles + at_once - 1) / at_once * ((stages + slabs - 1) / slabs * stage + fixed);
 }
 struct FfnPlan {
   int tile, slabs;
 };
 // most_slabs > 1: the contraction may be cut; each slab's sums are written and read again.
-inline FfnPlan ffn_plan(long long rows, long long cols, long long stages, int most_slabs) {
+inline FfnPlan ffn_plan(long long rows, long long cols, long long stages, int most_slabs, bool dh = false) {
   FfnPlan best = {0, 1};
   long long least = 1LL << 62;
   for (int m = 0; m < 3; ++m)
     for (int s = 1; s <= most_slabs && (s == 1 || s * 4 <= stages); ++s) {
       const long long extra = s == 1 ? 0 : 4000 + rows * cols * s * 8 / 5000;  // a launch, and 5 TB/s
-      const long long t = ffn_cost(m, rows, cols, stages, s) + extra;
+      const long long t = ffn_cost(m, rows, cols, stages, s, dh) + extra;
       if (t < least) {
         least = t;
         best = {m, s};

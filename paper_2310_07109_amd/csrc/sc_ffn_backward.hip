@@ -130,7 +130,7 @@ hipError_t launch_ffn_backward(const Ffn& a, hipStream_t s) {
     h.ld = Fp;
     h.blocks = sv.blocks;
     h.across = (Fp + 31) / 32;
-    const int tile = ffn_plan(T, Fp, (Dp + 63) / 64, 1).tile;
+    const int tile = ffn_plan(T, Fp, (Dp + 63) / 64, 1, true).tile;
     e = run_ffn<kDh, kActNone>(h, tile, s);
     if (e != hipSuccess) return e;
   }
