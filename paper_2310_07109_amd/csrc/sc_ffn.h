@@ -137,22 +137,17 @@ struct FfnPart {
     }
   }
   // kAlong with a contraction that ends inside the stage: units from `limit` on are zeros.
-  SC_DEV void issue(const u32x4 (&rsrc)[kSubs], unsigned lds, int w, int limit) const {
+  SC_DEV void issue_one(int t, const u32x4 (&rsrc)[kSubs], unsigned lds, int w, int limit) const {
+    const int sub = load_sub(w, t);
+    u32x4 d = rsrc[0];
+    if constexpr (kSubs == 2) d = sub ? rsrc[1] : rsrc[0];
+    const unsigned to = lds + (unsigned)(sub * 128 * kCols + load_at(w, t) * 1024);
     if (!kAcross && limit < 8) {
       const int lane = opaque_lane();
-#pragma unroll
-      for (int t = 0; t < kLoads; ++t) {
-        const int r = 8 * load_at(w, t) + (lane >> 3), unit = (lane & 7) ^ ((r >> 1) & 7);
-        lds_dma16_buf(rsrc[0], unit < limit ? voff[t] : kBeyond, lds + (unsigned)load_at(w, t) * 1024);
-      }
-      return;
-    }
-#pragma unroll
-    for (int t = 0; t < kLoads; ++t) {
-      const int sub = load_sub(w, t);
-      u32x4 d = rsrc[0];
-      if constexpr (kSubs == 2) d = sub ? rsrc[1] : rsrc[0];
-      lds_dma16_buf(d, voff[t], lds + (unsigned)(sub * 128 * kCols + load_at(w, t) * 1024));
+      const int r = 8 * load_at(w, t) + (lane >> 3), unit = (lane & 7) ^ ((r >> 1) & 7);
+      lds_dma16_buf(d, unit < limit ? voff[t] : kBeyond, to);
+    } else {
+      lds_dma16_buf(d, voff[t], to);
     }
   }
   // Fragment i of chunk c (32 of the stage's 64) of the part at LDS address `lds`.
@@ -330,21 +325,35 @@ struct FfnProduct {
     });
     b.offsets(lane, w, n0, p.b.ld, [&](int r) { return (unsigned)min(r, N - 1) * p.b.ld; });
   }
-  SC_DEV void issue(int s, int bf) const {
-    const unsigned at = lds0 + (unsigned)bf * kStage;
-    const int second = kKind == kDx && s >= seg, ks = k0 + (second ? s - seg : s);
-    const int limit = kOverRows || ks < seg - 1 ? 8 : (p.K - 64 * ks + 7) / 8;  // units of the stage (operands along the rows)
+  // A stage's loads, to be issued one by one; zeros past the tile's last stage, so that the
+  // number in flight is always the same.
+  struct Load {
+    u32x4 ra[1], rb[kSubs];
+    unsigned at;
+    int limit;
+  };
+  SC_DEV Load stage_load(int s, int bf) const {
+    Load l;
+    l.at = lds0 + (unsigned)bf * kStage;
+    const bool live = s < ns;
+    const int second = kKind == kDx && s >= seg, ks = live ? k0 + (second ? s - seg : s) : 0;
+    l.limit = kOverRows || ks < seg - 1 ? 8 : (p.K - 64 * ks + 7) / 8;  // units of the stage (operands along the rows)
     const unsigned skip_a = kAcrossA ? (unsigned)ks * 64 * p.a.ld : (unsigned)ks * 128;
     const unsigned skip_b = kAcrossB ? (unsigned)ks * 64 * p.b.ld : (unsigned)ks * 128;
-    const u32x4 ra[1] = {descriptor(second ? pa[1] : pa[0], bytes_a, skip_a)};
-    a.issue(ra, at, w, limit);
-    if constexpr (kSubs == 2) {
-      const u32x4 rb[2] = {descriptor(pb[0], bytes_b, skip_b), descriptor(pb[1], bytes_b, skip_b)};
-      b.issue(rb, at + A::kBytes, w, limit);
-    } else {
-      const u32x4 rb[1] = {descriptor((kKind == kDwgu ? sel : second) ? pb[1] : pb[0], bytes_b, skip_b)};
-      b.issue(rb, at + A::kBytes, w, limit);
-    }
+    const unsigned na = live ? bytes_a : skip_a, nb = live ? bytes_b : skip_b;
+    l.ra[0] = descriptor(second ? pa[1] : pa[0], na, skip_a);
+    l.rb[0] = descriptor((kKind == kDwgu ? sel : second) ? pb[1] : pb[0], nb, skip_b);
+    if constexpr (kSubs == 2) l.rb[1] = descriptor(pb[1], nb, skip_b);
+    return l;
+  }
+  SC_DEV void issue_a(const Load& l, int t) const { a.issue_one(t, l.ra, l.at, w, l.limit); }
+  SC_DEV void issue_b(const Load& l, int t) const { b.issue_one(t, l.rb, l.at + A::kBytes, w, l.limit); }
+  SC_DEV void issue(int s, int bf) const {
+    const Load l = stage_load(s, bf);
+#pragma unroll
+    for (int t = 0; t < A::kLoads; ++t) issue_a(l, t);
+#pragma unroll
+    for (int t = 0; t < B::kLoads; ++t) issue_b(l, t);
   }
   SC_DEV void cols(int q, int bf, int c) {
     const unsigned at = lds0 + (unsigned)bf * kStage + A::kBytes;
@@ -357,13 +366,20 @@ struct FfnProduct {
     for (int i = 0; i < FH; ++i) xf[q][i] = a.frag(at, h * FH + i, c);
     __builtin_amdgcn_sched_barrier(0);
   }
-  SC_DEV void mul(int h, int qx, int qw) {
+  // A half's products; between(i) after the i-th of its FH rows of fragments.
+  template <typename F>
+  SC_DEV void mul(int h, int qx, int qw, F between) {
 #pragma unroll
-    for (int i = 0; i < FH; ++i)
+    for (int i = 0; i < FH; ++i) {
 #pragma unroll
       for (int j = 0; j < FJ; ++j)
         acc[h * FH + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[qw][j], xf[qx][i], acc[h * FH + i][j], 0, 0, 0);
+      between(i);
+    }
     __builtin_amdgcn_sched_barrier(0);
+  }
+  SC_DEV void mul(int h, int qx, int qw) {
+    mul(h, qx, qw, [](int) {});
   }
   static SC_DEV int next_buf(int bf) { return bf == kNBuf - 1 ? 0 : bf + 1; }
 
@@ -375,15 +391,8 @@ struct FfnProduct {
                                  : kKind == kGate   ? FI
                                  : kKind == kDh     ? FI * FJ
                                                     : FI * FJ / 2;
+  static constexpr int kMost(int n) { return n < 63 ? n : 63; }  // the counter's end
   SC_DEV bool whole(const Tile& t) const { return t.m0 + BM <= rows() && t.n0 + BN / kSubs <= p.N; }
-  template <int kFrom>
-  SC_DEV void wait_first(bool stored, int later) const {
-    constexpr int kMost = 63 - (kNBuf - 1) * kDma;  // the counter ends at 63
-    if (stored)
-      wait_stages<kNBuf - kFrom, kDma, kStores < kMost ? kStores : kMost>(later);
-    else
-      wait_stages<kNBuf - kFrom, kDma>(later);
-  }
   // The tile's sums.  Every half's fragments are in flight during the products of the one
   // before, across stages too; one barrier a stage, before its last products: the next
   // stage has landed, and every wave holds its last fragments of this one, whose buffer is
@@ -394,42 +403,61 @@ struct FfnProduct {
 #pragma unroll
       for (int j = 0; j < FJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (kOverRows && ns == 0) return;
-    wait_first<0>(stored, min(ns, kNBuf) - 1);
+    if (stored)
+      wait_vm<kMost((kNBuf - 1) * kDma + kStores)>();
+    else
+      wait_vm<(kNBuf - 1) * kDma>();
     __syncthreads();
     int bf = 0;
     cols(0, 0, 0);
     rows(0, 0, 0, 0);
+    // The loads of a stage go out among the products, the first operand's in a stage's last
+    // half, the second's in the next one's first (all at once behind the barrier, the matrix
+    // units wait for them: dWg, dWu of 32768 x 1024 x 2816 386 us instead of 359).  The first
+    // stage's share of the second operand is loaded twice.
+    Load next = stage_load(kNBuf - 1, kNBuf - 1);
     for (int s = 0; s + 1 < ns; ++s) {
       const int bn = next_buf(bf);
+      half<true>(0, bf, next);
 #pragma unroll
-      for (int q = 0; q + 1 < 2 * kH; ++q) half(q, bf);
-      if (s + 1 < kNBuf)
-        wait_first<1>(stored, min(ns - 2 - s, kNBuf - 2));
+      for (int q = 1; q + 1 < 2 * kH; ++q) half<false>(q, bf, next);
+      if (stored && s + 1 < kNBuf)
+        wait_vm<kMost((kNBuf - 2) * kDma + kStores)>();
       else
-        wait_stages<kNBuf - 1, kDma>(min(ns - 2 - s, kNBuf - 2));
+        wait_vm<(kNBuf - 2) * kDma>();
       __syncthreads();
-      if (s + kNBuf < ns) issue(s + kNBuf, bf);
       cols(0, bn, 0);
       rows(0, bn, 0, 0);
-      mul((2 * kH - 1) % kH, 1, 1);
+      next = stage_load(s + kNBuf, bf);
+      mul((2 * kH - 1) % kH, 1, 1, [&](int i) {
+#pragma unroll
+        for (int t = i * A::kLoads / FH; t < (i + 1) * A::kLoads / FH; ++t) issue_a(next, t);
+        __builtin_amdgcn_sched_barrier(0);
+      });
       bf = bn;
     }
     // the last stage by itself: joined with the others, its products would wait for
     // fragments that the loop has just asked for
 #pragma unroll
-    for (int q = 0; q + 1 < 2 * kH; ++q) half(q, bf);
+    for (int q = 0; q + 1 < 2 * kH; ++q) half<false>(q, bf, next);
     mul((2 * kH - 1) % kH, 1, 1);
   }
   // Half q of a stage (of 2 kH, the last one apart), and the fragments of the next one.
-  SC_DEV void half(int q, int bf) {
+  template <bool kIssue>
+  SC_DEV void half(int q, int bf, const Load& next) {
     if (q + 1 == kH) cols(1, bf, 1);
     rows((q + 1) & 1, bf, (q + 1) / kH, (q + 1) % kH);
-    mul(q % kH, q & 1, q / kH);
+    mul(q % kH, q & 1, q / kH, [&](int i) {
+      if constexpr (kIssue) {
+#pragma unroll
+        for (int t = i * B::kLoads / FH; t < (i + 1) * B::kLoads / FH; ++t) issue_b(next, t);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    });
   }
   SC_DEV void start() {
 #pragma unroll
-    for (int s = 0; s < kNBuf; ++s)
-      if (s < ns) issue(s, s);
+    for (int s = 0; s < kNBuf; ++s) issue(s, s);
   }
 
   SC_DEV Tile tile() const { return {m0, n0, sel, slab}; }
@@ -594,9 +622,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
       p.start();
     }
     p.results(t);
-    if (!more) return;
+    if (!more) break;
     stored = p.whole(t);
   }
+  wait_vm<0>();  // no load may land after the workgroup's memory has gone to another
 }
 
 template <int kKind, int kM, int kAct>
@@ -614,8 +643,8 @@ hipError_t run_ffn(const FfnArgs& a, hipStream_t s) {
 inline long long ffn_cost(int m, long long rows, long long cols, long long stages, int slabs, bool dh) {
   const long long bm = m == 0 ? 256 : m == 1 ? 128 : 64;
   const long long tiles = (rows + bm - 1) / bm * ((cols + bm - 1) / bm) * slabs;
-  const bool full = tiles >= kFfnWgs;
-  const long long stage = m == 0 ? (full ? 1750 : 1450) : m == 1 ? (full ? 700 : 570) : (full ? 560 : 300);
+  const bool full = tiles > kFfnWgs / 2;
+  const long long stage = m == 0 ? (full ? 1750 : 1450) : m == 1 ? (full ? 700 : 570) : (tiles > kFfnWgs ? 560 : 300);
   const long long fixed = m == 0 ? (dh ? 38000 : 9000) : m == 1 ? (dh ? 11000 : 4000) : (dh ? 3500 : 2500);
   const long long at_once = m == 2 && tiles > kFfnWgs ? 2 * kFfnWgs : kFfnWgs;
   return (tiles + at_once - 1) / at_once * ((stages + slabs - 1) / slabs * stage + fixed);
