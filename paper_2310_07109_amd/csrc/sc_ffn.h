@@ -318,9 +318,10 @@ struct FfnProduct {
     m0 = __builtin_amdgcn_readfirstlane(m0);
     n0 = __builtin_amdgcn_readfirstlane(n0);
     const int M = rows(), N = p.N, lane = opaque_lane();
+    const bool mapped = p.map_a && R != p.T;
     a.offsets(lane, w, m0, p.a.ld, [&](int r) {
       int row = min(r, M - 1);
-      if (p.map_a) row = p.map[row];
+      if (mapped) row = p.map[row];
       return (unsigned)row * p.a.ld;
     });
     b.offsets(lane, w, n0, p.b.ld, [&](int r) { return (unsigned)min(r, N - 1) * p.b.ld; });
@@ -346,14 +347,9 @@ struct FfnProduct {
     if constexpr (kSubs == 2) l.rb[1] = descriptor(pb[1], nb, skip_b);
     return l;
   }
-  SC_DEV void issue_a(const Load& l, int t) const { a.issue_one(t, l.ra, l.at, w, l.limit); }
-  SC_DEV void issue_b(const Load& l, int t) const { b.issue_one(t, l.rb, l.at + A::kBytes, w, l.limit); }
-  SC_DEV void issue(int s, int bf) const {
-    const Load l = stage_load(s, bf);
-#pragma unroll
-    for (int t = 0; t < A::kLoads; ++t) issue_a(l, t);
-#pragma unroll
-    for (int t = 0; t < B::kLoads; ++t) issue_b(l, t);
+  SC_DEV void issue_one(const Load& l, int t) const {
+    if (t < A::kLoads) a.issue_one(t, l.ra, l.at, w, l.limit);
+    else b.issue_one(t - A::kLoads, l.rb, l.at + A::kBytes, w, l.limit);
   }
   SC_DEV void cols(int q, int bf, int c) {
     const unsigned at = lds0 + (unsigned)bf * kStage + A::kBytes;
@@ -411,16 +407,10 @@ struct FfnProduct {
     int bf = 0;
     cols(0, 0, 0);
     rows(0, 0, 0, 0);
-    // The loads of a stage go out among the products, the first operand's in a stage's last
-    // half, the second's in the next one's first (all at once behind the barrier, the matrix
-    // units wait for them: dWg, dWu of 32768 x 1024 x 2816 386 us instead of 359).  The first
-    // stage's share of the second operand is loaded twice.
-    Load next = stage_load(kNBuf - 1, kNBuf - 1);
     for (int s = 0; s + 1 < ns; ++s) {
       const int bn = next_buf(bf);
-      half<true>(0, bf, next);
 #pragma unroll
-      for (int q = 1; q + 1 < 2 * kH; ++q) half<false>(q, bf, next);
+      for (int q = 0; q + 1 < 2 * kH; ++q) half(q, bf);
       if (stored && s + 1 < kNBuf)
         wait_vm<kMost((kNBuf - 2) * kDma + kStores)>();
       else
@@ -428,10 +418,13 @@ struct FfnProduct {
       __syncthreads();
       cols(0, bn, 0);
       rows(0, bn, 0, 0);
-      next = stage_load(s + kNBuf, bf);
+      // The refill's loads go out among the products (all at once behind the barrier, the
+      // matrix units wait for them: dWg, dWu of 32768 x 1024 x 2816 386 us instead of 365;
+      // over all halves of the next stage, they land too late: 408).
+      const Load next = stage_load(s + kNBuf, bf);
       mul((2 * kH - 1) % kH, 1, 1, [&](int i) {
 #pragma unroll
-        for (int t = i * A::kLoads / FH; t < (i + 1) * A::kLoads / FH; ++t) issue_a(next, t);
+        for (int t = i * kDma / FH; t < (i + 1) * kDma / FH; ++t) issue_one(next, t);
         __builtin_amdgcn_sched_barrier(0);
       });
       bf = bn;
@@ -439,25 +432,22 @@ struct FfnProduct {
     // the last stage by itself: joined with the others, its products would wait for
     // fragments that the loop has just asked for
 #pragma unroll
-    for (int q = 0; q + 1 < 2 * kH; ++q) half<false>(q, bf, next);
+    for (int q = 0; q + 1 < 2 * kH; ++q) half(q, bf);
     mul((2 * kH - 1) % kH, 1, 1);
   }
   // Half q of a stage (of 2 kH, the last one apart), and the fragments of the next one.
-  template <bool kIssue>
-  SC_DEV void half(int q, int bf, const Load& next) {
+  SC_DEV void half(int q, int bf) {
     if (q + 1 == kH) cols(1, bf, 1);
     rows((q + 1) & 1, bf, (q + 1) / kH, (q + 1) % kH);
-    mul(q % kH, q & 1, q / kH, [&](int i) {
-      if constexpr (kIssue) {
-#pragma unroll
-        for (int t = i * B::kLoads / FH; t < (i + 1) * B::kLoads / FH; ++t) issue_b(next, t);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    });
+    mul(q % kH, q & 1, q / kH);
   }
   SC_DEV void start() {
 #pragma unroll
-    for (int s = 0; s < kNBuf; ++s) issue(s, s);
+    for (int s = 0; s < kNBuf; ++s) {
+      const Load l = stage_load(s, s);
+#pragma unroll
+      for (int t = 0; t < kDma; ++t) issue_one(l, t);
+    }
   }
 
   SC_DEV Tile tile() const { return {m0, n0, sel, slab}; }
@@ -552,7 +542,7 @@ struct FfnProduct {
       }
     }
     long long at = r;
-    if (!kOverRows && p.map && on) at = p.map[r];
+    if (!kOverRows && p.map && R != p.T && on) at = p.map[r];
     __bf16* row = static_cast<__bf16*>(t.sel ? p.out[1] : p.out[0]) + at * p.ld;
 #pragma unroll
     for (int j = 0; j < FJ; j += 2) store_pair(row, c + 16 * j, p.N, g, acc[i][j], acc[i][j + 1], on);
