@@ -724,3 +724,68 @@ def test_debug_library_refuses_bad_lengths():
         assert lib.sc_dropout(ctypes.byref(d.c()), x.data_ptr(), seed.data_ptr(), None, out.data_ptr(), None) == want
     torch.cuda.synchronize()
     assert torch.equal(out[1], x[1]) and not out[0, 5:].any()
+
+
+def off_by_one(t):
+    """The same values one element past an aligned address."""
+    buf = torch.empty(t.numel() + 1, dtype=t.dtype, device=t.device)
+    buf[1:] = t.reshape(-1)
+    return buf[1:].view(t.shape)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_any_element_address(dtype):
+    """Tensors aligned to their elements alone give what aligned ones give; the feed-forward block refuses them."""
+    dt, code, _ = TYPES[dtype]
+    g = gen(12)
+    for D in (64, 37):
+        x, r = (torch.randn((2, 9, D), generator=g).to(dt).to(DEV) for _ in range(2))
+        d, s = sc.DropoutDesc(2, 9, D, 0.3, dtype=code), torch.tensor([9], device=DEV)
+        want = sc.sc_dropout(d, x, s, residual=r)
+        assert torch.equal(sc.sc_dropout(d, off_by_one(x), s, residual=off_by_one(r), out=off_by_one(x)), want)
+    q = torch.randn((2, 9, 3, 64), generator=g).to(dt).to(DEV)
+    w = torch.rand(64, generator=g).to(DEV)
+    freq, _ = sc.sc_rotary_frequencies(64)
+    d = sc.RotaryDesc(2, 9, 3, 3, norm=True, dtype=code)
+    a, b = sc.sc_rotary(d, freq, q, q, q_w=w)[:2], sc.sc_rotary(d, freq, off_by_one(q), q, q_w=off_by_one(w))[:2]
+    for u, v in zip(a, b):
+        assert_close(u, v.double().cpu(), (4 * TYPES[dtype][2] * v.double().abs() + 64 * U).cpu(), "unaligned")
+    if dtype == "bf16":
+        f = sc.FfnDesc(2, 9, 64, 64)
+        x, m = q[:, :, 0].contiguous(), torch.zeros((64, 64), dtype=dt, device=DEV)
+        with pytest.raises(sc.ScError) as e:
+            sc.sc_gated_ffn(f, off_by_one(x), m, m, m)
+        assert e.value.status == -1
+
+
+def test_rotary_default_gradients_and_strides():
+    """Gradients allocated by the call, laid out as strided inputs; strides that are not a token's run are refused."""
+    B, n, H = 2, 11, 2
+    rows = torch.randn((B, n, 3 * H * 64 + 8), generator=gen(13)).to(torch.bfloat16).to(DEV)
+    q, k, v = (rows[..., i * 128:(i + 1) * 128].unflatten(-1, (H, 64)) for i in range(3))
+    go = [torch.randn((B, n, H, 64), generator=gen(i)).to(torch.bfloat16).to(DEV) for i in range(3)]
+    freq, _ = sc.sc_rotary_frequencies(64)
+    d = sc.RotaryDesc(B, n, H, H, norm=True)
+    w = dict(q_w=torch.rand(64, device=DEV), k_w=torch.rand(64, device=DEV))
+    a = sc.sc_rotary_backward(d, freq, *go, q=q, k=k, **w)
+    b = sc.sc_rotary_backward(d, freq, *go, q=q.contiguous(), k=k.contiguous(), **w)
+    assert all(torch.equal(a[nm], b[nm]) for nm in ("dq", "dk", "dv", "dq_w", "dk_w"))
+    only = sc.sc_rotary_backward(d, freq, go[0], q=q)
+    assert torch.equal(only["dq"], sc.sc_rotary_backward(d, freq, go[0], q=q.contiguous())["dq"]) and only["dk"] is None
+    for bad in (rows[..., :128].unflatten(-1, (64, H)).transpose(-1, -2), rows[:, ::1, :128].unflatten(-1, (H, 64)).flip(1)[:, :, :, ::2],
+                q.transpose(0, 1).contiguous().transpose(0, 1)):
+        with pytest.raises(ValueError):
+            sc.sc_rotary(d, freq, bad)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_rotary_many_heads(backward):
+    rotary_case(1, 5, 100, 1, 64, 64, "bf16", True, HALF, backward=backward)
+    rotary_case(2, 3, 2, 40, 256, 128, "f32", True, INTER, kind=sc.SC_NORM_LAYER, lens=(3, 2), backward=backward)
+
+
+@pytest.mark.parametrize("T", [1, 15, 16, 17, 32, 33, 64, 65, 127, 128, 129])
+def test_ffn_few_rows_exact(T):
+    """Around the borders of the few rows' kernels, widths that end inside their blocks and chunks."""
+    ffn_ints_check(1, T, 72, 104, None, seed=T)
+    ffn_ints_check(1, T, 1000, 2056, (T,), seed=T)
