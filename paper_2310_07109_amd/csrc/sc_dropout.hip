@@ -6,7 +6,9 @@
 //
 // A read of x (and the residual) and a write of out bound it, with the generator's twenty
 // 32 x 32 -> 64 bit products for eight elements beside them: at 16 bits an element both
-// take about as long, at 32 the products alone would.
+// take about as long, at 32 the products alone would.  32768 x 1024 bf16 with a residual, 30 us
+// for 201 MB, 38 among other work (part of the rows lie in the last-level cache); 1503 x 1111
+// float32, ragged, 5.
 #include <algorithm>
 
 #include "sc_device.h"

@@ -14,6 +14,13 @@
 //
 // A tile is BM x BN of a workgroup of eight waves; a stage is 64 of the contraction.
 // Sums are float32 in ascending order of the contraction, whatever the tile.
+//
+// The matrix units bound them, at the clock that their power leaves, and beside them the
+// results, which one workgroup a CU does not overlap with products.  32768 rows, D 1024,
+// F 2816, us (PFLOP/s): gate and its factors 391 (0.97), down 180 (1.05), dh 325 (0.58, with
+// 738 MB of factors and results), dx 300 (1.26), dWd 164 (1.15), dWg and dWu 341 (1.11); gate
+// alone, F 4096, 447 (1.23), down 225 (1.22).  A library's products of such shapes reach
+// 0.86 to 1.46 without the activation.
 #pragma once
 #include "sc_act.h"
 #include "sc_device.h"

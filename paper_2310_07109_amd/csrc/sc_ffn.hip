@@ -10,7 +10,8 @@ namespace {
 
 // A wavefront a row of one job: the numbering and the zeros of the batch's rows, then every
 // copy's rows (one after the other in the same wave, five jobs of an odd-sized batch took
-// 11 us for 1503 rows, side by side 8).
+// 11 us for 1503 rows, side by side 8).  The search for a row's place and memory bound it:
+// 32768 rows of 1024 to zero or number 6 us.
 __global__ __launch_bounds__(256) void k_ffn_rows(FfnRows a) {
   __shared__ int pre[kPackMaxB + 1];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

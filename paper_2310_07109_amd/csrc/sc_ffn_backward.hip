@@ -45,7 +45,8 @@ size_t carve(const Ffn& a, void* base, BackwardWs* out) {
   return c.off;
 }
 
-// The slabs' sums, in order, rounded once: up to three gradients of `count` elements.
+// The slabs' sums, in order, rounded once: up to three gradients of `count` elements.  HBM
+// bounds it: five slabs each of dWd, dWg and dWu of 1024 x 2816, 173 MB, 31 us.
 struct SlabSums {
   const float* part[3];
   __bf16* out[3];

@@ -69,12 +69,12 @@ sc_status rotary_parts(const sc_rotary_desc* d, const bool (&present)[3], Rotary
   return SC_OK;
 }
 
-// Whether a strided tensor of `rows` rows meets `other` (of `no` bytes): tensors that are
-// parts of the same fused rows lie between one another without sharing an element.
-bool strided_overlap(const sc_rotary_desc* d, const void* p, const RotaryPart& part, const void* other, size_t no) {
-  if (!p || !other || !overlaps(p, part.strided, other, no)) return false;
-  return true;
+// Whether a strided tensor meets `other`, of `no` bytes.
+bool strided_overlap(const void* p, const RotaryPart& part, const void* other, size_t no) {
+  return p && other && overlaps(p, part.strided, other, no);
 }
+// Whether two strided tensors do: parts of the same fused rows lie between one another
+// without sharing an element.
 bool strided_overlap(const sc_rotary_desc* d, const void* p, const RotaryPart& a, const void* q, const RotaryPart& b) {
   if (!p || !q || !overlaps(p, a.strided, q, b.strided)) return false;
   if (a.stride != b.stride) return true;
@@ -155,7 +155,7 @@ sc_status rotary_impl(const sc_rotary_desc* d, const double* freq, const void* q
     if (any_overlap(o, small)) return SC_EINVAL;
     for (int j = 0; j < 3; ++j) {
       const bool same = i == j && outs[i] == ins[j] && p[i].stride == p[i].heads * d->d;  // in place
-      if (!same && strided_overlap(d, ins[j], p[j], outs[i], p[i].dense)) return SC_EINVAL;
+      if (!same && strided_overlap(ins[j], p[j], outs[i], p[i].dense)) return SC_EINVAL;
       if (j < i && overlaps(outs[i], p[i].dense, outs[j], p[j].dense)) return SC_EINVAL;
     }
   }
@@ -200,18 +200,18 @@ sc_status rotary_backward_impl(const sc_rotary_desc* d, const double* freq, cons
       if (overlaps(sums[i].p, sums[i].n, sums[j].p, sums[j].n)) return SC_EINVAL;
     for (int j = 0; j < 3; ++j)
       if (present[j] && (overlaps(sums[i].p, sums[i].n, grads[j], p[j].dense) ||
-                         strided_overlap(d, ins[j], p[j], sums[i].p, sums[i].n) ||
-                         strided_overlap(d, outs[j], p[j], sums[i].p, sums[i].n)))
+                         strided_overlap(ins[j], p[j], sums[i].p, sums[i].n) ||
+                         strided_overlap(outs[j], p[j], sums[i].p, sums[i].n)))
         return SC_EINVAL;
   }
   for (int i = 0; i < 3; ++i) {
     if (!present[i]) continue;
     for (const Span& s : small)
-      if (strided_overlap(d, outs[i], p[i], s.p, s.n)) return SC_EINVAL;
+      if (strided_overlap(outs[i], p[i], s.p, s.n)) return SC_EINVAL;
     for (int j = 0; j < 3; ++j) {
       if (!present[j]) continue;
       const bool same = i == j && outs[i] == grads[j] && p[i].stride == p[i].heads * d->d;  // in place
-      if (!same && strided_overlap(d, outs[i], p[i], grads[j], p[j].dense)) return SC_EINVAL;
+      if (!same && strided_overlap(outs[i], p[i], grads[j], p[j].dense)) return SC_EINVAL;
       if (ins[j] && strided_overlap(d, outs[i], p[i], ins[j], p[j])) return SC_EINVAL;
       if (j < i && strided_overlap(d, outs[i], p[i], outs[j], p[j])) return SC_EINVAL;
     }

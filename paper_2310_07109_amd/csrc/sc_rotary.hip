@@ -5,9 +5,11 @@
 //   dx = inv (g - hat mean(g hat) - mean(g)),  g = w du,  hat = (x - mean) inv
 //   (mean only for LayerNorm), dw = sum du hat.
 //
-// One read and one write of every head bound it.  A lane holds eight pairs of a head,
-// both halves of each, so the rotation is within a lane and d / 16 lanes (rounded up
-// to a power of two) hold a head; its sums go over them by DPP.
+// One read and one write of every head bound it: 65536 rows of 12 + 12 + 12 heads of 64,
+// bf16, a third of them valid, 97 us for 413 MB (4.2 TB/s, where a copy reaches 5.1); backward
+// with RMS norms, 32768 rows of 16 + 4 + 4 heads of 64, bf16, 63 us for 285 MB (4.5).  A lane
+// holds eight pairs of a head, both halves of each, so the rotation is within a lane and
+// d / 16 lanes (rounded up to a power of two) hold a head; its sums go over them by DPP.
 //
 // The angles of a token serve all its heads: a workgroup makes the cosines and sines
 // of its tokens once, in LDS.  An angle is a turn in 64-bit fixed point: position times
@@ -396,7 +398,8 @@ __global__ __launch_bounds__(kThreads) void k_rotary(RotaryArgs a) {
   }
 }
 
-// The workgroups' sums of 16 columns, 16 lanes a column, then a tree.
+// The workgroups' sums of 16 columns, 16 lanes a column, then a tree: a chain of loads
+// bounds it, 4 us for 512 records of 64 channels of q and of k.
 struct WeightSums {
   const float* part[2];
   float* out[2];
