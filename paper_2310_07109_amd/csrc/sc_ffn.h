@@ -17,10 +17,10 @@
 //
 // The matrix units bound them, at the clock that their power leaves, and beside them the
 // results, which one workgroup a CU does not overlap with products.  32768 rows, D 1024,
-// F 2816, us (PFLOP/s): gate and its factors 391 (0.97), down 180 (1.05), dh 325 (0.58, with
-// 738 MB of factors and results), dx 300 (1.26), dWd 164 (1.15), dWg and dWu 341 (1.11); gate
-// alone, F 4096, 447 (1.23), down 225 (1.22).  A library's products of such shapes reach
-// 0.86 to 1.46 without the activation.
+// F 2816, us (PFLOP/s): gate and its factors 390 (0.97), down 180 (1.05), dh and dWd 474
+// (0.80, with 738 MB of factors and results of dh; apart 325 and 164), dx, dWg and dWu 643
+// (1.18; apart 300 and 341); gate alone, F 4096, 447 (1.23), down 225 (1.22).  A library's
+// products of such shapes reach 0.86 to 1.46 without the activation.
 #pragma once
 #include "sc_act.h"
 #include "sc_device.h"
@@ -295,9 +295,6 @@ struct FfnProduct {
     return (p.N + bn - 1) / bn * (both() ? 2 : 1);
   }
   SC_DEV bool both() const { return kKind == kDwgu && p.out[0] && p.out[1]; }
-  SC_DEV long long items() const {
-    return (long long)((rows() + BM - 1) / BM) * tiles_n() * (kOverRows ? p.slabs : 1);
-  }
   // Tiles in groups of kGroupTiles row tiles by all column tiles.
   SC_DEV void place(long long item) {
     const int T = (rows() + BM - 1) / BM, Nt = tiles_n();
@@ -592,28 +589,20 @@ struct FfnProduct {
   }
 };
 
-template <int kKind, int kM, int kAct>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_ffn(FfnArgs a) {
-  using P = FfnProduct<kKind, kM, kAct>;
-  __shared__ __attribute__((aligned(1024))) char stage[P::kNBuf * P::kStage];
-  const int R = a.count ? __builtin_amdgcn_readfirstlane(a.count[0]) : a.T;
-  P p(a, stage, R);
-  // The tiles go to the XCDs in contiguous ranges (workgroup i runs on XCD i % 8): what an
-  // XCD runs at a time shares rows and weights in its L2.
-  const long long items = p.items();
-  const int xcd = blockIdx.x & 7, step = gridDim.x >> 3;
-  const long long last = items * (xcd + 1) / 8;
-  long long it = items * xcd / 8 + (blockIdx.x >> 3);
+// A workgroup's tiles: `it` and what next() gives, until it is `last` or more.
+template <int kKind, int kM, int kAct, typename Next>
+SC_DEV void ffn_tiles(const FfnArgs& a, char* stage, int R, long long it, long long last, Next next) {
   if (it >= last) return;
+  FfnProduct<kKind, kM, kAct> p(a, stage, R);
   p.place(it);
   p.start();
   bool stored = false;
   while (true) {
     p.sums(stored);
-    const typename P::Tile t = p.tile();
-    const bool more = it + step < last;
+    const auto t = p.tile();
+    it = next(it);
+    const bool more = it < last;
     if (more) {  // the next tile's first stages are loaded during this one's results
-      it += step;
       p.place(it);
       __syncthreads();  // every wave has read the last stage
       p.start();
@@ -622,12 +611,76 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
     if (!more) break;
     stored = p.whole(t);
   }
-  wait_vm<0>();  // no load may land after the workgroup's memory has gone to another
+  wait_vm<0>();  // no load may land after the memory has gone to another
 }
+// The tiles go to the XCDs in contiguous ranges (workgroup i runs on XCD i % 8): what an XCD
+// runs at a time shares rows and weights in its L2.
+struct FfnShare {
+  long long first, last;
+  SC_DEV explicit FfnShare(long long items)
+      : first(items * (blockIdx.x & 7) / 8), last(items * ((blockIdx.x & 7) + 1) / 8) {}
+};
+template <int kKind, int kM>
+SC_DEV long long ffn_items(const FfnArgs& a, int R) {
+  using S = FfnTile<kM>;
+  constexpr bool over = kKind == kDwd || kKind == kDwgu, gate = kKind == kGate || kKind == kGateKeep;
+  constexpr int bn = S::kBN / (gate ? 2 : 1);
+  const int rows = over ? a.M : R;
+  return (long long)((rows + S::kBM - 1) / S::kBM) * ((a.N + bn - 1) / bn) * (over ? a.slabs : 1) *
+         (kKind == kDwgu && a.out[0] && a.out[1] ? 2 : 1);
+}
+SC_DEV int ffn_rows_of(const FfnArgs& a) { return a.count ? __builtin_amdgcn_readfirstlane(a.count[0]) : a.T; }
 
 template <int kKind, int kM, int kAct>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_ffn(FfnArgs a) {
+  using P = FfnProduct<kKind, kM, kAct>;
+  __shared__ __attribute__((aligned(1024))) char stage[P::kNBuf * P::kStage];
+  const int R = ffn_rows_of(a), step = gridDim.x >> 3;
+  const FfnShare share(ffn_items<kKind, kM>(a, R));
+  ffn_tiles<kKind, kM, kAct>(a, stage, R, share.first + (blockIdx.x >> 3), share.last,
+                             [=](long long it) { return it + step; });
+}
+
+// Two products that do not wait for each other in one launch: kSum over the batch's rows, in
+// slabs as long as about `ratio` tiles of kRow.  Every workgroup of an XCD takes its share of
+// the slabs; those that are left over go to the first workgroups, and the others take `ratio`
+// tiles of kRow for each.  Every second workgroup begins with its tiles of kRow, so that the
+// results of some are written during the products of others.
+template <int kRow, int kSum, int kM>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_ffn_two(FfnArgs a, FfnArgs b, int ratio) {
+  using P = FfnProduct<kRow, kM, kActNone>;
+  using Q = FfnProduct<kSum, kM, kActNone>;
+  static_assert(P::kNBuf * P::kStage == Q::kNBuf * Q::kStage, "one memory for both");
+  __shared__ __attribute__((aligned(1024))) char stage[P::kNBuf * P::kStage];
+  const int R = ffn_rows_of(a), wgs = gridDim.x >> 3, j = blockIdx.x >> 3;
+  const FfnShare row(ffn_items<kRow, kM>(a, R)), sum(ffn_items<kSum, kM>(b, R));
+  const int left = (int)((sum.last - sum.first) % wgs), others = wgs - left;
+  const long long edge = left ? row.first + (long long)ratio * others : row.first;
+  const bool before = left && j >= left;
+  for (int turn = 0; turn < 2; ++turn) {
+    if ((turn + j) & 1) {
+      ffn_tiles<kRow, kM, kActNone>(a, stage, R, before ? row.first + j - left : edge + j, row.last,
+                                    [=](long long it) {
+                                      if (it >= edge) return it + wgs;
+                                      return it + others < edge ? it + others : edge + j;
+                                    });
+    } else {
+      ffn_tiles<kSum, kM, kActNone>(b, stage, R, sum.first + j, sum.last, [=](long long it) { return it + wgs; });
+    }
+    __syncthreads();
+  }
+}
+
+template <int kM>
+constexpr int kFfnGrid = kM == 2 ? 2 * kFfnWgs : kFfnWgs;
+template <int kKind, int kM, int kAct>
 hipError_t run_ffn(const FfnArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((k_ffn<kKind, kM, kAct>), dim3(kM == 2 ? 2 * kFfnWgs : kFfnWgs), dim3(512), 0, s, a);
+  hipLaunchKernelGGL((k_ffn<kKind, kM, kAct>), dim3(kFfnGrid<kM>), dim3(512), 0, s, a);
+  return hipGetLastError();
+}
+template <int kRow, int kSum, int kM>
+hipError_t run_ffn_two(const FfnArgs& a, const FfnArgs& b, int ratio, hipStream_t s) {
+  hipLaunchKernelGGL((k_ffn_two<kRow, kSum, kM>), dim3(kFfnGrid<kM>), dim3(512), 0, s, a, b, ratio);
   return hipGetLastError();
 }
 // What a product costs with tiles of kind m, in ns: rounds of workgroups times the stages of
@@ -637,14 +690,20 @@ hipError_t run_ffn(const FfnArgs& a, hipStream_t s) {
 // 35, 39, 56, down 65, 27, 25, dh 40, 30, 32, dx 122, 53, 54; 1504 of 504 x 1112, gate 20,
 // 12, 18, down 31, 14, 8, dh 25, 14, 11, dx 57, 25, 17; 8192 of 1024 x 4096, gate 157, 263,
 // 371, down 106, 102, 146, dh 132, 158, 184, dx 202, 209, 321.
-inline long long ffn_cost(int m, long long rows, long long cols, long long stages, int slabs, bool dh) {
+inline long long ffn_fixed(int m, bool dh) {
+  return m == 0 ? (dh ? 38000 : 9000) : m == 1 ? (dh ? 11000 : 4000) : (dh ? 3500 : 2500);
+}
+inline long long ffn_stage(int m, long long tiles) {
+  return m == 0 ? (tiles > kFfnWgs / 2 ? 1750 : 1450) : m == 1 ? (tiles > kFfnWgs / 2 ? 700 : 570) : tiles > kFfnWgs ? 560 : 300;
+}
+inline long long ffn_at_once(int m, long long tiles) { return m == 2 && tiles > kFfnWgs ? 2 * kFfnWgs : kFfnWgs; }
+inline long long ffn_tiles_of(int m, long long rows, long long cols) {
   const long long bm = m == 0 ? 256 : m == 1 ? 128 : 64;
-  const long long tiles = (rows + bm - 1) / bm * ((cols + bm - 1) / bm) * slabs;
-  const bool full = tiles > kFfnWgs / 2;
-  const long long stage = m == 0 ? (full ? 1750 : 1450) : m == 1 ? (full ? 700 : 570) : (tiles > kFfnWgs ? 560 : 300);
-  const long long fixed = m == 0 ? (dh ? 38000 : 9000) : m == 1 ? (dh ? 11000 : 4000) : (dh ? 3500 : 2500);
-  const long long at_once = m == 2 && tiles > kFfnWgs ? 2 * kFfnWgs : kFfnWgs;
-  return (tiles + at_once - 1) / at_once * ((stages + slabs - 1) / slabs * stage + fixed);
+  return (rows + bm - 1) / bm * ((cols + bm - 1) / bm);
+}
+inline long long ffn_cost(int m, long long rows, long long cols, long long stages, int slabs, bool dh) {
+  const long long tiles = ffn_tiles_of(m, rows, cols) * slabs, at_once = ffn_at_once(m, tiles);
+  return (tiles + at_once - 1) / at_once * ((stages + slabs - 1) / slabs * ffn_stage(m, tiles) + ffn_fixed(m, dh));
 }
 struct FfnPlan {
   int tile, slabs;
@@ -664,11 +723,52 @@ inline FfnPlan ffn_plan(long long rows, long long cols, long long stages, int mo
     }
   return best;
 }
+// One product over rows and one in slabs, of plans of their own, as one launch with tiles of
+// kind `tile`, or as two (-1).  Plans of one kind are joined; others where the tiles of a
+// launch, dealt evenly with half of the longest at its end, cost less than both rounded up
+// and a launch.  The whole backward in a graph, us, joined and not: 512 x 512 x 1536 36.7 and
+// 40.7, 1504 x 504 x 1112 42 and 53, 1024 x 768 x 2304 58 and 67, 2048 x 1024 x 2816 126 and
+// 146, 16384 x 768 x 2048 377 and 396; of two kinds joined as 256 x 256, 8192 x 768 x 2304
+// 310 and 285.
+struct FfnSize {
+  long long rows, cols, stages;
+  bool dh;
+};
+struct FfnTwoPlan {
+  int tile, ratio;  // ratio: tiles of the first that take as long as one of the second
+};
+inline FfnTwoPlan ffn_plan_two(const FfnSize& a, const FfnPlan& pa, const FfnSize& b, const FfnPlan& pb) {
+  const long long launch = 2000;
+  long long least = ffn_cost(pa.tile, a.rows, a.cols, a.stages, 1, a.dh) +
+                    ffn_cost(pb.tile, b.rows, b.cols, b.stages, pb.slabs, b.dh) + launch;
+  FfnTwoPlan best = {-1, 1};
+  const bool same = pa.tile == pb.tile;
+  for (int m = same ? pa.tile : 1; m < (same ? pa.tile + 1 : 3); ++m) {
+    const long long na = ffn_tiles_of(m, a.rows, a.cols), nb = ffn_tiles_of(m, b.rows, b.cols) * pb.slabs, n = na + nb;
+    const long long ta = a.stages * ffn_stage(m, n) + ffn_fixed(m, a.dh),
+                    tb = (b.stages + pb.slabs - 1) / pb.slabs * ffn_stage(m, n) + ffn_fixed(m, b.dh);
+    const long long most = ta > tb ? ta : tb, at_once = ffn_at_once(m, n);
+    const long long t = n <= at_once ? most : (na * ta + nb * tb) / at_once + most / 2;
+    if (same || t < least) {
+      least = t;
+      const long long r = (tb + ta / 2) / ta;
+      best = {m, (int)(r < 1 ? 1 : r > 1 << 20 ? 1 << 20 : r)};
+    }
+  }
+  return best;
+}
 template <int kKind, int kAct>
 hipError_t run_ffn(const FfnArgs& a, int tile, hipStream_t s) {
   if (tile == 0) return run_ffn<kKind, 0, kAct>(a, s);
   if (tile == 1) return run_ffn<kKind, 1, kAct>(a, s);
   return run_ffn<kKind, 2, kAct>(a, s);
+}
+
+template <int kRow, int kSum>
+hipError_t run_ffn_two(const FfnArgs& a, const FfnArgs& b, int tile, int ratio, hipStream_t s) {
+  if (tile == 0) return run_ffn_two<kRow, kSum, 0>(a, b, ratio, s);
+  if (tile == 1) return run_ffn_two<kRow, kSum, 1>(a, b, ratio, s);
+  return run_ffn_two<kRow, kSum, 2>(a, b, ratio, s);
 }
 
 // -------------------------------------------------------------- sizes ----

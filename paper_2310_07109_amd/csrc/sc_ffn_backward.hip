@@ -120,74 +120,85 @@ hipError_t launch_ffn_backward(const Ffn& a, hipStream_t s) {
   FfnArgs base = {};
   base.T = (int)T;
   base.count = ws.count;
-  if (a.dx || a.dwg || a.dwu) {
-    FfnArgs h = base;
-    h.a = opdy;
-    h.b = {{wd, nullptr}, nullptr, 2u * Dp, a.F};
-    h.N = Fp;
-    h.K = Dp;
-    h.out[0] = ws.dg;
-    h.out[1] = ws.du;
-    h.ld = Fp;
-    h.blocks = sv.blocks;
-    h.across = (Fp + 31) / 32;
-    const int tile = ffn_plan(T, Fp, (Dp + 63) / 64, 1, true).tile;
-    e = run_ffn<kDh, kActNone>(h, tile, s);
-    if (e != hipSuccess) return e;
-  }
-  if (a.dx) {
-    FfnArgs d = base;
-    d.map = ws.map;
-    d.a = {{ws.dg, ws.du}, nullptr, 2u * Fp, 0};
-    d.b = {{wg, wu}, nullptr, 2u * Fp, a.D};
-    d.N = a.D;
-    d.K = Fp;
-    d.out[0] = a.dx;
-    d.ld = a.D;
-    e = run_ffn<kDx, kActNone>(d, ffn_plan(T, a.D, 2 * ((Fp + 63) / 64), 1).tile, s);
-    if (e != hipSuccess) return e;
-  }
+  FfnArgs dh = base, dx = base, dwd = base, dwgu = base;
   SlabSums sums = {};
   sums.count = DF;
-  if (a.dwd) {
-    FfnArgs d = base;
-    d.a = {{sv.h, nullptr}, nullptr, 2u * Fp, 0};
-    d.b = opdy;
-    d.M = a.F;
-    d.N = a.D;
-    d.out[0] = a.dwd;
-    d.ld = a.D;
-    const FfnPlan plan = weight_plan(a, 1);
-    d.slabs = plan.slabs;
-    d.part = ws.part_d;
-    e = run_ffn<kDwd, kActNone>(d, plan.tile, s);
+  const bool need_dh = a.dx || a.dwg || a.dwu;
+  const FfnSize size_h = {T, Fp, (Dp + 63) / 64, true}, size_x = {T, a.D, 2 * ((Fp + 63) / 64), false},
+                size_d = {a.D, a.F, (T + 63) / 64, false}, size_gu = {a.D, 2LL * a.F, (T + 63) / 64, false};
+  const FfnPlan plan_h = ffn_plan(size_h.rows, size_h.cols, size_h.stages, 1, true),
+                plan_x = ffn_plan(size_x.rows, size_x.cols, size_x.stages, 1), plan_d = weight_plan(a, 1),
+                plan_gu = weight_plan(a, 2);
+  const FfnTwoPlan two_h = ffn_plan_two(size_h, plan_h, size_d, plan_d),
+                   two_x = ffn_plan_two(size_x, plan_x, size_gu, plan_gu);
+  dh.a = opdy;
+  dh.b = {{wd, nullptr}, nullptr, 2u * Dp, a.F};
+  dh.N = Fp;
+  dh.K = Dp;
+  dh.out[0] = ws.dg;
+  dh.out[1] = ws.du;
+  dh.ld = Fp;
+  dh.blocks = sv.blocks;
+  dh.across = (Fp + 31) / 32;
+  dx.map = ws.map;
+  dx.a = {{ws.dg, ws.du}, nullptr, 2u * Fp, 0};
+  dx.b = {{wg, wu}, nullptr, 2u * Fp, a.D};
+  dx.N = a.D;
+  dx.K = Fp;
+  dx.out[0] = a.dx;
+  dx.ld = a.D;
+  dwd.a = {{sv.h, nullptr}, nullptr, 2u * Fp, 0};
+  dwd.b = opdy;
+  dwd.M = a.F;
+  dwd.N = a.D;
+  dwd.out[0] = a.dwd;
+  dwd.ld = a.D;
+  dwd.slabs = plan_d.slabs;
+  dwd.part = ws.part_d;
+  dwgu.a = opx;
+  dwgu.b = {{ws.dg, ws.du}, nullptr, 2u * Fp, 0};
+  dwgu.M = a.D;
+  dwgu.N = a.F;
+  dwgu.out[0] = a.dwg;
+  dwgu.out[1] = a.dwu;
+  dwgu.ld = a.F;
+  dwgu.slabs = plan_gu.slabs;
+  dwgu.part = ws.part_gu;
+  if (a.dwd && dwd.slabs > 1) {
+    sums.part[0] = ws.part_d;
+    sums.out[0] = static_cast<__bf16*>(a.dwd);
+    sums.slabs[0] = dwd.slabs;
+  }
+  if (dwgu.slabs > 1)
+    for (int i = 0; i < 2; ++i) {
+      sums.part[1 + i] = ws.part_gu + i * dwgu.slabs * DF;
+      sums.out[1 + i] = static_cast<__bf16*>(i ? a.dwu : a.dwg);
+      sums.slabs[1 + i] = dwgu.slabs;
+    }
+  if (need_dh && a.dwd && two_h.tile >= 0) {
+    e = run_ffn_two<kDh, kDwd>(dh, dwd, two_h.tile, two_h.ratio, s);
     if (e != hipSuccess) return e;
-    if (d.slabs > 1) {
-      sums.part[0] = ws.part_d;
-      sums.out[0] = static_cast<__bf16*>(a.dwd);
-      sums.slabs[0] = d.slabs;
+  } else {
+    if (need_dh) {
+      e = run_ffn<kDh, kActNone>(dh, plan_h.tile, s);
+      if (e != hipSuccess) return e;
+    }
+    if (a.dwd) {
+      e = run_ffn<kDwd, kActNone>(dwd, plan_d.tile, s);
+      if (e != hipSuccess) return e;
     }
   }
-  if (a.dwg || a.dwu) {
-    FfnArgs d = base;
-    d.a = opx;
-    d.b = {{ws.dg, ws.du}, nullptr, 2u * Fp, 0};
-    d.M = a.D;
-    d.N = a.F;
-    d.out[0] = a.dwg;
-    d.out[1] = a.dwu;
-    d.ld = a.F;
-    const FfnPlan plan = weight_plan(a, 2);
-    d.slabs = plan.slabs;
-    d.part = ws.part_gu;
-    e = run_ffn<kDwgu, kActNone>(d, plan.tile, s);
+  if (a.dx && a.dwg && a.dwu && two_x.tile >= 0) {
+    e = run_ffn_two<kDx, kDwgu>(dx, dwgu, two_x.tile, two_x.ratio, s);
     if (e != hipSuccess) return e;
-    if (d.slabs > 1) {
-      for (int i = 0; i < 2; ++i) {
-        sums.part[1 + i] = ws.part_gu + i * d.slabs * DF;
-        sums.out[1 + i] = static_cast<__bf16*>(i ? a.dwu : a.dwg);
-        sums.slabs[1 + i] = d.slabs;
-      }
+  } else {
+    if (a.dx) {
+      e = run_ffn<kDx, kActNone>(dx, plan_x.tile, s);
+      if (e != hipSuccess) return e;
+    }
+    if (a.dwg || a.dwu) {
+      e = run_ffn<kDwgu, kActNone>(dwgu, plan_gu.tile, s);
+      if (e != hipSuccess) return e;
     }
   }
   if (sums.out[0] || sums.out[1] || sums.out[2]) {

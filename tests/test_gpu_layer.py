@@ -789,3 +789,19 @@ def test_ffn_few_rows_exact(T):
     """Around the borders of the few rows' kernels, widths that end inside their blocks and chunks."""
     ffn_ints_check(1, T, 72, 104, None, seed=T)
     ffn_ints_check(1, T, 1000, 2056, (T,), seed=T)
+
+
+@pytest.mark.parametrize("B,n,D,F,lens", [
+    (1, 1024, 768, 2304, None), (2, 1024, 1024, 2816, (1024, 700)), (2, 1024, 4096, 512, (1000, 1024)),
+    (1, 5000, 80, 64, None), (8, 2048, 768, 2048, (2048, 2048, 5, 0, 1999)), (8, 2048, 768, 2048, (0, 3, 0, 0))])
+def test_ffn_joined_products(B, n, D, F, lens):
+    """Backward products that share a launch, with as many tiles as the sizes say, fewer and none; a gradient asked for
+    alone, in launches of its own, is the same."""
+    ffn_ints_check(B, n, D, F, lens)
+    L_dev, m, x, wg, wu, wd, dy = (t.to(DEV) if t is not None else None for t in ffn_ints(B, n, D, F, lens, 1))
+    d = sc.FfnDesc(B, n, D, F, valid_len=L_dev)
+    _, saved = sc.sc_gated_ffn(d, x, wg, wu, wd, saved=True)
+    out = sc.sc_gated_ffn_backward(d, x, wg, wu, wd, saved, dy)
+    for nm, v in out.items():
+        alone = sc.sc_gated_ffn_backward(d, x, wg, wu, wd, saved, dy, grads={nm: torch.empty_like(v)})[nm]
+        assert torch.equal(alone, v), nm
