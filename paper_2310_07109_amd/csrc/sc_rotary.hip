@@ -5,11 +5,12 @@
 //   dx = inv (g - hat mean(g hat) - mean(g)),  g = w du,  hat = (x - mean) inv
 //   (mean only for LayerNorm), dw = sum du hat.
 //
-// One read and one write of every head bound it: 65536 rows of 12 + 12 + 12 heads of 64,
-// bf16, a third of them valid, 97 us for 413 MB (4.2 TB/s, where a copy reaches 5.1); backward
-// with RMS norms, 32768 rows of 16 + 4 + 4 heads of 64, bf16, 63 us for 285 MB (4.5).  A lane
-// holds eight pairs of a head, both halves of each, so the rotation is within a lane and
-// d / 16 lanes (rounded up to a power of two) hold a head; its sums go over them by DPP.
+// One read and one write of every head bound it: 32768 rows of 12 + 12 + 12 heads of 64, bf16,
+// 63 us for 302 MB (4.8 TB/s, where a copy reaches 5.1), of 65536 rows, a third of them valid,
+// 80 us for 413 MB; backward with RMS norms, 32768 rows of 16 + 4 + 4 heads, 62 us for 285 MB
+// (4.6).  A lane holds eight pairs of a head, both halves of each, so the rotation is within a
+// lane and d / 16 lanes (rounded up to a power of two) hold a head; its sums go over them by
+// DPP.
 //
 // The angles of a token serve all its heads: a workgroup makes the cosines and sines
 // of its tokens once, in LDS.  An angle is a turn in 64-bit fixed point: position times
@@ -36,14 +37,14 @@ struct RotaryPart {
   long long xs, gs, os;   // bytes between tokens
   const float* w;         // or null
   float* part;            // backward: [workgroups, d] sums of the weight's gradient, or null
-  int heads, wgs;
+  int heads, wgs, move;
 };
 struct RotaryArgs {
   RotaryPart part[3];  // q, k, v
   const int* len;
   const int* pos;
   int B, n, d, R, lanes;  // lanes of a head
-  int tokens, norm, rms;
+  int tokens, tiles, norm, rms, in_turn;
   float eps, amplitude;
   RotaryTurns turns;
 };
@@ -79,68 +80,45 @@ SC_DEV float head_sum(float v, int lanes) {
   return v;
 }
 
+// kN (4 or 8) successive elements at a vector's address.
+template <int kN, typename T>
+SC_DEV void take(const T* p, float* v) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int h = 0; h < kN / 4; ++h) {
+      const f32x4 x = reinterpret_cast<const f32x4*>(p)[h];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[4 * h + i] = x[i];
+    }
+  } else {
+    typedef __attribute__((ext_vector_type(kN / 2))) unsigned Vec;
+    const Vec u = *reinterpret_cast<const Vec*>(p);
+#pragma unroll
+    for (int i = 0; i < kN / 2; ++i) {
+      v[2 * i] = __builtin_bit_cast(float, u[i] << 16);
+      v[2 * i + 1] = __builtin_bit_cast(float, u[i] & 0xffff0000u);
+    }
+  }
+}
+template <int kN, typename T>
+SC_DEV void put(T* p, const float* v) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int h = 0; h < kN / 4; ++h)
+      reinterpret_cast<f32x4*>(p)[h] = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+  } else {
+    typedef __attribute__((ext_vector_type(kN / 2))) unsigned Vec;
+    Vec u;
+#pragma unroll
+    for (int i = 0; i < kN / 2; ++i) u[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+    *reinterpret_cast<Vec*>(p) = u;
+  }
+}
+
 // Eight pairs of a head, pair i at elements e0 + i, e1 + i (half) or e0 + 2 i,
 // e0 + 2 i + 1 (interleaved).
-template <typename T, bool kVec>
 struct Pairs {
   float a[8], b[8];
-  SC_DEV static void vec(const T* p, float (&v)[8]) {  // eight elements at 16 bytes
-    if constexpr (sizeof(T) == 4) {
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i < 4 ? lo[i & 3] : hi[i & 3];
-    } else {
-      const u32x4 u = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __builtin_bit_cast(float, u[i] << 16);
-        v[2 * i + 1] = __builtin_bit_cast(float, u[i] & 0xffff0000u);
-      }
-    }
-  }
-  SC_DEV static void put(T* p, const float (&v)[8]) {
-    if constexpr (sizeof(T) == 4) {
-      *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-      *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
-    } else {
-      *reinterpret_cast<u32x4*>(p) =
-          u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-    }
-  }
-  SC_DEV void take(const T* p) {  // eight interleaved pairs
-    if constexpr (sizeof(T) == 4) {
-      f32x4 x[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = reinterpret_cast<const f32x4*>(p)[j];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        a[i] = x[i / 2][2 * (i & 1)];
-        b[i] = x[i / 2][2 * (i & 1) + 1];
-      }
-    } else {
-      u32x4 x[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) x[j] = reinterpret_cast<const u32x4*>(p)[j];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const unsigned u = x[i / 4][i & 3];
-        a[i] = __builtin_bit_cast(float, u << 16);
-        b[i] = __builtin_bit_cast(float, u & 0xffff0000u);
-      }
-    }
-  }
-  SC_DEV void give(T* p) const {
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        reinterpret_cast<f32x4*>(p)[j] = f32x4{a[2 * j], b[2 * j], a[2 * j + 1], b[2 * j + 1]};
-    } else {
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-        reinterpret_cast<u32x4*>(p)[j] = u32x4{pack_bf16(a[4 * j], b[4 * j]), pack_bf16(a[4 * j + 1], b[4 * j + 1]),
-                                               pack_bf16(a[4 * j + 2], b[4 * j + 2]), pack_bf16(a[4 * j + 3], b[4 * j + 3])};
-    }
-  }
 };
 
 // Where a lane's pairs are: pair i (of the lane) is live below `live`, rotated below
@@ -160,21 +138,33 @@ struct Place {
   }
 };
 
-template <typename T, bool kVec, bool kInter>
-SC_DEV void load_pairs(Pairs<T, kVec>& v, const T* x, const Place<kInter>& pl) {
+// kVec: pairs of a vector, 8 or 4, which are all rotated, all passed or all beyond the head's
+// end; 0: an element an access.
+template <int kVec, typename T, bool kInter>
+SC_DEV void load_pairs(Pairs& v, const T* x, const Place<kInter>& pl) {
   if constexpr (kVec) {
-    // lanes beyond the head's end read its start, and keep nothing of it
-    const bool live = pl.live > 0;
-    if constexpr (kInter) {
-      v.take(x + (live ? pl.first(0) : 0));
-    } else {
-      Pairs<T, kVec>::vec(x + (live ? pl.first(0) : 0), v.a);
-      Pairs<T, kVec>::vec(x + (live ? pl.second(0) : 0), v.b);
-    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      v.a[i] = live ? v.a[i] : 0.f;
-      v.b[i] = live ? v.b[i] : 0.f;
+    for (int h = 0; h < 8; h += kVec) {
+      const bool live = h < pl.live;  // beyond the head's end its start is read, and nothing of it kept
+      if constexpr (kInter) {
+        float e[2 * kVec];
+        const T* p = x + (live ? pl.first(h) : 0);
+        take<kVec>(p, e);
+        take<kVec>(p + kVec, e + kVec);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          v.a[h + i] = live ? e[2 * i] : 0.f;
+          v.b[h + i] = live ? e[2 * i + 1] : 0.f;
+        }
+      } else {
+        take<kVec>(x + (live ? pl.first(h) : 0), v.a + h);
+        take<kVec>(x + (live ? pl.second(h) : 0), v.b + h);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          v.a[h + i] = live ? v.a[h + i] : 0.f;
+          v.b[h + i] = live ? v.b[h + i] : 0.f;
+        }
+      }
     }
   } else {
 #pragma unroll
@@ -185,15 +175,25 @@ SC_DEV void load_pairs(Pairs<T, kVec>& v, const T* x, const Place<kInter>& pl) {
   }
 }
 
-template <typename T, bool kVec, bool kInter>
-SC_DEV void store_pairs(const Pairs<T, kVec>& v, T* x, const Place<kInter>& pl) {
+template <int kVec, typename T, bool kInter>
+SC_DEV void store_pairs(const Pairs& v, T* x, const Place<kInter>& pl) {
   if constexpr (kVec) {
-    if (pl.live <= 0) return;
-    if constexpr (kInter) {
-      v.give(x + pl.first(0));
-    } else {
-      Pairs<T, kVec>::put(x + pl.first(0), v.a);
-      Pairs<T, kVec>::put(x + pl.second(0), v.b);
+#pragma unroll
+    for (int h = 0; h < 8; h += kVec) {
+      if (h >= pl.live) return;
+      if constexpr (kInter) {
+        float e[2 * kVec];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          e[2 * i] = v.a[h + i];
+          e[2 * i + 1] = v.b[h + i];
+        }
+        put<kVec>(x + pl.first(h), e);
+        put<kVec>(x + pl.first(h) + kVec, e + kVec);
+      } else {
+        put<kVec>(x + pl.first(h), v.a + h);
+        put<kVec>(x + pl.second(h), v.b + h);
+      }
     }
   } else {
 #pragma unroll
@@ -218,8 +218,8 @@ SC_DEV void load_weight(const float* w, const Place<kInter>& pl, float (&a)[8], 
 
 // The normalised head in place of x (elements beyond the head's end stay 0); returns
 // 1 / deviation.
-template <typename P, bool kInter>
-SC_DEV float normalise(P& v, const RotaryArgs& a, const Place<kInter>& pl) {
+template <bool kInter>
+SC_DEV float normalise(Pairs& v, const RotaryArgs& a, const Place<kInter>& pl) {
   const float scale = 1.f / (float)a.d;
   if (!a.rms) {
     float s = 0.f;
@@ -245,47 +245,34 @@ SC_DEV float normalise(P& v, const RotaryArgs& a, const Place<kInter>& pl) {
 }
 
 // The rotation of a lane's pairs by the cosines and sines of a token, kept apart in LDS.
-template <typename P, bool kInter>
-SC_DEV void rotate(P& v, const float* cs, const float* sn, const Place<kInter>& pl, bool whole) {
-  if (whole) {  // all eight pairs or none
-    if (pl.rot <= 0) return;
-    float c[8], s[8];
+template <bool kInter>
+SC_DEV void rotate(Pairs& v, const float* cs, const float* sn, const Place<kInter>& pl) {
+  if (pl.rot <= 0) return;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(cs + pl.p0 + 4 * h);
-      const f32x4 y = *reinterpret_cast<const f32x4*>(sn + pl.p0 + 4 * h);
+  for (int h = 0; h < 8; h += 4) {
+    const f32x4 c = *reinterpret_cast<const f32x4*>(cs + pl.p0 + h), s = *reinterpret_cast<const f32x4*>(sn + pl.p0 + h);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) c[4 * h + e] = x[e], s[4 * h + e] = y[e];
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int e = 0; e < 4; ++e) {
+      const int i = h + e;
       const float p = v.a[i], q = v.b[i];
-      v.a[i] = p * c[i] - q * s[i];
-      v.b[i] = p * s[i] + q * c[i];
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float c = cs[pl.p0 + i], s = sn[pl.p0 + i], p = v.a[i], q = v.b[i];
-      v.a[i] = i < pl.rot ? p * c - q * s : p;
-      v.b[i] = i < pl.rot ? p * s + q * c : q;
+      v.a[i] = i < pl.rot ? p * c[e] - q * s[e] : p;
+      v.b[i] = i < pl.rot ? p * s[e] + q * c[e] : q;
     }
   }
 }
 
-template <typename T, bool kVec, bool kInter, bool kBack>
+template <typename T, int kVec, bool kInter, bool kBack>
 __global__ __launch_bounds__(kThreads) void k_rotary(RotaryArgs a) {
   __shared__ __attribute__((aligned(16))) float cs[kMaxTokens][kRotaryMaxD / 2], sn[kMaxTokens][kRotaryMaxD / 2];
   __shared__ int live_of[kMaxTokens];
   __shared__ float red[kBack ? 4 : 1][256];
   const int tid = threadIdx.x, lane = tid & 63, lanes = a.lanes;
-  const int q0 = a.part[0].wgs, k0 = q0 + a.part[1].wgs;
-  const int which = (int)blockIdx.x < q0 ? 0 : (int)blockIdx.x < k0 ? 1 : 2;
+  const int q0 = a.part[0].wgs, k0 = q0 + a.part[1].wgs, bid = blockIdx.x;
+  const int which = a.in_turn ? bid % 3 : bid < q0 ? 0 : bid < k0 ? 1 : 2;
   const RotaryPart pt = which == 0 ? a.part[0] : which == 1 ? a.part[1] : a.part[2];
-  const int wg = (int)blockIdx.x - (which == 0 ? 0 : which == 1 ? q0 : k0);
+  const int wg = a.in_turn ? bid / 3 : bid - (which == 0 ? 0 : which == 1 ? q0 : k0);
   const bool turned = which < 2, norm = a.norm && turned;
   const int sub = tid & (lanes - 1), R2 = turned ? a.R / 2 : 0, heads = pt.heads;
-  const bool whole = kVec && a.R % 16 == 0;
   const long long rows = (long long)a.B * a.n;
   const Place<kInter> pl(a.d, a.R, sub);
   float wa[8], wb[8], dwa[8], dwb[8];
@@ -294,15 +281,24 @@ __global__ __launch_bounds__(kThreads) void k_rotary(RotaryArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) dwa[i] = dwb[i] = 0.f;
   }
-  for (long long t0 = (long long)wg * a.tokens; t0 < rows; t0 += (long long)pt.wgs * a.tokens) {
+  // A workgroup's place in a whole round of tiles moves on from one to the next, so that it
+  // comes to another part of a sequence, and not to the padding of every one or of none.
+  int place = wg;
+  for (int tile = wg; tile < a.tiles; tile += pt.wgs) {
+    const int round = tile - wg;
+    const long long t0 = (long long)(round + (round + pt.wgs <= a.tiles ? place : wg)) * a.tokens;
+    place += pt.move;
+    if (place >= pt.wgs) place -= pt.wgs;
     const int nt = (int)min((long long)a.tokens, rows - t0);
     __syncthreads();  // the last tokens' angles are read
     if (tid < nt) {
       const unsigned row = (unsigned)(t0 + tid), b = row / (unsigned)a.n;
       live_of[tid] = !a.len || (int)(row - b * a.n) < clampi(a.len[b], 0, a.n);
     }
+    __syncthreads();
     for (int i = tid; i < nt * R2; i += kThreads) {
       const int t = i / R2, f = i - t * R2;
+      if (!live_of[t]) continue;
       const long long row = t0 + t;
       const long long p = a.pos ? a.pos[row] : (int)((unsigned)row % (unsigned)a.n);
       const unsigned turn = (unsigned)(((unsigned long long)p * a.turns.t[f]) >> 32);
@@ -321,30 +317,32 @@ __global__ __launch_bounds__(kThreads) void k_rotary(RotaryArgs a) {
       const int tok = on ? t : 0;
       const long long row = t0 + tok, at = (long long)head * a.d * (int)sizeof(T);
       const bool live = on && live_of[tok];
-      Pairs<T, kVec> v, g;
+      Pairs v, g;
 #pragma unroll
       for (int i = 0; i < 8; ++i) v.a[i] = v.b[i] = 0.f;
-      if (live && (!kBack || norm)) load_pairs(v, reinterpret_cast<const T*>(pt.x + row * pt.xs + at), pl);
+      if (live && (!kBack || norm)) load_pairs<kVec>(v, reinterpret_cast<const T*>(pt.x + row * pt.xs + at), pl);
       T* o = reinterpret_cast<T*>(pt.o + row * pt.os + at);
       if constexpr (!kBack) {
-        if (norm) {
-          normalise(v, a, pl);
+        if (live && turned) {  // a head's lanes are live together
+          if (norm) {
+            normalise(v, a, pl);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            v.a[i] *= wa[i];
-            v.b[i] *= wb[i];
+            for (int i = 0; i < 8; ++i) {
+              v.a[i] *= wa[i];
+              v.b[i] *= wb[i];
+            }
           }
+          rotate(v, cs[tok], sn[tok], pl);
         }
-        if (turned && live) rotate(v, cs[tok], sn[tok], pl, whole);
-        if (on) store_pairs(v, o, pl);
+        if (on) store_pairs<kVec>(v, o, pl);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) g.a[i] = g.b[i] = 0.f;
         if (live) {
-          load_pairs(g, reinterpret_cast<const T*>(pt.g + row * pt.gs + at), pl);
-          if (turned) rotate(g, cs[tok], sn[tok], pl, whole);
+          load_pairs<kVec>(g, reinterpret_cast<const T*>(pt.g + row * pt.gs + at), pl);
+          if (turned) rotate(g, cs[tok], sn[tok], pl);
         }
-        if (norm) {
+        if (norm && live) {
           const float inv = normalise(v, a, pl);
           float gh = 0.f, gs = 0.f;
 #pragma unroll
@@ -361,11 +359,11 @@ __global__ __launch_bounds__(kThreads) void k_rotary(RotaryArgs a) {
           gs = a.rms ? 0.f : head_sum(gs, lanes) * scale;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            g.a[i] = live ? inv * (g.a[i] - fmaf(v.a[i], gh, gs)) : 0.f;
-            g.b[i] = live ? inv * (g.b[i] - fmaf(v.b[i], gh, gs)) : 0.f;
+            g.a[i] = inv * (g.a[i] - fmaf(v.a[i], gh, gs));
+            g.b[i] = inv * (g.b[i] - fmaf(v.b[i], gh, gs));
           }
         }
-        if (on) store_pairs(g, o, pl);
+        if (on) store_pairs<kVec>(g, o, pl);
       }
       item += step;
       t += dt;
@@ -440,12 +438,22 @@ int tokens_of(long long rows, int d, int heads) {
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
-template <typename T, bool kVec, bool kBack>
+template <typename T, int kVec, bool kBack>
 void start(const RotaryArgs& a, int grid, int interleaved, hipStream_t s) {
   if (interleaved)
     hipLaunchKernelGGL((k_rotary<T, kVec, true, kBack>), dim3(grid), dim3(kThreads), 0, s, a);
   else
     hipLaunchKernelGGL((k_rotary<T, kVec, false, kBack>), dim3(grid), dim3(kThreads), 0, s, a);
+}
+
+template <typename T, bool kBack>
+void start(const RotaryArgs& a, int width, int grid, int interleaved, hipStream_t s) {
+  if (width == 8)
+    start<T, 8, kBack>(a, grid, interleaved, s);
+  else if (width == 4)
+    start<T, 4, kBack>(a, grid, interleaved, s);
+  else
+    start<T, 0, kBack>(a, grid, interleaved, s);
 }
 
 template <bool kBack>
@@ -459,7 +467,8 @@ hipError_t run(const Rotary& r, hipStream_t s) {
   const float* ws[3] = {r.q_w, r.k_w, nullptr};
   float* dw[3] = {r.dq_w, r.dk_w, nullptr};
   a.tokens = tokens_of(rows, r.d, std::max(r.Hq, r.Hk));
-  const long long tiles = (rows + a.tokens - 1) / a.tokens;
+  const long long tiles = (rows + a.tokens - 1) / a.tokens;  // below 2^28: 16 tokens each where there are many
+  a.tiles = (int)tiles;
   bool vec = true;
   float* part = r.ws;
   WeightSums sums = {};
@@ -477,6 +486,10 @@ hipError_t run(const Rotary& r, hipStream_t s) {
     p.w = ws[i];
     p.part = nullptr;
     p.wgs = os[i] ? (int)std::min<long long>(tiles, kBack && dw[i] ? kWeightWgs : 1 << 16) : 0;
+    // 5 / 13 of a sequence further from round to round (64 x 1024 rows, a third of them valid,
+    // 16 + 4 + 4 heads of 64, backward with RMS norms: 107 us, with rounds of whole sequences 134)
+    const int per = std::max(1, r.n / a.tokens);
+    p.move = p.wgs ? ((5 * per / 13 - p.wgs) % per + per) % per % p.wgs : 0;
     grid += p.wgs;
     if (kBack && dw[i]) {
       p.part = part;
@@ -488,8 +501,14 @@ hipError_t run(const Rotary& r, hipStream_t s) {
     if (os[i])
       vec = vec && aligned16(xs[i]) && aligned16(gs[i]) && aligned16(os[i]) && ld[i] * e % 16 == 0 && dense * e % 16 == 0;
   }
-  // sixteen elements of a lane as vectors: of the rotated part or of the rest, not both
-  vec = vec && r.d % 16 == 0 && (r.interleaved || r.R % 16 == 0);
+  // The pairs of a vector are all of the rotated part, or all of the rest (heads of 80 with 40
+  // rotated, halves, bf16, 16384 rows of 48: 68 us by 4 pairs, 178 by elements).
+  auto fits = [&](int pairs) { return r.d % (2 * pairs) == 0 && (r.interleaved || r.R % (2 * pairs) == 0); };
+  const int width = !vec ? 0 : fits(8) ? 8 : fits(4) ? 4 : 0;
+  // Workgroups of the same tokens follow one another where the parts are alike (a call of
+  // 65536 rows, a third of them valid, 12 + 12 + 12 heads of 64: 97 us, part after part 115);
+  // otherwise the longest part goes first (32768 rows of 16 + 4 + 4 heads of 128: 97, in turn 103).
+  a.in_turn = a.part[0].wgs == a.part[1].wgs && a.part[0].wgs == a.part[2].wgs && r.Hq == r.Hk;
   a.len = r.len;
   a.pos = r.pos;
   a.B = r.B;
@@ -502,16 +521,10 @@ hipError_t run(const Rotary& r, hipStream_t s) {
   a.eps = r.eps;
   a.amplitude = r.amplitude;
   a.turns = r.turns;
-  if (r.f32) {
-    if (vec)
-      start<float, true, kBack>(a, grid, r.interleaved, s);
-    else
-      start<float, false, kBack>(a, grid, r.interleaved, s);
-  } else if (vec) {
-    start<__bf16, true, kBack>(a, grid, r.interleaved, s);
-  } else {
-    start<__bf16, false, kBack>(a, grid, r.interleaved, s);
-  }
+  if (r.f32)
+    start<float, kBack>(a, width, grid, r.interleaved, s);
+  else
+    start<__bf16, kBack>(a, width, grid, r.interleaved, s);
   if (sums.out[0] || sums.out[1])
     hipLaunchKernelGGL(k_rotary_weights, dim3((r.d + 15) / 16, 2), dim3(256), 0, s, sums, r.d);
   return hipGetLastError();

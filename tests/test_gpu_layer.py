@@ -805,3 +805,20 @@ def test_ffn_joined_products(B, n, D, F, lens):
     for nm, v in out.items():
         alone = sc.sc_gated_ffn_backward(d, x, wg, wu, wd, saved, dy, grads={nm: torch.empty_like(v)})[nm]
         assert torch.equal(alone, v), nm
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("B,n,Hq,Hk,d,R,dtype,layout", [
+    (2, 40, 4, 4, 80, 40, "bf16", HALF), (2, 40, 4, 2, 80, 40, "f32", HALF), (1, 50, 3, 3, 24, 8, "bf16", HALF),
+    (1, 50, 3, 1, 88, 24, "f32", INTER), (1, 50, 3, 3, 40, 40, "bf16", INTER), (2, 30, 2, 2, 76, 20, "bf16", HALF)])
+def test_rotary_vectors_of_four_pairs(B, n, Hq, Hk, d, R, dtype, layout, backward):
+    """Halves that end inside a lane's eight pairs."""
+    rotary_case(B, n, Hq, Hk, d, R, dtype, True, layout, sc.SC_NORM_RMS, lens=(n, n - 3), backward=backward)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("Hq,Hk", [(2, 2), (3, 1)])
+def test_rotary_many_padded_sequences(Hq, Hk, backward):
+    """Several rounds of tiles, most of them padding."""
+    rotary_case(40, 512, Hq, Hk, 64, 32, "bf16", True, HALF, sc.SC_NORM_RMS, lens=[(37 * i) % 300 for i in range(40)],
+                backward=backward)
