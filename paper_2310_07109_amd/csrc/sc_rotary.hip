@@ -5,12 +5,11 @@
 //   dx = inv (g - hat mean(g hat) - mean(g)),  g = w du,  hat = (x - mean) inv
 //   (mean only for LayerNorm), dw = sum du hat.
 //
-// One read and one write of every head bound it: 32768 rows of 12 + 12 + 12 heads of 64, bf16,
-// 63 us for 302 MB (4.8 TB/s, where a copy reaches 5.1), of 65536 rows, a third of them valid,
-// 80 us for 413 MB; backward with RMS norms, 32768 rows of 16 + 4 + 4 heads, 62 us for 285 MB
-// (4.6).  A lane holds eight pairs of a head, both halves of each, so the rotation is within a
-// lane and d / 16 lanes (rounded up to a power of two) hold a head; its sums go over them by
-// DPP.
+// One read and one write of every head bound it: 65536 rows of 12 + 12 + 12 heads of 64, bf16,
+// a third of them valid, 80 us for 413 MB (5.2 TB/s, as a copy; 91 in the median of calls back
+// to back); backward with RMS norms, 32768 rows of 16 + 4 + 4 heads, 62 us for 285 MB (4.6).
+// A lane holds eight pairs of a head, both halves of each, so the rotation is within a lane
+// and d / 16 lanes (rounded up to a power of two) hold a head; its sums go over them by DPP.
 //
 // The angles of a token serve all its heads: a workgroup makes the cosines and sines
 // of its tokens once, in LDS.  An angle is a turn in 64-bit fixed point: position times
