@@ -822,3 +822,62 @@ def test_rotary_many_padded_sequences(Hq, Hk, backward):
     """Several rounds of tiles, most of them padding."""
     rotary_case(40, 512, Hq, Hk, 64, 32, "bf16", True, HALF, sc.SC_NORM_RMS, lens=[(37 * i) % 300 for i in range(40)],
                 backward=backward)
+
+
+# ------------------------------------------------------ activations everywhere ----
+@pytest.mark.parametrize("act", [sc.SC_ACT_NONE, sc.SC_ACT_GELU, sc.SC_ACT_SILU])
+@pytest.mark.parametrize("B,n,D,F,lens", [
+    (1, 1, 512, 776, None), (1, 17, 520, 768, (17,)), (2, 20, 504, 1032, (20, 9)), (16, 8, 768, 2304, (8, 4, 5, 1)),
+    (1, 129, 512, 768, None), (3, 501, 512, 1024, (501, 7, 0)), (1, 1500, 504, 1024, None),
+    (2, 2048, 512, 4096, (2048, 1999)), (1, 2048, 512, 4096, None)])
+def test_ffn_activations(B, n, D, F, lens, act):
+    """Every activation with and without what is kept, from one row to tiles of every kind; a form with gate and up
+    exchanged, or with another activation, is beyond the tolerance of the norm, which is the module's.
+
+    A value's tolerance: two roundings to bf16 behind it, (1 + 2^-8)^2 - 1 of the products' magnitudes at most, and 2^-13
+    for the activation's 3e-5, the kept factors' 2^-15 and float32 products.  To that the float32 sums add, where they
+    cancel (g of 1.5e-6 from 512 products of magnitude 28): K additions of partial sums that are never above the sum A
+    of the magnitudes are off by K u A.  So g, u and dh are off by e = D u A; act(g) by 1.13 e_g + 1e-6 and its slope by
+    0.8 e_g + 2e-6 (the largest slopes of the activations and of their slopes, and their own errors next to 0), which
+    the products pass on to h, dg and du, and the last sums to the results, with K u of their own magnitudes."""
+    g_ = gen(B + D + act)
+    L_dev, L = lens_of(lens, B, n)
+    m = valid_mask(L, n).to(DEV)
+    x, dy = (torch.randn((B, n, D), generator=g_).to(torch.bfloat16).to(DEV) for _ in range(2))
+    w = [(torch.randn(s, generator=g_) * k / math.sqrt(s[0])).to(torch.bfloat16).to(DEV)
+         for s, k in (((D, F), 2), ((D, F), 2), ((F, D), 1))]
+    d = sc.FfnDesc(B, n, D, F, valid_len=L_dev, act=act)
+    y, _ = sc.sc_gated_ffn(d, x, *w)
+    y_kept, saved = sc.sc_gated_ffn(d, x, *w, saved=True)
+    out = sc.sc_gated_ffn_backward(d, x, *w, saved, dy)
+    xs, ds = x[m].double(), dy[m].double()
+    wg, wu, wd = (t.double() for t in w)
+    g, u = xs @ wg, xs @ wu
+    a, slope = act64(act, g)
+    h, dh = a * u, ds @ wd.t()
+    dg, du = dh * u * slope, dh * a
+    A = torch.abs
+    eg, eu, edh = D * U * (A(xs) @ A(wg)), D * U * (A(xs) @ A(wu)), D * U * (A(ds) @ A(wd).t())
+    ea, es = 1.13 * eg + 1e-6, 0.8 * eg + 2e-6
+    eh, edu = ea * A(u) + A(a) * eu, A(a) * edh + A(dh) * ea
+    edg = A(u * slope) * edh + A(dh) * (A(slope) * eu + A(u) * es)
+    R = xs.shape[0]
+
+    def wide(v, e, right, K):
+        return (2 * 2.0 ** -8 + 2.0 ** -13 + K * U) * (A(v) @ A(right)) + 1.01 * (e @ A(right))
+    want = dict(y=(h @ wd, wide(h, eh, wd, F)),
+                dx=(dg @ wg.t() + du @ wu.t(), wide(dg, edg, wg.t(), 2 * F) + wide(du, edu, wu.t(), 2 * F)),
+                dwg=(xs.t() @ dg, wide(dg.t(), edg.t(), xs, R).t()), dwu=(xs.t() @ du, wide(du.t(), edu.t(), xs, R).t()),
+                dwd=(h.t() @ ds, wide(h.t(), eh.t(), ds, R)))
+    want["y_kept"] = want["y"]
+    for nm, (v, tol) in want.items():
+        got = dict(out, y=y, y_kept=y_kept)[nm].double()
+        if nm in ("y", "y_kept", "dx"):
+            assert not got[~m].any(), nm
+            got = got[m]
+        assert float((got - v).norm()) <= 0.0035 * float(v.norm()), nm
+        assert_close(got, v.cpu(), tol.cpu(), nm)
+    for other, (gate, up) in ((act, (u, g)), ((act + 1) % 3, (g, u))):
+        wrong = (act64(other, gate)[0] * up) @ wd
+        if other != act or act != sc.SC_ACT_NONE:  # without an activation the product is symmetric
+            assert float((wrong - want["y"][0]).norm()) > 0.01 * float(wrong.norm())
