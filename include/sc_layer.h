@@ -127,7 +127,7 @@ typedef struct sc_ffn_desc {
 size_t sc_gated_ffn_workspace_size(const sc_ffn_desc *desc, int32_t save);
 
 /* Bytes of what the backward needs of the forward, of the valid rows: h, and
- * act(g) and u act'(g) cut to 24 bits, in a layout private to the library. */
+ * act(g) and u act'(g) rounded to 24 bits, in a layout private to the library. */
 size_t sc_gated_ffn_saved_size(const sc_ffn_desc *desc);
 
 /*

@@ -171,9 +171,11 @@ struct FfnPart {
 };
 
 // ------------------------------------------------------------ results ----
-// 24 of a float32's bits, four values in three words, and back.
+// Float32 rounded to 24 bits (the nearest, halves away from 0: 2^-16 of a value at most, where
+// a cut would take up to 2^-15 off every one), four values in three words, and back.  Infinities
+// stay, and so do NaNs: bf16's and the hardware's own have no low bits that could carry.
 SC_DEV void pack24(const f32x4& v, unsigned* w) {
-  const u32x4 u = __builtin_bit_cast(u32x4, v);
+  const u32x4 u = __builtin_bit_cast(u32x4, v) + 0x80u;
   w[0] = __builtin_amdgcn_perm(u[1], u[0], 0x05030201u);
   w[1] = __builtin_amdgcn_perm(u[2], u[1], 0x06050302u);
   w[2] = __builtin_amdgcn_perm(u[3], u[2], 0x07060503u);

@@ -881,3 +881,23 @@ def test_ffn_activations(B, n, D, F, lens, act):
         wrong = (act64(other, gate)[0] * up) @ wd
         if other != act or act != sc.SC_ACT_NONE:  # without an activation the product is symmetric
             assert float((wrong - want["y"][0]).norm()) > 0.01 * float(wrong.norm())
+
+
+@pytest.mark.parametrize("T,F,row", [(1, 8, 0), (300, 8, 7), (1500, 1000, 1400), (4096, 4096, 4000)])
+def test_ffn_kept_factors_are_rounded(T, F, row):
+    """What is kept of g and u is rounded to the nearest of 24 bits, not cut: 3 * 2^-17 beside a tie of bf16 at 1 to 2,
+    more than half of the 2^-15 between neighbours, stays on its side, for either sign and either even neighbour."""
+    D = 8
+    x = torch.tensor([1, 2.0 ** -7, 2.0 ** -8, 3 * 2.0 ** -17, 0, 0, 0, 0])
+    cols = [[s, s * odd, s, s * side, 0, 0, 0, 0] for s in (1, -1) for odd in (0, 1) for side in (1, -1)]
+    wu = torch.tensor(cols).t().float().repeat(1, F // 8)
+    wg = wu.roll(3, 1)
+    wd, dy = torch.zeros((F, D)), torch.zeros((1, T, D))
+    wd[:, 0], dy[0, row, 0] = 1, 1  # dh = 1 in one row
+    dev = [t.to(torch.bfloat16).to(DEV) for t in (x.expand(1, T, D), wg, wu, wd)]
+    d = sc.FfnDesc(1, T, D, F, act=sc.SC_ACT_NONE)
+    _, saved = sc.sc_gated_ffn(d, *dev, saved=True)
+    out = sc.sc_gated_ffn_backward(d, *dev, saved, dy.to(torch.bfloat16).to(DEV))
+    for nm, w in (("dwg", wu), ("dwu", wg)):
+        want = (x @ w).to(torch.bfloat16)  # exact in float32
+        assert torch.equal(out[nm][0].cpu(), want), nm
