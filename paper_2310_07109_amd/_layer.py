@@ -77,6 +77,26 @@ def _heads(call, desc, t, name, part, dt):
     raise ValueError(f"{name}: on {t.device}, the call's stream on device {call.device}")
 
 
+def _default_heads(desc, call, outer, steps, dt):
+    """New gradients of the parts whose `outer` are given, steps[part] elements between tokens (None: any).  Parts of
+    rows wider than themselves lie side by side in rows of one array, q, k, v, as far as they fit."""
+    outs, rows, wide, at = [], None, 0, 0
+    for part, (g, step) in enumerate(zip(outer, steps)):
+        shape = (desc.B, desc.n, desc.heads(part), desc.d)
+        row = shape[2] * desc.d
+        fits = rows is not None and step in (None, wide) and at + row <= wide
+        if g is None:
+            outs.append(None)
+        elif step == row or (step is None and not fits):
+            outs.append(call.new(dt, shape))
+        else:
+            if not fits:
+                rows, wide, at = call.new(dt, (desc.B * desc.n * step,)), step, 0
+            outs.append(rows.as_strided(shape, (desc.n * wide, wide, desc.d, 1), at))
+            at += row
+    return outs
+
+
 def _rotary_common(desc, call, q_w, k_w, positions):
     import torch
     call.lengths(desc.valid_len, desc.B)
@@ -119,7 +139,8 @@ def sc_rotary_backward(desc: RotaryDesc, freq, dq_out=None, dk_out=None, dv_out=
     absent: a weight that was not given has no gradient.
 
     q, k: the forward's inputs, with desc.norm only.  grads: optional dict of preallocated outputs, of which dq, dk, dv
-    may be parts of fused rows laid out as q, k, v; only those it names are computed."""
+    may be parts of fused rows laid out as q, k, v; only those it names are computed.  Without, dq, dk and dv are dense,
+    or, where q and k are parts of fused rows, lie side by side in rows of that width of one array."""
     import torch
     L = load()
     dt, f32 = _float_type(desc.dtype, "dtype"), torch.float32
@@ -133,26 +154,20 @@ def sc_rotary_backward(desc: RotaryDesc, freq, dq_out=None, dk_out=None, dv_out=
             raise ValueError(f"grads: unknown outputs {sorted(unknown)}")
     out = {}
     strides, gptr, optr, iptr = [], [], [], []
-    for part, (g, nm) in enumerate(zip(outer, names)):
+    outs = outer if grads is None else [grads.get(nm) for nm in names]
+    ins = [_heads(call, desc, x, "qkv"[part], part, dt) if desc.norm and x is not None and outs[part] is not None
+           else (None, None) for part, x in enumerate((q, k, None))]
+    if grads is None:
+        outs = _default_heads(desc, call, outer, [s for _, s in ins], dt)
+    for part, (g, nm, o, (px, sx)) in enumerate(zip(outer, names, outs, ins)):
         shape = (desc.B, desc.n, desc.heads(part), desc.d)
-        o = call.new(dt, shape) if grads is None and g is not None else (grads or {}).get(nm)
         if o is not None and g is None:
             raise ValueError(f"{nm}: needs {nm}_out")
         po, step = _heads(call, desc, o, nm, part, dt)
-        x = (q, k, None)[part] if desc.norm and o is not None else None
-        if x is not None:
-            px, sx = _heads(call, desc, x, "qkv"[part], part, dt)
-            if sx != step:
-                if grads is None:  # gradients laid out as their inputs, in rows of their own
-                    o = torch.empty(desc.B * desc.n * sx, dtype=dt, device=x.device).as_strided(
-                        shape, (desc.n * sx, sx, desc.d, 1))
-                    po, step = o.data_ptr(), sx
-                else:
-                    raise ValueError(f"{nm}: {step} elements between tokens, {sx} in {'qkv'[part]}")
-            iptr.append(px)
-        else:
-            iptr.append(None)
+        if px is not None and sx != step:
+            raise ValueError(f"{nm}: {step} elements between tokens, {sx} in {'qkv'[part]}")
         out[nm] = o
+        iptr.append(px)
         strides.append(step)
         optr.append(po)
         gptr.append(call.opt(g, nm + "_out", dt, shape) if o is not None else None)

@@ -901,3 +901,45 @@ def test_ffn_kept_factors_are_rounded(T, F, row):
     for nm, w in (("dwg", wu), ("dwu", wg)):
         want = (x @ w).to(torch.bfloat16)  # exact in float32
         assert torch.equal(out[nm][0].cpu(), want), nm
+
+
+@pytest.mark.parametrize("Hq,Hk,pad,which", [(4, 2, 0, "qkv"), (4, 2, 8, "qkv"), (3, 3, 0, "qk"), (2, 2, 0, "kv"),
+                                            (2, 2, 16, "q")])
+def test_rotary_default_gradients_share_rows(Hq, Hk, pad, which):
+    """Gradients that the call allocates for parts of fused rows lie side by side in one array of such rows, no larger
+    than what it is the gradient of; parts of rows of different widths, or too wide for one row, in rows of their own."""
+    B, n, d = 3, 21, 64
+    W = (Hq + 2 * Hk) * d + pad
+    rows = torch.randn((B, n, W), generator=gen(21)).to(torch.bfloat16).to(DEV)
+    cut = (0, Hq * d, (Hq + Hk) * d, (Hq + 2 * Hk) * d)
+    parts = [rows[..., cut[i]:cut[i + 1]].unflatten(-1, (-1, d)) for i in range(3)]
+    go = [torch.randn((B, n, h, d), generator=gen(h)).to(torch.bfloat16).to(DEV) if nm in which else None
+          for nm, h in zip("qkv", (Hq, Hk, Hk))]
+    freq, _ = sc.sc_rotary_frequencies(d)
+    D = sc.RotaryDesc(B, n, Hq, Hk, norm=True)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    out = sc.sc_rotary_backward(D, freq, *go, q=parts[0], k=parts[1])
+    size = (B * n * W * 2 + 511) // 512 * 512  # the allocator's granularity
+    assert torch.cuda.memory_allocated() - before <= size
+    want = sc.sc_rotary_backward(D, freq, *go, q=parts[0].contiguous(), k=parts[1].contiguous())
+    have = [nm for nm in ("dq", "dk", "dv") if out[nm] is not None]
+    assert have == ["d" + nm for nm in which]
+    for nm in have:
+        assert torch.equal(out[nm], want[nm])
+        assert out[nm].untyped_storage().data_ptr() == out[have[0]].untyped_storage().data_ptr()
+    if which == "qkv":  # together they are the gradient of the fused rows
+        fused = out["dq"].as_strided((B, n, W), (n * W, W, 1))
+        assert torch.equal(fused[..., :W - pad], torch.cat([want[nm].flatten(-2) for nm in have], -1))
+    # rows of other widths
+    k2 = torch.randn((B, n, Hk * d + 8), generator=gen(22)).to(torch.bfloat16).to(DEV)[..., :Hk * d].unflatten(-1, (-1, d))
+    a = sc.sc_rotary_backward(D, freq, *go, q=parts[0], k=k2)
+    b = sc.sc_rotary_backward(D, freq, *go, q=parts[0].contiguous(), k=k2.contiguous())
+    assert all(torch.equal(a[nm], b[nm]) for nm in have)
+    # rows that hold one part and no second one
+    q2 = torch.randn((2, B, n, Hk * d + 8), generator=gen(23)).to(torch.bfloat16).to(DEV)[..., :Hk * d].unflatten(-1, (-1, d))
+    E, g2 = sc.RotaryDesc(B, n, Hk, Hk, norm=True), torch.randn((3, B, n, Hk, d), generator=gen(24)).to(torch.bfloat16).to(DEV)
+    a = sc.sc_rotary_backward(E, freq, *g2, q=q2[0], k=q2[1])
+    b = sc.sc_rotary_backward(E, freq, *g2, q=q2[0].contiguous(), k=q2[1].contiguous())
+    assert all(torch.equal(a[nm], b[nm]) for nm in ("dq", "dk", "dv"))
+    assert a["dq"].untyped_storage().data_ptr() != a["dk"].untyped_storage().data_ptr()
