@@ -138,7 +138,9 @@ size_t sc_gated_ffn_saved_size(const sc_ffn_desc *desc);
  *   saved    sc_gated_ffn_saved_size() bytes for sc_gated_ffn_backward, or NULL.
  *   workspace  sc_gated_ffn_workspace_size(desc, saved != NULL) bytes.
  * Tensors, saved and workspace are aligned to 16 bytes.  A row's result does not
- * depend on the other rows' values; the order of its sums goes by the sizes.
+ * depend on the other rows' values or on valid_len; the order of its sums goes by
+ * the sizes and, where B n <= 128, by whether `saved` is given too (y with and
+ * without it may then differ in a rounding).
  * Errors: SC_EINVAL (null pointers, sizes, types, alignment, y, saved or
  * workspace overlapping anything), SC_EUNSUPPORTED (dtype SC_F32; B n >= 2^31;
  * with valid_len, B > 8192; tensors of 4 GiB: with D and F rounded up to 8,

@@ -943,3 +943,30 @@ def test_rotary_default_gradients_share_rows(Hq, Hk, pad, which):
     b = sc.sc_rotary_backward(E, freq, *g2, q=q2[0].contiguous(), k=q2[1].contiguous())
     assert all(torch.equal(a[nm], b[nm]) for nm in ("dq", "dk", "dv"))
     assert a["dq"].untyped_storage().data_ptr() != a["dk"].untyped_storage().data_ptr()
+
+
+@pytest.mark.parametrize("act", [sc.SC_ACT_GELU, sc.SC_ACT_SILU])
+@pytest.mark.parametrize("B,n,D,F", [(2, 16, 256, 520), (2, 64, 256, 520), (2, 65, 256, 520), (2, 700, 500, 1111),
+                                     (2, 1024, 512, 4096)])
+def test_ffn_rows_by_themselves(B, n, D, F, act):
+    """A row's bits depend neither on other rows, NaNs and infinities among them, nor on the lengths; beyond 128 rows, nor
+    on whether anything is kept."""
+    g = gen(n)
+    x = torch.randn((B, n, D), generator=g).to(torch.bfloat16).to(DEV)
+    w = [(torch.randn(s, generator=g) / math.sqrt(s[0])).to(torch.bfloat16).to(DEV) for s in ((D, F), (D, F), (F, D))]
+    other = torch.randn((B, n, D), generator=g).to(torch.bfloat16).to(DEV)
+    other[:, 1::4], other[:, 3::8] = float("nan"), float("inf")
+    other[:, ::2] = x[:, ::2]
+    L = torch.tensor([n, n // 2], dtype=torch.int32, device=DEV)
+    ys = {}
+    for kept in (False, True):
+        y = ys[kept] = sc.sc_gated_ffn(sc.FfnDesc(B, n, D, F, act=act), x, *w, saved=kept)[0]
+        assert bool(y.isfinite().all())
+        assert torch.equal(sc.sc_gated_ffn(sc.FfnDesc(B, n, D, F, act=act), other, *w, saved=kept)[0][:, ::2], y[:, ::2])
+        r = sc.sc_gated_ffn(sc.FfnDesc(B, n, D, F, act=act, valid_len=L), x, *w, saved=kept)[0]
+        assert torch.equal(r[0], y[0]) and torch.equal(r[1, :n // 2], y[1, :n // 2]) and not r[1, n // 2:].any()
+    if B * n > 128:
+        assert torch.equal(ys[False], ys[True])
+    else:  # rounded once more, from sums and an h that differ in a rounding
+        a, b = ys[False].double(), ys[True].double()
+        assert float((a - b).norm()) <= 2 * 0.0035 * float(b.norm())
