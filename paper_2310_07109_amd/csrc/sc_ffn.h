@@ -13,13 +13,18 @@
 //   kDwgu  dWg = x^T dg, dWu = x^T du
 //
 // A tile is BM x BN of a workgroup of eight waves; a stage is 64 of the contraction.
-// Sums are float32 in ascending order of the contraction, whatever the tile.
+// Sums are float32 in ascending order of the contraction, whatever the tile.  What the next
+// product reads, h, dg and du, is rounded to bf16, as the matrix units take it (a second bf16
+// part of each would be two thirds as many products again in a training step); y and every
+// gradient then have two roundings behind them, 0.0023 of their norm off where float32 in
+// between would leave 0.0017.
 //
 // The matrix units bound them, at the clock that their power leaves, and beside them the
 // results, which one workgroup a CU does not overlap with products.  32768 rows, D 1024,
-// F 2816, us (PFLOP/s): gate and its factors 390 (0.97), down 180 (1.05), dh and dWd 474
-// (0.80, with 738 MB of factors and results of dh; apart 325 and 164), dx, dWg and dWu 643
-// (1.18; apart 300 and 341); gate alone, F 4096, 447 (1.23), down 225 (1.22).  A library's
+// F 2816, least of 20, us (PFLOP/s): gate and its factors 390 (0.97), down 177 (1.07), dh and
+// dWd 463 (0.82; apart 333 and 160), dx, dWg and dWu 638 (1.18; apart 296 and 342); gate
+// alone, F 4096, 447 (1.23), down 225 (1.22).  dh is as long as its products (160, as dWd's)
+// and a copy of its 923 MB of factors and results (180) one after the other.  A library's
 // products of such shapes reach 0.86 to 1.46 without the activation.
 #pragma once
 #include "sc_act.h"
@@ -648,6 +653,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
 // the slabs; those that are left over go to the first workgroups, and the others take `ratio`
 // tiles of kRow for each.  Every second workgroup begins with its tiles of kRow, so that the
 // results of some are written during the products of others.
+//
+// With 256 x 256 tiles the state of both products is more than a lane's 256 registers: 9 (dh
+// with dWd) and 8 (dx with dWg, dWu) of them lie in scratch, and their reloads wait for loads
+// and stores in flight; the four products apart have none there.  The medians of 20, joined
+// and apart, are still even or better joined: 32768 rows of 1024 x 2816, 480 us and 345 + 165,
+// 657 and 307 + 348; 16384 of 768 x 2048, 176 and 117 + 57, 205 and 109 + 97.
 template <int kRow, int kSum, int kM>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_ffn_two(FfnArgs a, FfnArgs b, int ratio) {
   using P = FfnProduct<kRow, kM, kActNone>;
