@@ -970,3 +970,18 @@ def test_ffn_rows_by_themselves(B, n, D, F, act):
     else:  # rounded once more, from sums and an h that differ in a rounding
         a, b = ys[False].double(), ys[True].double()
         assert float((a - b).norm()) <= 2 * 0.0035 * float(b.norm())
+
+
+@pytest.mark.parametrize("B,n,Hq,Hk", [(5, 1, 2, 2), (1, 1, 2, 1), (1, 9, 1, 1), (6, 1, 1, 1)])
+def test_rotary_default_gradients_of_few_tokens(B, n, Hq, Hk):
+    """One token, one sequence, one head: sizes whose strides say nothing."""
+    W = (Hq + 2 * Hk) * 64
+    rows = torch.randn((B, n, W), generator=gen(31)).to(torch.bfloat16).to(DEV)
+    q, k, _ = (t.unflatten(-1, (-1, 64)) for t in rows.split((Hq * 64, Hk * 64, Hk * 64), -1))
+    go = [torch.randn((B, n, h, 64), generator=gen(h)).to(torch.bfloat16).to(DEV) for h in (Hq, Hk, Hk)]
+    freq, _ = sc.sc_rotary_frequencies(64)
+    D = sc.RotaryDesc(B, n, Hq, Hk, norm=True)
+    w = dict(q_w=torch.rand(64, generator=gen(32)).to(DEV), k_w=torch.rand(64, generator=gen(33)).to(DEV))
+    a = sc.sc_rotary_backward(D, freq, *go, q=q, k=k, **w)
+    b = sc.sc_rotary_backward(D, freq, *go, q=q.contiguous().clone(), k=k.contiguous().clone(), **w)
+    assert all(torch.equal(a[nm], b[nm]) for nm in b)
